@@ -278,6 +278,111 @@ int srft_kv_channel_absmax(const srft_plan_t* plan, const void* x_f16_dev, int64
  */
 int srft_lambda_from_absmax(const float* amax_host, int d, float* lambda_host);
 
+/*
+ * Rotary positions on rows of heads, several tensors of the same tokens in one call (queries and keys).
+ * The first `rot` channels of a row are rot / 2 pairs (a, b); with t = positions[token] * freq[pair]
+ *     a' = factor (a cos t - b sin t),   b' = factor (a sin t + b cos t);   the channels from rot on are copied.
+ * inverse != 0 turns by -t: with the same factor that is the gradient of the call with inverse = 0.
+ *   rows        HOST array of `count` tensors (1 .. SRFT_ROTARY_MAX), each [n_tokens][n_heads][d] in in_dev and out_dev with the
+ *               given strides in elements (the channels next to each other).  out_dev == in_dev with the same strides and type
+ *               turns in place; overlapping otherwise is not allowed.  Every pointer is aligned to its element.
+ *   layout      SRFT_ROTARY_HALF: pair i is channels i and i + rot / 2.  SRFT_ROTARY_PAIRS: channels 2 i and 2 i + 1.
+ *   positions_dev  [n_tokens] int32;  freq_dev [rot / 2] fp64, radians per token (of a long context: whatever scaling the
+ *               model takes, srft_rotary knows of none).  Angles are formed and reduced in 64 bits.
+ * d even, 2 <= d <= 1024, rot even, 0 <= rot <= d, types of srft_dtype, n_tokens * n_heads < 2^31 (else SRFT_ERR_BAD_N).  n_tokens == 0 is
+ * a successful no-op.  One kernel.
+ */
+typedef enum srft_dtype { SRFT_F32 = 0, SRFT_F16 = 1, SRFT_BF16 = 2 } srft_dtype;
+typedef enum srft_rotary_layout { SRFT_ROTARY_HALF = 0, SRFT_ROTARY_PAIRS = 1 } srft_rotary_layout;
+enum { SRFT_ROTARY_MAX = 4 };
+typedef struct srft_rotary_rows {
+    const void* in_dev;
+    void* out_dev;
+    int64_t in_token, in_head, out_token, out_head;          /* strides in elements */
+    int32_t n_heads;
+    int32_t in_type, out_type;                               /* srft_dtype */
+    int32_t reserved;                                        /* 0 */
+} srft_rotary_rows;
+int srft_rotary(const srft_rotary_rows* rows, int count, int64_t n_tokens, int d, int rot, int layout,
+                const int32_t* positions_dev, const double* freq_dev, double factor, int inverse, void* hip_stream);
+
+/*
+ * Paged cache of one layer: a pool of pages for K and one for V, shared by sequences of any length.     (Sec. 7.2, with the pages of
+ * a sequence in any order.)  A page holds R = page_tokens tokens of n_heads key heads as the plans' record; the tokens behind a
+ * sequence's last full page are exact fp16 in a window of R tokens, as in srft_cache, and become a page when the window is full:
+ *     codes_dev   [n_pages][n_heads][R][d/2] bytes ([d] at 8 bits)      scales_dev  [n_pages][n_heads][R][d/g] fp32
+ *     window_dev  [n_windows][n_heads][R][d] fp16                       (all 16-byte aligned)
+ * All device buffers are the caller's.  Which pages and windows a sequence has is the caller's bookkeeping (page tables on the device,
+ * read by the kernels, so that a step can be captured in a graph and replayed with other lengths).
+ *
+ * srft_pool_create   plan_k, plan_v: same d, group size, code width, transform and device.  page_tokens is 16, 32, 64, 128 or 256,
+ *                    n_heads * page_tokens a multiple of 32, n_pages and n_windows >= 1 (else SRFT_ERR_BAD_N).  Allocates device tables
+ *                    (8 d^2 bytes) on the plans' GPU.  The plans must outlive the pool.
+ */
+typedef struct srft_pool srft_pool_t;
+typedef struct srft_pool_buffers {
+    uint8_t* codes_dev;
+    float* scales_dev;
+    void* window_f16_dev;
+} srft_pool_buffers;
+int srft_pool_create(srft_pool_t** out, const srft_plan_t* plan_k, const srft_plan_t* plan_v, int n_heads, int page_tokens,
+                     int64_t n_pages, int64_t n_windows, const srft_pool_buffers* k, const srft_pool_buffers* v);
+int srft_pool_destroy(srft_pool_t* pool);        /* NULL is accepted; the buffers stay the caller's */
+
+/*
+ * The sequences of one call.  Sequence b brings the new tokens starts[b] .. starts[b + 1] - 1 (rows of k, v and q) and holds
+ * lengths[b] tokens with them; its token j lies in page page_table[b][j / R] if that page is full, else in window
+ * windows[b][1].  windows[b][0] is the window that it had before the call: where the call fills a page, windows[b][1] has to be
+ * another window than windows[b][0] (no other sequence's either), else it is the same.
+ * max_new and max_length bound what the device arrays hold: they size launches and workspaces.  What is beyond them is cut off;
+ * a page or window number out of range names no memory: its tokens are neither read nor written, and count for nothing.
+ * 0 <= n_seq <= 4096, 0 <= max_new, 0 <= max_length < 2^30, max_pages >= max_length / R (else SRFT_ERR_BAD_N).
+ */
+typedef struct srft_paged_seqs {
+    int32_t n_seq;
+    int32_t max_new;
+    int64_t max_length;
+    int64_t max_pages;               /* entries of a row of page_table */
+    const int32_t* page_table_dev;   /* [n_seq][max_pages] */
+    const int32_t* windows_dev;      /* [n_seq][2] */
+    const int32_t* lengths_dev;      /* [n_seq] */
+    const int32_t* starts_dev;       /* [n_seq + 1] */
+} srft_paged_seqs;
+
+/*
+ * Append: the pages that the new tokens fill are quantized out of the window and the new tokens (the record of srft_kv_quantize, bit for
+ * bit), the tokens behind them are copied into the window.  The result does not depend on how the tokens are split into calls.
+ *   k_f16_dev, v_f16_dev   [n_new][n_heads][d] fp16, 16-byte aligned, strides in elements, multiples of 8.
+ *   workspace_dev          srft_pool_append_workspace_bytes bytes, 16-byte aligned, overwritten.
+ */
+int64_t srft_pool_append_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, int64_t n_new);
+int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const void* k_f16_dev, const void* v_f16_dev,
+                     int64_t n_new, int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* workspace_dev,
+                     void* hip_stream);
+
+/*
+ * Attention of the new tokens over the cache that holds them: out = softmax(softmax_scale * q K^T) V, causal (the i-th of the n new
+ * tokens of a sequence of length L sees the tokens 0 .. L - n + i), query head h reading key head h / (n_q_heads / n_heads).  K and V
+ * are the read path's reconstruction before its fp16 rounding where a page is full, and the window's fp16 values behind it.  A row that
+ * sees nothing is zero.
+ *   q_dev, out_dev   [n_new][n_q_heads][d], both of `type` (SRFT_F16 or SRFT_BF16), 16-byte aligned, strides in elements, multiples of 8.
+ *   n_q_heads        a multiple of n_heads, at most 64 n_heads.
+ *   softmax_scale    finite.
+ *   workspace_dev    srft_pool_attention_workspace_bytes bytes, 256-byte aligned, overwritten.
+ */
+int64_t srft_pool_attention_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, int64_t n_new, int n_q_heads);
+int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, const void* q_dev, int type, int64_t n_new, int n_q_heads,
+                        int64_t q_token, int64_t q_head, float softmax_scale, void* out_dev, int64_t out_token, int64_t out_head,
+                        void* workspace_dev, void* hip_stream);
+
+/*
+ * Copies inside pools: page pages[i][0] to page pages[i][1] and window windows[i][0] to windows[i][1], K and V, in each of n_pools pools of
+ * one geometry (the layers of a model): what a fork or a compaction needs.  Device arrays [n][2] of int32.  No destination may be
+ * another destination or a source of the same call; a pair with a number out of range is skipped.  Up to 64 pools go into one launch.
+ */
+int srft_pool_copy(const srft_pool_t* const* pools, int n_pools, const int32_t* pages_dev, int64_t n_page_pairs,
+                   const int32_t* windows_dev, int64_t n_window_pairs, void* hip_stream);
+
 /* Plan introspection (host side, no HIP calls). */
 int srft_plan_d(const srft_plan_t* plan);             /* d, or a negative status */
 int srft_plan_group_size(const srft_plan_t* plan);    /* g */

@@ -34,6 +34,8 @@ EXPORTS = [
     "srft_plan_create_bits", "srft_plan_bits", "srft_plan_form", "srft_plan_create_ex",
     "srft_scores_workspace_bytes", "srft_kv_scores", "srft_kv_scores_static", "srft_kv_quantize_butterfly",
     "srft_attend_workspace_bytes", "srft_kv_attend", "srft_decode_attention_workspace_bytes", "srft_kv_decode_attention",
+    "srft_rotary", "srft_pool_create", "srft_pool_destroy", "srft_pool_append_workspace_bytes", "srft_pool_append",
+    "srft_pool_attention_workspace_bytes", "srft_pool_attention", "srft_pool_copy",
 ]
 
 
@@ -101,6 +103,14 @@ def lib() -> C.CDLL:
     L.srft_lambda_from_absmax.argtypes = [vp, ci, vp]
     L.srft_kv_quantize_batched.argtypes = [vp, vp, vp, vp, vp, ci, vp]
     L.srft_kv_dequantize_batched.argtypes = [vp, vp, vp, vp, vp, ci, vp]
+    L.srft_rotary.argtypes = [vp, ci, i64, ci, ci, ci, vp, vp, C.c_double, ci, vp]
+    L.srft_pool_create.argtypes = [C.POINTER(vp), vp, vp, ci, ci, i64, i64, vp, vp]
+    L.srft_pool_destroy.argtypes = [vp]
+    L.srft_pool_append_workspace_bytes.argtypes = [vp, vp, i64]
+    L.srft_pool_append.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp]
+    L.srft_pool_attention_workspace_bytes.argtypes = [vp, vp, i64, ci]
+    L.srft_pool_attention.argtypes = [vp, vp, vp, ci, i64, ci, i64, i64, C.c_float, vp, i64, i64, vp, vp]
+    L.srft_pool_copy.argtypes = [vp, ci, vp, i64, vp, i64, vp]
     for name in ("srft_plan_d", "srft_plan_group_size", "srft_plan_groups", "srft_plan_code_bytes"):
         getattr(L, name).argtypes = [vp]
     L.srft_plan_get_signs.argtypes = [vp, vp]
@@ -114,6 +124,8 @@ def lib() -> C.CDLL:
     L.srft_scores_workspace_bytes.restype = i64
     L.srft_attend_workspace_bytes.restype = i64
     L.srft_decode_attention_workspace_bytes.restype = i64
+    L.srft_pool_append_workspace_bytes.restype = i64
+    L.srft_pool_attention_workspace_bytes.restype = i64
     L.srft_cache_tokens.restype = i64
     L.srft_cache_quantized_tokens.restype = i64
     if _marshal is not None:
@@ -443,6 +455,176 @@ class Cache:
             self.close()
         except Exception:
             pass
+
+
+# ---------------------------------------------------------------------------- rotary positions
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+ROTARY_LAYOUTS = {"half": 0, "pairs": 1}
+
+
+class _RotaryRows(C.Structure):
+    _fields_ = [("in_dev", C.c_void_p), ("out_dev", C.c_void_p), ("in_token", C.c_int64), ("in_head", C.c_int64),
+                ("out_token", C.c_int64), ("out_head", C.c_int64), ("n_heads", C.c_int32), ("in_type", C.c_int32),
+                ("out_type", C.c_int32), ("reserved", C.c_int32)]
+
+
+def _rows(t: torch.Tensor, name: str) -> tuple[int, int, int]:
+    """Address and strides of a tensor [tokens, heads, d] whose channels lie next to each other."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in device memory")
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [tokens, heads, d] with its channels next to each other")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def srft_rotary(items, positions: torch.Tensor, freq: torch.Tensor, layout: str = "half", factor: float = 1.0, inverse: bool = False,
+                stream=None) -> None:
+    """Rotary positions on (x, out) pairs of tensors [tokens, heads, d] of the same tokens: the first 2 len(freq) channels are turned
+    by positions[token] * freq (int32, fp64 radians per token).  out may be x.  inverse=True is the gradient of inverse=False."""
+    items = list(items)
+    if not items:
+        return
+    n, _, d = items[0][0].shape
+    if positions.shape != (n,) or freq.dim() != 1:
+        raise ValueError("positions must be [tokens], freq one-dimensional")
+    rows = (_RotaryRows * len(items))()
+    for r, (x, y) in zip(rows, items):
+        if x.shape != y.shape or x.shape[0] != n or x.shape[2] != d:
+            raise ValueError("all tensors of a call must have the same tokens and channels, out the shape of x")
+        if x.dtype not in DTYPES or y.dtype not in DTYPES:
+            raise ValueError("rotary takes float32, float16 and bfloat16")
+        r.in_dev, r.in_token, r.in_head = _rows(x, "x")
+        r.out_dev, r.out_token, r.out_head = _rows(y, "out")
+        r.n_heads, r.in_type, r.out_type = x.shape[1], DTYPES[x.dtype], DTYPES[y.dtype]
+    _check(lib().srft_rotary(rows, len(items), n, d, 2 * freq.shape[0], ROTARY_LAYOUTS[layout], _dev_ptr(positions, torch.int32, "positions"),
+                             _dev_ptr(freq, torch.float64, "freq"), factor, bool(inverse), _stream_handle(stream)), "srft_rotary")
+
+
+# ---------------------------------------------------------------------------- paged cache
+class _PoolBuffers(C.Structure):
+    _fields_ = [("codes_dev", C.c_void_p), ("scales_dev", C.c_void_p), ("window_f16_dev", C.c_void_p)]
+
+
+class _PagedSeqs(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("max_new", C.c_int32), ("max_length", C.c_int64), ("max_pages", C.c_int64),
+                ("page_table_dev", C.c_void_p), ("windows_dev", C.c_void_p), ("lengths_dev", C.c_void_p), ("starts_dev", C.c_void_p)]
+
+
+class PagedSeqs:
+    """The sequences of a step (srft_paged_seqs): int32 device tensors page_table [n, max_pages], windows [n, 2], lengths [n] and
+    starts [n + 1], and bounds for what they hold, now and whenever the tensors are written again.  The tensors are kept alive."""
+
+    def __init__(self, page_table, windows, lengths, starts, max_new: int, max_length: int):
+        n = lengths.shape[0]
+        if page_table.dim() != 2 or page_table.shape[0] != n or windows.shape != (n, 2) or starts.shape != (n + 1,):
+            raise ValueError("page_table must be [n, max_pages], windows [n, 2], lengths [n], starts [n + 1]")
+        self.n_seq, self.max_new, self.max_length = n, max_new, max_length
+        self.page_table, self.windows, self.lengths, self.starts = page_table, windows, lengths, starts
+        self.struct = _PagedSeqs(n, max_new, max_length, page_table.shape[1], _dev_ptr(page_table, torch.int32, "page_table"),
+                                 _dev_ptr(windows, torch.int32, "windows"), _dev_ptr(lengths, torch.int32, "lengths"),
+                                 _dev_ptr(starts, torch.int32, "starts"))
+        self.address = C.addressof(self.struct)
+
+
+class PagePool:
+    """One layer's pages (srft_pool_create) over tensors of the caller's: k and v are (codes [pages, heads, R, code bytes] uint8,
+    scales [pages, heads, R, groups] float32, window [windows, heads, R, d] float16) each."""
+
+    def __init__(self, plan_k: "Plan", plan_v: "Plan", k, v):
+        self.handle = None
+        self.plans, self.k, self.v = (plan_k, plan_v), tuple(k), tuple(v)
+        pages, heads, R, _ = self.k[0].shape
+        windows, d = self.k[2].shape[0], plan_k.d
+        self.heads, self.R, self.d, self.n_pages, self.n_windows = heads, R, d, pages, windows
+        for plan, (codes, scales, window) in zip(self.plans, (self.k, self.v)):
+            if codes.shape != (pages, heads, R, plan.code_bytes) or scales.shape != (pages, heads, R, plan.groups) or \
+                    window.shape != (windows, heads, R, d):
+                raise ValueError("codes must be [pages, heads, R, code bytes], scales [pages, heads, R, groups], window [windows, heads, R, d]")
+        of = [_PoolBuffers(_dev_ptr(c, torch.uint8, "codes"), _dev_ptr(s, torch.float32, "scales"), _dev_ptr(w, torch.float16, "window"))
+              for c, s, w in (self.k, self.v)]
+        handle = C.c_void_p()
+        _check(lib().srft_pool_create(C.byref(handle), plan_k.handle, plan_v.handle, heads, R, pages, windows, C.byref(of[0]), C.byref(of[1])),
+               "srft_pool_create")
+        self.handle = handle.value
+
+    @classmethod
+    def empty(cls, plan_k: "Plan", plan_v: "Plan", heads: int, page_tokens: int, pages: int, windows: int, device="cuda") -> "PagePool":
+        def buffers(plan):
+            return (torch.zeros(pages, heads, page_tokens, plan.code_bytes, dtype=torch.uint8, device=device),
+                    torch.zeros(pages, heads, page_tokens, plan.groups, dtype=torch.float32, device=device),
+                    torch.zeros(windows, heads, page_tokens, plan.d, dtype=torch.float16, device=device))
+        return cls(plan_k, plan_v, buffers(plan_k), buffers(plan_v))
+
+    def close(self) -> None:
+        if self.handle:
+            _check(lib().srft_pool_destroy(self.handle), "srft_pool_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class PoolTable:
+    """The pools of the layers of a model, for calls over all of them.  The pools are kept alive."""
+
+    def __init__(self, pools):
+        self.pools = list(pools)
+        self.handles = (C.c_void_p * len(self.pools))(*[int(p.handle) for p in self.pools])
+
+
+def _sized(bytes_: int, where: str) -> int:
+    if bytes_ < 0:
+        raise SrftError(int(bytes_), where)
+    return bytes_
+
+
+def _pool_workspace(workspace: torch.Tensor, need: int) -> int:
+    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace must be {need} contiguous bytes of device memory")
+    return workspace.data_ptr()
+
+
+def srft_pool_append_workspace_bytes(pool: PagePool, seqs: PagedSeqs, n_new: int) -> int:
+    return _sized(lib().srft_pool_append_workspace_bytes(pool.handle, seqs.address, n_new), "srft_pool_append_workspace_bytes")
+
+
+def srft_pool_append(pool: PagePool, seqs: PagedSeqs, k: torch.Tensor, v: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """New tokens k, v [n_new, heads, d] fp16 into the pages and windows of their sequences."""
+    n = k.shape[0]
+    if k.dtype != torch.float16 or v.dtype != torch.float16 or k.shape != (n, pool.heads, pool.d) or v.shape != k.shape:
+        raise ValueError("k and v must be float16 [n_new, heads, d]")
+    (k_at, k_token, k_head), (v_at, v_token, v_head) = _rows(k, "k"), _rows(v, "v")
+    space = _pool_workspace(workspace, srft_pool_append_workspace_bytes(pool, seqs, n))
+    _check(lib().srft_pool_append(pool.handle, seqs.address, k_at, v_at, n, k_token, k_head, v_token, v_head, space, _stream_handle(stream)),
+           "srft_pool_append")
+
+
+def srft_pool_attention_workspace_bytes(pool: PagePool, seqs: PagedSeqs, n_new: int, n_q_heads: int) -> int:
+    return _sized(lib().srft_pool_attention_workspace_bytes(pool.handle, seqs.address, n_new, n_q_heads), "srft_pool_attention_workspace_bytes")
+
+
+def srft_pool_attention(pool: PagePool, seqs: PagedSeqs, q: torch.Tensor, softmax_scale: float, out: torch.Tensor, workspace: torch.Tensor,
+                        stream=None) -> None:
+    """out <- causal attention of q [n_new, q heads, d] (float16 or bfloat16) over the tokens that the pool holds."""
+    n, heads, d = q.shape
+    if q.dtype not in (torch.float16, torch.bfloat16) or out.dtype != q.dtype or out.shape != q.shape or d != pool.d:
+        raise ValueError("q and out must be [n_new, q heads, d], both float16 or both bfloat16")
+    (q_at, q_token, q_head), (o_at, o_token, o_head) = _rows(q, "q"), _rows(out, "out")
+    space = _pool_workspace(workspace, srft_pool_attention_workspace_bytes(pool, seqs, n, heads))
+    _check(lib().srft_pool_attention(pool.handle, seqs.address, q_at, DTYPES[q.dtype], n, heads, q_token, q_head, softmax_scale, o_at, o_token,
+                                     o_head, space, _stream_handle(stream)), "srft_pool_attention")
+
+
+def srft_pool_copy(table: PoolTable, pages: torch.Tensor, windows: torch.Tensor, stream=None) -> None:
+    """Pages pages[i, 0] -> pages[i, 1] and windows windows[i, 0] -> windows[i, 1] (int32 [n, 2] on the device) in every pool of the table."""
+    for t, name in ((pages, "pages"), (windows, "windows")):
+        if t.dim() != 2 or t.shape[1] != 2:
+            raise ValueError(f"{name} must be [n, 2]")
+    _check(lib().srft_pool_copy(table.handles, len(table.pools), _dev_ptr(pages, torch.int32, "pages"), pages.shape[0],
+                                _dev_ptr(windows, torch.int32, "windows"), windows.shape[0], _stream_handle(stream)), "srft_pool_copy")
 
 
 # ---------------------------------------------------------------------------- convenience wrapper

@@ -67,6 +67,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));   // scales and scores are 4-byte aligned
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTileVecs = 32;          // vectors per tile = N of the 32x32x16 MFMA
 constexpr int kMaxD = 256;
@@ -288,6 +289,9 @@ int srft_launch_decode_attention(const srft_plan* pk, const srft_plan* pv, const
                                  float softmax_scale, float* out, void* workspace, hipStream_t st);
 
 // ---- host side (plan.hip, api.hip) ----
+// the fp16 hi + lo split of a matrix and the order of a slab's rows, for tables built outside plan.hip
+int srft_split_hi_lo(const std::vector<double>& m, std::vector<uint16_t>& hi, std::vector<uint16_t>& lo);
+int srft_slab_output_of_row(int i);
 int srft_hip_fail(hipError_t e);         // records the error for srft_last_hip_error, returns SRFT_ERR_HIP
 #define SRFT_HIP(call)                                   \
     do {                                                 \

@@ -286,8 +286,11 @@ __device__ __forceinline__ void publish_amax(float* part, size_t team_floats, un
     if (c < D) atomic_max_nonneg(&amax[c], m * unscale);
 }
 
-// Where the input rows of the write path lie.  srft_rows_dense: one after the other from x on.
-struct srft_rows_dense {};
+// Where the rows of the write path lie: row r of a tile's input (but for srft_rows_dense, whose rows follow one another from x on), and the
+// record of the tile's first row, in rows behind the start of the codes and scales.
+struct srft_rows_dense {
+    __device__ __forceinline__ long long record(int tile) const { return (long long)tile * kTileVecs; }
+};
 // srft_rows_paged: the rows of a cache's pages that a flush converts (cache_flush.h).  Row v is slot v % R of sequence v / R %
 // n_seq of page v / (n_seq R), token j = page R + slot of its sequence counted from the first page on; the first `held` tokens of
 // a sequence are in the view already, in the place of row v, the others are where the caller has them, [n_seq][t_all][U units].
@@ -296,11 +299,37 @@ struct srft_rows_paged {
     const uint4 *fresh, *view;
     int page_rows, R, held, t_all;
     uint32_t page_magic, slot_magic;
+    __device__ __forceinline__ long long record(int tile) const { return (long long)tile * kTileVecs; }
     template <int U>
-    __device__ __forceinline__ const uint4* row(int v) const {
+    __device__ __forceinline__ const uint4* row(int tile, int r) const {
+        const int v = tile * kTileVecs + r;
         const int page = srft_even_segment((uint32_t)v, page_magic), in_page = v - page * page_rows;
         const int seq = srft_even_segment((uint32_t)in_page, slot_magic), j = page * R + in_page - seq * R;
         return j < held ? view + (unsigned)(v * U) : fresh + (unsigned)((seq * t_all + j - held) * U);
+    }
+};
+
+// srft_rows_pool: the pages of a pool that an append fills (pool.h), heads R rows each, a whole number of tiles.  Entry f of the list, f =
+// tile / tiles of a page: {row of the new tokens that slot 0 would be, slots that the window holds, window, page}.
+struct srft_rows_pool {
+    const uint4 *fresh, *window;
+    const i32x4* list;
+    long long token, head;                  // strides of the new tokens in 16-byte units
+    int heads, log_R;
+    uint32_t tiles_magic;                   // division by the tiles of a page
+    __device__ __forceinline__ i32x4 entry(int f) const {
+        return *(const __attribute__((address_space(4))) i32x4*)(list + f);        // (constant memory to this launch: scalar loads)
+    }
+    __device__ __forceinline__ long long record(int tile) const {
+        const int f = srft_even_segment((uint32_t)tile, tiles_magic), tiles = heads << log_R >> 5;
+        return (long long)entry(f).w * (heads << log_R) + (tile - f * tiles) * kTileVecs;
+    }
+    template <int U>
+    __device__ __forceinline__ const uint4* row(int tile, int r) const {
+        const int f = srft_even_segment((uint32_t)tile, tiles_magic), tiles = heads << log_R >> 5;
+        const i32x4 e = entry(f);
+        const int v = (tile - f * tiles) * kTileVecs + r, h = v >> log_R, slot = v - (h << log_R);
+        return slot < e.y ? window + (((long long)e.z * heads + h << log_R) + slot) * U : fresh + (e.x + slot) * token + h * head;
     }
 };
 

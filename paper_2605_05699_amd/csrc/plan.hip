@@ -353,6 +353,9 @@ int occupancy_grids(srft_plan* p, int cus) {
 
 }  // namespace
 
+int srft_split_hi_lo(const std::vector<double>& m, std::vector<uint16_t>& hi, std::vector<uint16_t>& lo) { return split_hi_lo(m, hi, lo); }
+int srft_slab_output_of_row(int i) { return slab_output_of_row(i); }
+
 int srft_hip_fail(hipError_t e) {
     g_last_hip_error = (int)e;
     return SRFT_ERR_HIP;

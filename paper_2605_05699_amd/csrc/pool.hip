@@ -1,0 +1,253 @@
+// pool.hip -- the paged cache of one layer: its handle, the append (list of filled pages, window copies, quantizer) and the copies of
+// pages and windows.  Attention over the pages is in pool_attention.hip.
+#include <algorithm>
+#include <memory>
+
+#include "device_util.h"
+#include "pool.h"
+
+namespace {
+
+// In front of the quantizer: workgroup 0 writes the list of the pages that the call fills, the others copy the tokens that stay in
+// windows.  A window that is read for a filled page is never the one that tokens are copied into (the caller's two windows), so the
+// two kernels need no order between their parts.  The list is in no fixed order (a counter in LDS); every page is quantized by itself, so the
+// results do not depend on it.
+__global__ void __launch_bounds__(256) srft_pool_window_kernel(const pool_append_args a, int U, int split) {
+    const pool_seqs& s = a.s;
+    const int R = 1 << s.log_R;
+    if (blockIdx.x == 0) {
+        __shared__ int prefix[kPoolMaxSeqs + 1];
+        __shared__ int wave_sums[4];
+        __shared__ int listed;
+        int base = 0;
+        if (threadIdx.x == 0) listed = 0;
+        for (int b0 = 0; b0 < s.n_seq; b0 += 256) {          // exclusive sums of the candidates per sequence
+            const int b = b0 + threadIdx.x;
+            int n = 0;
+            if (b < s.n_seq) {
+                const pool_seq q = pool_seq_of(s, b);
+                n = max((q.length >> s.log_R) - (max(q.before, 0) >> s.log_R), 0);
+            }
+            int sum = n;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int other = __shfl_up(sum, d);
+                if ((int)(threadIdx.x & 63) >= d) sum += other;
+            }
+            if ((threadIdx.x & 63) == 63) wave_sums[threadIdx.x >> 6] = sum;
+            __syncthreads();
+            int before = base;
+            for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += wave_sums[w];
+            base += wave_sums[0] + wave_sums[1] + wave_sums[2] + wave_sums[3];
+            if (b < s.n_seq) prefix[b] = before + sum - n;
+            __syncthreads();
+        }
+        if (threadIdx.x == 0) prefix[s.n_seq] = base;
+        __syncthreads();
+        for (int f = threadIdx.x; f < base; f += 256) {
+            int b = 0, end = s.n_seq;                        // the last sequence whose sum is not above f
+            while (end - b > 1) {
+                const int mid = (b + end) >> 1;
+                if (prefix[mid] <= f) b = mid;
+                else end = mid;
+            }
+            const pool_seq q = pool_seq_of(s, b);
+            const int j = (max(q.before, 0) >> s.log_R) + f - prefix[b], held = max(q.before - j * R, 0);
+            if (j >= s.max_pages) continue;
+            const int page = s.table[b * s.max_pages + j], window = s.windows[2 * b];
+            if (!pool_there(page, s.n_pages) || (held > 0 && !pool_there(window, s.n_windows))) continue;
+            const int at = atomicAdd(&listed, 1);
+            reinterpret_cast<i32x4*>(a.list + 4)[at] = i32x4{q.start + j * R - q.before, held, window, page};
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) a.list[0] = listed;
+        return;
+    }
+    const int i = (blockIdx.x - 1) / split, part = (blockIdx.x - 1) % split, b = i >> 1;
+    const bool v = i & 1;
+    const pool_seq q = pool_seq_of(s, b);
+    const int window = s.windows[2 * b + 1], first = max(max(q.full, q.before), 0), n = q.length - first;
+    if (n <= 0 || !pool_there(window, s.n_windows)) return;
+    const char* const from = v ? a.v : a.k;
+    const long long token = v ? a.v_token : a.k_token, head = v ? a.v_head : a.k_head;
+    uint4* const to = (uint4*)(v ? a.vb.window_f16_dev : a.kb.window_f16_dev) + (long long)window * a.heads * R * U;
+    for (int u = part * 256 + threadIdx.x; u < n * a.heads * U; u += split * 256) {
+        const int row = u / U, c = u - row * U, j = row / a.heads, h = row - j * a.heads;
+        to[(h * R + first - q.full + j) * U + c] = reinterpret_cast<const uint4*>(from + (q.start + first - q.before + j) * token + h * head)[c];
+    }
+}
+
+// Copies of pages and windows: one workgroup per pair and pool.  Bound by memory: a page at d = 128, 8 heads, 16 tokens is 20 KB of K
+// and V, five 16-byte units a thread, all on their way before the first is stored.
+constexpr int kCopyPools = 64;
+struct pool_copy_args {
+    struct { char *codes, *scales, *window; } of[kCopyPools][2];
+    const int32_t* pairs;
+    int n_pairs, count, units[2];            // numbers that exist; 16-byte units of codes and scales, or of a window and 0
+    bool windows;
+};
+static_assert(sizeof(pool_copy_args) <= 4096, "kernel arguments are limited to 4 KiB");
+__global__ void __launch_bounds__(256) srft_pool_copy_kernel(const pool_copy_args a) {
+    const int from = a.pairs[2 * (long long)blockIdx.x], to = a.pairs[2 * (long long)blockIdx.x + 1];
+    if (!pool_there(from, a.count) || !pool_there(to, a.count) || from == to) return;
+    const auto& p = a.of[blockIdx.y];
+    const int n = a.units[0] + a.units[1], all = 2 * n;
+    constexpr int AHEAD = 8;
+    for (int u0 = threadIdx.x; u0 < all; u0 += AHEAD * 256) {
+        uint4 x[AHEAD];
+        uint4* at[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int u = min(u0 + i * 256, all - 1), v = u >= n, w = u - v * n;
+            const bool first = w < a.units[0];
+            char* const base = a.windows ? p[v].window : first ? p[v].codes : p[v].scales;
+            const int units = first ? a.units[0] : a.units[1], c = first ? w : w - a.units[0];
+            x[i] = reinterpret_cast<const uint4*>(base)[(long long)from * units + c];
+            at[i] = reinterpret_cast<uint4*>(base) + (long long)to * units + c;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) *at[i] = x[i];       // (what is past the end stores the last unit again)
+    }
+}
+
+bool known_page(int tokens) { return tokens >= 16 && tokens <= 256 && (tokens & (tokens - 1)) == 0; }
+
+}  // namespace
+
+int srft_pool_check(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new) {
+    if (!p || !s) return SRFT_ERR_NULL;
+    if (s->n_seq < 0 || s->n_seq > kPoolMaxSeqs || s->max_new < 0 || s->max_length < 0 || s->max_length >= kPoolMaxLength || s->max_pages < 0 ||
+        s->max_pages >= (1LL << 31) || s->max_pages < s->max_length / p->R || n_new < 0 || n_new * p->heads >= (1LL << 31))
+        return SRFT_ERR_BAD_N;
+    return SRFT_OK;
+}
+int srft_pool_check_pointers(const srft_paged_seqs* s) {
+    if ((!s->page_table_dev && s->max_pages > 0) || !s->windows_dev || !s->lengths_dev || !s->starts_dev) return SRFT_ERR_NULL;
+    for (const int32_t* p : {s->page_table_dev, s->windows_dev, s->lengths_dev, s->starts_dev})
+        if (!srft_aligned(p, 4)) return SRFT_ERR_ALIGN;
+    return SRFT_OK;
+}
+
+extern "C" {
+
+int srft_pool_create(srft_pool_t** out, const srft_plan_t* plan_k, const srft_plan_t* plan_v, int n_heads, int page_tokens, int64_t n_pages,
+                     int64_t n_windows, const srft_pool_buffers* k, const srft_pool_buffers* v) {
+    if (!out) return SRFT_ERR_NULL;
+    *out = nullptr;
+    if (!plan_k || !plan_v || !k || !v) return SRFT_ERR_NULL;
+    if (n_heads < 1 || n_heads > 1024 || !known_page(page_tokens) || n_heads * page_tokens % kTileVecs != 0 || n_pages < 1 || n_windows < 1 ||
+        n_pages >= (1LL << 31) || n_windows >= (1LL << 31))
+        return SRFT_ERR_BAD_N;
+    if (!srft_plans_compatible(plan_k, plan_v)) return SRFT_ERR_MISMATCH;
+    for (const srft_pool_buffers* b : {k, v}) {
+        if (!b->codes_dev || !b->scales_dev || !b->window_f16_dev) return SRFT_ERR_NULL;
+        if (!srft_aligned(b->codes_dev, 16) || !srft_aligned(b->scales_dev, 16) || !srft_aligned(b->window_f16_dev, 16)) return SRFT_ERR_ALIGN;
+    }
+    return srft_no_throw([&] {
+        std::unique_ptr<srft_pool, int (*)(srft_pool*)> p(new srft_pool(), srft_pool_destroy);
+        p->plan_k = plan_k;
+        p->plan_v = plan_v;
+        p->k = *k;
+        p->v = *v;
+        p->heads = n_heads;
+        p->R = page_tokens;
+        while ((1 << p->log_R) < page_tokens) ++p->log_R;
+        p->n_pages = (int)n_pages;
+        p->n_windows = (int)n_windows;
+        const int rc = srft_pool_tables(p.get());
+        if (rc == SRFT_OK) *out = p.release();
+        return rc;
+    });
+}
+
+int srft_pool_destroy(srft_pool_t* pool) {
+    if (!pool) return SRFT_OK;
+    const hipError_t e = pool->tables ? hipFree(pool->tables) : hipSuccess;
+    delete pool;
+    return e == hipSuccess ? (int)SRFT_OK : srft_hip_fail(e);
+}
+
+int64_t srft_pool_append_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, int64_t n_new) {
+    const int rc = srft_pool_check(pool, seqs, n_new);
+    return rc != SRFT_OK ? rc : 16 + 16 * pool_fills(pool, seqs->n_seq, n_new);
+}
+
+int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const void* k_f16_dev, const void* v_f16_dev, int64_t n_new,
+                     int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* workspace_dev, void* hip_stream) {
+    int rc = srft_pool_check(pool, seqs, n_new);
+    if (rc != SRFT_OK) return rc;
+    if (k_token % 8 || k_head % 8 || v_token % 8 || v_head % 8) return SRFT_ERR_ALIGN;
+    const int64_t fills = pool_fills(pool, seqs->n_seq, n_new), page_tiles = (int64_t)pool->heads * pool->R / kTileVecs;
+    if (fills * page_tiles * page_tiles >= (1LL << 31) || fills * pool->heads * pool->R >= (1LL << 31)) return SRFT_ERR_BAD_N;
+    if (n_new == 0 || seqs->n_seq == 0) return SRFT_OK;
+    rc = srft_pool_check_pointers(seqs);
+    if (rc != SRFT_OK) return rc;
+    if (!k_f16_dev || !v_f16_dev || !workspace_dev) return SRFT_ERR_NULL;
+    if (!srft_aligned(k_f16_dev, 16) || !srft_aligned(v_f16_dev, 16) || !srft_aligned(workspace_dev, 16)) return SRFT_ERR_ALIGN;
+    const srft_plan *pk = pool->plan_k, *pv = pool->plan_v;
+    pool_append_args a;
+    a.s = pool_seqs_of(pool, seqs, n_new);
+    a.k = (const char*)k_f16_dev;
+    a.v = (const char*)v_f16_dev;
+    a.k_token = 2 * k_token, a.k_head = 2 * k_head, a.v_token = 2 * v_token, a.v_head = 2 * v_head;
+    a.kb = pool->k;
+    a.vb = pool->v;
+    a.k_table = srft_plan_write_table(pk);
+    a.v_table = srft_plan_write_table(pv);
+    a.k_unscale = pk->unscale_w;
+    a.v_unscale = pv->unscale_w;
+    a.heads = pool->heads;
+    a.gw = pk->gw;
+    a.tiles_magic = srft_even_magic((int)page_tiles);
+    a.list = (int*)workspace_dev;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const int split = std::max(1, std::min(pool->R / 32, std::max(1, 1024 / (2 * seqs->n_seq))));
+    rc = srft_launch(srft_pool_window_kernel, dim3((unsigned)(1 + 2 * seqs->n_seq * split)), 256, st, a, pool->units(), split);
+    if (rc != SRFT_OK) return rc;
+    int threads = 0;
+    const pool_append_kernel_t kernel = srft_plan_pool_append_kernel(pk, &threads);
+    if (!kernel) return SRFT_ERR_BAD_D;
+    const int64_t budget = std::max(1, (pk->max_wgs > 0 ? pk->max_wgs : pk->grid_q) / 2);
+    return srft_launch(kernel, dim3((unsigned)(2 * std::min(fills * page_tiles, budget))), threads, st, a);
+}
+
+int srft_pool_copy(const srft_pool_t* const* pools, int n_pools, const int32_t* pages_dev, int64_t n_page_pairs, const int32_t* windows_dev,
+                   int64_t n_window_pairs, void* hip_stream) {
+    if (n_pools < 0 || n_page_pairs < 0 || n_window_pairs < 0 || n_page_pairs >= (1LL << 31) || n_window_pairs >= (1LL << 31)) return SRFT_ERR_BAD_N;
+    if (n_pools == 0) return SRFT_OK;
+    if (!pools) return SRFT_ERR_NULL;
+    for (int i = 0; i < n_pools; ++i) {
+        if (!pools[i]) return SRFT_ERR_NULL;
+        if (!srft_plans_compatible(pools[i]->plan_k, pools[0]->plan_k) || pools[i]->heads != pools[0]->heads || pools[i]->R != pools[0]->R ||
+            pools[i]->n_pages != pools[0]->n_pages || pools[i]->n_windows != pools[0]->n_windows)
+            return SRFT_ERR_MISMATCH;
+    }
+    if ((n_page_pairs > 0 && !pages_dev) || (n_window_pairs > 0 && !windows_dev)) return SRFT_ERR_NULL;
+    if (!srft_aligned(pages_dev, 4) || !srft_aligned(windows_dev, 4)) return SRFT_ERR_ALIGN;
+    const srft_pool* p = pools[0];
+    const int rows = p->heads * p->R, d = p->plan_k->d;
+    for (int i0 = 0; i0 < n_pools; i0 += kCopyPools) {
+        pool_copy_args a;
+        const int n = std::min(kCopyPools, n_pools - i0);
+        for (int i = 0; i < n; ++i)
+            for (int v = 0; v < 2; ++v) {
+                const srft_pool_buffers& b = v ? pools[i0 + i]->v : pools[i0 + i]->k;
+                a.of[i][v] = {(char*)b.codes_dev, (char*)b.scales_dev, (char*)b.window_f16_dev};
+            }
+        for (int windows = 0; windows < 2; ++windows) {
+            const int64_t pairs = windows ? n_window_pairs : n_page_pairs;
+            if (pairs == 0) continue;
+            a.windows = windows;
+            a.pairs = windows ? windows_dev : pages_dev;
+            a.n_pairs = (int)pairs;
+            a.count = windows ? p->n_windows : p->n_pages;
+            a.units[0] = windows ? rows * d / 8 : rows * d * p->plan_k->bits / 128;
+            a.units[1] = windows ? 0 : rows * (d / p->plan_k->g) / 4;
+            const int rc = srft_launch(srft_pool_copy_kernel, dim3((unsigned)pairs, (unsigned)n), 256, (hipStream_t)hip_stream, a);
+            if (rc != SRFT_OK) return rc;
+        }
+    }
+    return SRFT_OK;
+}
+
+}  // extern "C"

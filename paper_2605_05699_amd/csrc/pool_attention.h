@@ -1,0 +1,316 @@
+// pool_attention.h -- attention of new tokens over a pool's pages: what its kernels share.
+//
+// The work is done in the rotated domain, as in kernels/decode_attention.hip: with x = R w the read path (w = code * scale, R = S Q^T
+// diag(1 / max(lambda, 1e-6))), <q, k> = <R_k^T q, w_k> and sum_t p_t v_t = R_v (sum_t p_t w_t).  So
+//   1. pool_rotate:  q' = R_k^T q for all rows, and w of the windows' tokens, both as fp16 with a power of two per row; and how many units of
+//      work (a tile of keys of one sequence and key head) there are in front of each sequence;
+//   2. pool_decode (few rows a key head) and pool_chunk (many): one pass over the keys with the running maximum and sum of the softmax.
+//      Each workgroup takes an equal share of all units, in their order, whatever sequences they belong to; what it has of one
+//      sequence, key head and block of rows is a segment.  A segment that is the whole of it is finished at once;
+//   3. pool_merge: the others' sums are brought under one maximum, added in their order, and finished.
+// Finishing is the division by the sum of weights and R_v, on the matrix cores.
+//
+// Roundings to 16 bits: q', the dequantized w (code * scale, the scale rounded first) and the weights p are fp16 operands of the matrix
+// instructions, 2^-12 of their value each on average half of that; sums, maxima and exponents are fp32.  None of the
+// three can leave fp16's range: q' has a power of two per row, w one per tile (K) or a running one (V) taken from the scales, the
+// weights are at most 2^kLazy.  What of w is below 2^-26 of the largest in its tile (K) or so far (V) loses bits below 2^-40 of that.
+//
+// Order of channels.  A dword of codes is decoded into eight fp16 values in the order 0 4 1 5 2 6 3 7 (4 bits; 0 2 1 3 at 8 bits), so
+// all operands have their channels in that order within units of eight ("positions"), q' by the way it is stored, the output by the
+// order of the columns of its matrix.
+#ifndef SRFT_POOL_ATTENTION_H
+#define SRFT_POOL_ATTENTION_H
+#include "device_util.h"
+#include "pool.h"
+
+constexpr float kPoolLowest = -3.0e38f;                      // "no key yet": finite, so that differences of two are
+constexpr int kPoolNoExponent = -200;                        // of V: "no value yet"
+constexpr float kLazy = 8.0f;                                // how far (in powers of two) weights may grow past the maximum that they are taken from
+constexpr int kPoolDecodeRows = 32;                          // rows of one key head that pool_decode takes
+constexpr int kPoolDecodeKeys = 32, kPoolDecodeWaves = 4;    // keys of a tile, a wavefront's; wavefronts of a workgroup
+constexpr int kPoolBlock = 32;                               // rows of a wavefront
+template <int D> constexpr int kPoolChunkKeys = D <= 128 ? 64 : 32;
+template <int D> constexpr int kPoolChunkWaves = 8;
+constexpr int pool_chunk_keys(int d) { return d <= 128 ? 64 : 32; }
+constexpr int pool_chunk_waves(int) { return 8; }
+
+struct pool_attention_args {
+    pool_seqs s;
+    srft_pool_buffers kb, vb;
+    int heads, group, g;                                     // key heads, query heads to each, channels to a scale
+    const char* q;                                           // strides in bytes
+    char* out;
+    long long q_token, q_head, out_token, out_head;
+    int bf16;
+    float exponent, sign;                                    // |softmax_scale| log2 e, and its sign
+    const uint4 *q_table, *k_table, *v_table, *out_table;
+    float q_unscale, k_unscale, v_unscale, out_unscale;
+    int q_tiles, q_grid;                                     // tiles of 32 query rows, workgroups that take them
+    // workspace
+    int *decode_before, *chunk_before;                       // [n_seq + 1]: units of work in front of a sequence
+    unsigned short* q_rows;                                  // [n_new][n_q_heads][D] fp16
+    float* q_factor;                                         // [n_new][n_q_heads]: exponent * what q_rows are to be multiplied with
+    unsigned short* tail_rows;                               // [K, V][n_seq][heads][R][D] fp16
+    float* tail_factor;                                      // [K, V][n_seq][heads][R]
+    float *decode_parts, *chunk_parts;                       // sums of segments (pool_part)
+    int decode_grid, chunk_grid;
+    int merge_blocks;                                        // of 32 rows, of a sequence and key head
+};
+// Sums of a block of 32 rows that a segment leaves: [D / 8 float4][64 lanes], then per lane maximum, sum of weights and V's exponent.
+template <int D> constexpr int kPoolPart = 32 * D + 3 * 64;
+constexpr long long pool_part(int d) { return 32LL * d + 3 * 64; }
+
+// ---- units of work.  A tile is of pages' keys or of the window's, never of both.
+__device__ __forceinline__ int pool_tiles(int seen, int full, int keys) {
+    const int pages = max(min(seen, full), 0), window = max(seen - full, 0);
+    return (pages + keys - 1) / keys + (window + keys - 1) / keys;
+}
+__device__ __forceinline__ bool pool_is_decode(const pool_seq& q, int group) { return q.n_new * group <= kPoolDecodeRows; }
+// tokens that the rows of block rt (of `rows` rows) see at most
+__device__ __forceinline__ int pool_seen(const pool_seq& q, int group, int rows, int rt) {
+    return q.before + (min((rt + 1) * rows, q.n_new * group) - 1) / group + 1;
+}
+// sum over the lanes of a wavefront, in all of them
+__device__ __forceinline__ int pool_wave_sum(int x) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+// tiles of the blocks of rows 0 .. n - 1 of one key head (by the whole wavefront)
+__device__ __forceinline__ int pool_chunk_units(const pool_seq& q, int group, int rows, int keys, int n) {
+    int sum = 0;
+    for (int rt = threadIdx.x & 63; rt < n; rt += 64) sum += pool_tiles(pool_seen(q, group, rows, rt), q.full, keys);
+    return pool_wave_sum(sum);
+}
+// The workgroups that take part, and where the share of workgroup w begins: w * units / workgroups.
+struct pool_shares {
+    int units, groups;
+    __device__ __forceinline__ pool_shares(int units_, int grid, int least) : units(units_), groups(max(min(grid, (units_ + least - 1) / least), 1)) {}
+    __device__ __forceinline__ int begin(int w) const { return (int)((long long)w * units / groups); }
+    __device__ __forceinline__ int owner(int unit) const { return (int)((((long long)unit + 1) * groups - 1) / units); }
+};
+// the sequence that a unit belongs to (by the whole wavefront; units before before[0] = 0 are none): the last b with before[b] <= unit
+__device__ __forceinline__ int pool_sequence_of(const int* before, int n_seq, int unit) {
+    int at = 0, n = n_seq + 1;                               // the answer is among before[at .. at + n - 1]
+    while (n > 1) {
+        const int step = (n + 63) / 64, i = at + (int)(threadIdx.x & 63) * step;
+        const int below = (int)__popcll(__ballot(i < at + n && before[min(i, n_seq)] <= unit));      // (ascending: the first ones)
+        at += (below - 1) * step;
+        n = min(step, n_seq + 1 - at);
+    }
+    return min(at, n_seq - 1);
+}
+
+// ---- exponents.  With E of the largest scale, code * scale * 2^-E is below 2^15 (codes below 2^AMP).
+template <int BITS> constexpr int kPoolAmp = BITS == 4 ? 3 : 7;
+template <int BITS>
+__device__ __forceinline__ int pool_exponent(float scale) {
+    return max((int)((__float_as_uint(scale) >> 23) & 0xFF) - 127, -99) + kPoolAmp<BITS> - 14;
+}
+__device__ __forceinline__ float pool_power(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+
+// ---- 16 codes of a row (two dwords at 4 bits, four at 8) -> two units of eight fp16 values times a scale
+template <int BITS> struct pool_codes;
+template <> struct pool_codes<4> { typedef uint2 type; };
+template <> struct pool_codes<8> { typedef uint4 type; };
+__device__ __forceinline__ half8 pool_times(uint4 x, _Float16 f) {
+    const half8 s = {f, f, f, f, f, f, f, f};
+    return __builtin_bit_cast(half8, x) * s;
+}
+__device__ __forceinline__ void pool_decode16(uint2 c, _Float16 f, half8& a, half8& b) {
+    a = pool_times(decode8(c.x), f);
+    b = pool_times(decode8(c.y), f);
+}
+__device__ __forceinline__ void pool_decode16(uint4 c, _Float16 f, half8& a, half8& b) {
+    const uint2 x = decode4_bytes(c.x), y = decode4_bytes(c.y), z = decode4_bytes(c.z), w = decode4_bytes(c.w);
+    a = pool_times(make_uint4(x.x, x.y, y.x, y.y), f);
+    b = pool_times(make_uint4(z.x, z.y, w.x, w.y), f);
+}
+
+// ---- lanes l and l ^ 32 hold the two halves of a row's keys
+__device__ __forceinline__ float pool_halves_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// maximum over the 64 lanes of a non-negative number, in all of them
+template <int CTRL> __device__ __forceinline__ float pool_row_rotated(float x) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float pool_wave_max(float x) {
+    x = fmaxf(x, pool_row_rotated<0x128>(x));                // row_ror: 8, 4, 2, 1 within 16 lanes
+    x = fmaxf(x, pool_row_rotated<0x124>(x));
+    x = fmaxf(x, pool_row_rotated<0x122>(x));
+    x = fmaxf(x, pool_row_rotated<0x121>(x));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return other_half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+typedef short pool_v4i16 __attribute__((ext_vector_type(4)));
+// Eight keys of one position: the transposed reads of two blocks of 4 keys x 16 positions by 16 lanes each.  Lane l of a 16 gives the
+// address of key l / 4, positions 4 (l % 4) .., and receives its position (l) of the four keys.
+__device__ __forceinline__ half8 pool_transposed(const unsigned char* keys0, const unsigned char* keys1) {
+    const pool_v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pool_v4i16*)keys0);
+    const pool_v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pool_v4i16*)keys1);
+    const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
+    return __builtin_bit_cast(half8, make_uint4(x.x, x.y, y.x, y.y));
+}
+
+// What a wavefront holds of 32 rows: sums[b][v] is position 32 b + 8 (v / 4) + 4 (l / 32) + v % 4 of row l % 32.
+template <int D> struct pool_block {
+    floatx16 sums[D / 32];
+    float top, den;                                          // maximum (a power of two's exponent), sum of weights (of this lane's keys)
+    int e;                                                   // sums are to be multiplied by 2^e
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) sums[b] = floatx16{0};
+        top = kPoolLowest;
+        den = 0.0f;
+        e = kPoolNoExponent;
+    }
+    __device__ __forceinline__ void scale(float f) {
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) sums[b] *= f;
+    }
+    // p: kPoolPart<D> floats in memory or LDS
+    __device__ __forceinline__ void put(float* p, int lane) const {
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                reinterpret_cast<floatx4*>(p)[(4 * b + i) * 64 + lane] = floatx4{sums[b][4 * i], sums[b][4 * i + 1], sums[b][4 * i + 2], sums[b][4 * i + 3]};
+        p[32 * D + lane] = top;
+        p[32 * D + 64 + lane] = den;
+        p[32 * D + 128 + lane] = __uint_as_float((uint32_t)e);
+    }
+    // adds what put() left at p
+    __device__ __forceinline__ void add(const float* p, int lane) {
+        const float top_p = p[32 * D + lane], den_p = p[32 * D + 64 + lane];
+        const int e_p = (int)__float_as_uint(p[32 * D + 128 + lane]);
+        const float t = fmaxf(top, top_p), f = __builtin_amdgcn_exp2f(top - t), f_p = __builtin_amdgcn_exp2f(top_p - t);
+        const int m = max(e, e_p);
+        const float g = f * pool_power(e - m), g_p = f_p * pool_power(e_p - m);
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const floatx4 x = reinterpret_cast<const floatx4*>(p)[(4 * b + i) * 64 + lane];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sums[b][4 * i + j] = fmaf(x[j], g_p, sums[b][4 * i + j] * g);
+            }
+        top = t;
+        den = fmaf(den_p, f_p, den * f);
+        e = m;
+    }
+};
+
+// A tile's weights.  s: scores of K keys, register v of 32 of them key 8 (v / 4) + 4 (l / 32) + v % 4; c > 0 turns them into
+// exponents.  Masked scores are -infinity.  On return the weights, under b.top; the block's sums are scaled where that grew.
+template <int D, int N>
+__device__ __forceinline__ void pool_weights(pool_block<D>& b, floatx16 (&s)[N], float c, int e, bool first) {
+    float m = fmaxf(s[0][0], s[0][1]);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int v = n == 0 ? 2 : 0; v < 16; ++v) m = fmaxf(m, s[n][v]);
+    m = fmaxf(other_half_max(m) * c, kPoolLowest);
+    // The sums are kept under an older maximum as long as no weight passes 2^kLazy: after the first tiles they are hardly ever scaled.
+    const bool grown = m > b.top + kLazy;
+    const int e_new = max(b.e, e);                           // (uniform)
+    if (__ballot(grown) || e_new != b.e) {
+        const float t = grown ? m : b.top, f = __builtin_amdgcn_exp2f(b.top - t);
+        if (!first) b.scale(f * pool_power(b.e - e_new));
+        b.den *= f;
+        b.top = t;
+        b.e = e_new;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            s[n][v] = __builtin_amdgcn_exp2f(fmaf(s[n][v], c, -b.top));
+            sum += s[n][v];
+        }
+    b.den += sum;
+}
+// eight weights (registers 8 i .. 8 i + 7) as an operand
+__device__ __forceinline__ half8 pool_half8(const floatx16& s, int i) {
+    half8 h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)s[8 * i + e];
+    return h;
+}
+
+// The end of 32 rows: division by the sum of weights (over both halves' keys already) and R_v.  The sums are taken as fp16 hi + lo
+// under a power of two per row, the matrix as hi + lo, so that nothing is lost here.  dst: the lane's row (l % 32), or null.
+template <int D>
+__device__ __forceinline__ void pool_finish(pool_block<D>& b, const uint4* __restrict__ table, float unscale, char* dst, int bf16, int lane) {
+    float m = 0.0f;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) m = fmaxf(m, fabsf(b.sums[k][v]));
+    m = other_half_max(m);
+    const int e = max((int)((__float_as_uint(m) >> 23) & 0xFF) - 127, -100);
+    const float up = pool_power(14 - e);
+    // (a power of two for each part: together they may leave fp32's range before the product does)
+    const float down = (b.den > 0.0f ? 1.0f / b.den : 0.0f) * unscale, p0 = pool_power(e - 14), p1 = pool_power(b.e);
+    half8 hi[D / 16], lo[D / 16];
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = b.sums[k / 2][8 * (k % 2) + i] * up;
+            hi[k][i] = (_Float16)x;
+            lo[k][i] = (_Float16)(x - (float)hi[k][i]);
+        }
+    const int h = lane >> 5;
+#pragma unroll 1
+    for (int j = 0; j < D / 32; ++j) {
+        floatx16 acc{0};
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const half8 ah = __builtin_bit_cast(half8, table[((j * (D / 16) + k) * 2 + 0) * 64 + lane]);
+            const half8 al = __builtin_bit_cast(half8, table[((j * (D / 16) + k) * 2 + 1) * 64 + lane]);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, hi[k], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, hi[k], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, lo[k], acc, 0, 0, 0);
+        }
+        if (dst) {
+            uint4 w[2];
+            uint32_t* const o = reinterpret_cast<uint32_t*>(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = acc[2 * i] * down * p0 * p1, y = acc[2 * i + 1] * down * p0 * p1;
+                if (bf16) {
+                    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+                    o[i] = __builtin_bit_cast(uint32_t, bf2{(__bf16)x, (__bf16)y});
+                } else {
+                    o[i] = pack_half2(x, y);
+                }
+            }
+            uint4* const p = reinterpret_cast<uint4*>(dst) + (32 * j + 16 * h) / 8;
+            p[0] = w[0];
+            p[1] = w[1];
+        }
+    }
+}
+
+// The lane's row of a block of rows that starts at row r0 of a key head's n_new * group: where it is in q and out, and the last
+// token that it sees (-1: none, or no row).
+struct pool_row {
+    int token, head, last;
+    bool there;
+};
+__device__ __forceinline__ pool_row pool_row_of(const pool_seq& q, int key_head, int group, int row) {
+    const int n = q.n_new * group, r = min(row, n - 1), t = r / group;
+    return {q.start + t, key_head * group + r - t * group, row < n ? min(q.before + t, q.length - 1) : -1, row < n};
+}
+
+typedef void (*pool_attention_kernel_t)(const pool_attention_args);
+pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits);
+pool_attention_kernel_t srft_pick_pool_decode(int d, int bits);
+pool_attention_kernel_t srft_pick_pool_chunk(int d, int bits);
+pool_attention_kernel_t srft_pick_pool_merge(int d, bool chunk);
+
+#endif  // SRFT_POOL_ATTENTION_H

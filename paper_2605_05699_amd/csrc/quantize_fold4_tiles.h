@@ -117,7 +117,7 @@ srft_quantize_fold4_tiles(const uint4* __restrict__ wf4, const uint4* __restrict
         const int lim = (tile == n_tiles - 1) ? last_lim : kTileVecs - 1;
         const uint4* src;
         if constexpr (std::is_same_v<ROWS, srft_rows_dense>) src = x + (long long)tile * kTileVecs * U + (unsigned)(min(frow, lim) * U + 4 * fchunk);
-        else src = rows.template row<U>(tile * kTileVecs + min(frow, lim)) + 4 * fchunk;
+        else src = rows.template row<U>(tile, min(frow, lim)) + 4 * fchunk;
         a = src[0];          // plain loads: four loads touch every line, and non-temporal ones then fetch it again
         b = src[1];
         c = src[2];
@@ -205,7 +205,7 @@ srft_quantize_fold4_tiles(const uint4* __restrict__ wf4, const uint4* __restrict
     };
     // vector-ALU tail of the tile whose keep is in `keep` and whose exchange values are in exch[b] / lds[b]
     auto finish = [&](int b, const floatx16& keep, int tile) __attribute__((always_inline)) {
-        const long long row0 = (long long)tile * kTileVecs;
+        const long long row0 = rows.record(tile);
         const int lim = (tile == n_tiles - 1) ? last_lim : kTileVecs - 1;
         const int c = min(col, lim);
         const float* slots = reinterpret_cast<const float*>(&lds[b][0]);
@@ -299,7 +299,7 @@ srft_quantize_fold4_tiles(const uint4* __restrict__ wf4, const uint4* __restrict
     // staged record of `tile` -> global memory: 16 bytes per thread, whole rows next to each other (rows past the end
     // alias to the last row); the first wavefront also moves the scales
     auto flush = [&](int b, int tile) __attribute__((always_inline)) {
-        const long long row0 = (long long)tile * kTileVecs;
+        const long long row0 = rows.record(tile);
         const int lim = (tile == n_tiles - 1) ? last_lim : kTileVecs - 1;
         if constexpr (STAGE) {
             constexpr int PIECES = CU8 / 2;              // 16-byte pieces per code row

@@ -122,7 +122,7 @@ srft_quantize_fold_tiles(const uint4* __restrict__ wfold, const uint4* __restric
         const int q = tid + i * NT, r = q / (U / 2), c = q % (U / 2);
         const uint4* src;
         if constexpr (std::is_same_v<ROWS, srft_rows_dense>) src = tile_base + (unsigned)(min(r, lim) * U + 2 * c);
-        else src = rows.template row<U>(tile * kTileVecs + min(r, lim)) + 2 * c;
+        else src = rows.template row<U>(tile, min(r, lim)) + 2 * c;
         a = src[0];
         b = src[1];
     };
@@ -203,7 +203,7 @@ srft_quantize_fold_tiles(const uint4* __restrict__ wfold, const uint4* __restric
     };
     // vector-ALU tail of one tile, whose exchange values are in xch[b]
     auto finish = [&](int b, floatx16& e, floatx16& o, int tile) __attribute__((always_inline)) {
-        const long long row0 = (long long)tile * kTileVecs;
+        const long long row0 = rows.record(tile);
         const int lim = (tile == n_tiles - 1) ? last_lim : kTileVecs - 1;
         const int c = min(col, lim);
         float below = xch[b][slot_in * kTileVecs + col];                 // packed index 32 * slot_in
@@ -308,7 +308,7 @@ srft_quantize_fold_tiles(const uint4* __restrict__ wfold, const uint4* __restric
     // staged record of `tile` -> global memory (rows past the end alias to the last row)
     auto flush = [&](int b, int tile) __attribute__((always_inline)) {
         if constexpr (STAGE) {
-            const long long row0 = (long long)tile * kTileVecs;
+            const long long row0 = rows.record(tile);
             const int lim = (tile == n_tiles - 1) ? last_lim : kTileVecs - 1;
             constexpr int PIECES = CU8 / 2;              // 16-byte pieces per code row
             uint4* cbase = reinterpret_cast<uint4*>(codes) + row0 * PIECES;

@@ -61,7 +61,7 @@ srft_quantize_tiles(const uint4* __restrict__ wfrag, const uint4* __restrict__ x
     auto fetch1 = [&](uint4& v, int i, const uint4* tile_base, int lim, int tile) __attribute__((always_inline)) {
         const int u = tid + i * NT, r = u / U, c = u % U;
         if constexpr (std::is_same_v<ROWS, srft_rows_dense>) v = tile_base[(unsigned)(min(r, lim) * U + c)];
-        else v = rows.template row<U>(tile * kTileVecs + min(r, lim))[c];
+        else v = rows.template row<U>(tile, min(r, lim))[c];
     };
     auto fetch = [&](uint4& a, uint4& b, uint4& c, uint4& d, int tile) __attribute__((always_inline)) {
         if (tile > n_tiles - 1) tile = n_tiles - 1;          // prefetch past the end re-reads the last tile
@@ -105,7 +105,7 @@ srft_quantize_tiles(const uint4* __restrict__ wfrag, const uint4* __restrict__ x
     [[maybe_unused]] const int ns = GM == kGroupWide ? G / gw : SMAX;
     // vector-ALU tail of one tile: per-group abs-max, scale, int4 codes, into staging buffer b or to memory
     auto finish = [&](Acc& accs, int tile, [[maybe_unused]] const int b) __attribute__((always_inline)) {
-        const long long row0 = (long long)tile * kTileVecs;
+        const long long row0 = rows.record(tile);
         const int lim = (tile == n_tiles - 1) ? last_lim : kTileVecs - 1;     // uniform
         const int c = min(col, lim);                                      // alias rows past the end
         if constexpr (OUT == kOutAmax) {
@@ -183,7 +183,7 @@ srft_quantize_tiles(const uint4* __restrict__ wfrag, const uint4* __restrict__ x
     // without a scale store behind the end of the buffer, that is nowhere)
     auto flush = [&](int b, int tile) __attribute__((always_inline)) {
         if constexpr (STAGE) {
-            const long long row0 = (long long)tile * kTileVecs;
+            const long long row0 = rows.record(tile);
             const int lim = (tile == n_tiles - 1) ? last_lim : kTileVecs - 1;
             constexpr int WIDTH = BITS * S >= 8 ? 2 : 1, ROWS_OF = CU8 / WIDTH, PIECES = kTileVecs * ROWS_OF;    // 8-byte units a piece
             static_assert(PIECES % NT == 0, "as many pieces for every thread");
