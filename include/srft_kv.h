@@ -317,7 +317,7 @@ int srft_rotary(const srft_rotary_rows* rows, int count, int64_t n_tokens, int d
  *
  * srft_pool_create   plan_k, plan_v: same d, group size, code width, transform and device.  page_tokens is 16, 32, 64, 128 or 256,
  *                    n_heads * page_tokens a multiple of 32, n_pages and n_windows >= 1 (else SRFT_ERR_BAD_N).  Allocates device tables
- *                    (8 d^2 bytes) on the plans' GPU.  The plans must outlive the pool.
+ *                    (12 d^2 bytes) on the plans' GPU.  The plans must outlive the pool.
  */
 typedef struct srft_pool srft_pool_t;
 typedef struct srft_pool_buffers {

@@ -26,8 +26,9 @@
 constexpr float kPoolLowest = -3.0e38f;                      // "no key yet": finite, so that differences of two are
 constexpr int kPoolNoExponent = -200;                        // of V: "no value yet"
 constexpr float kLazy = 8.0f;                                // how far (in powers of two) weights may grow past the maximum that they are taken from
-constexpr int kPoolDecodeRows = 32;                          // rows of one key head that pool_decode takes
-constexpr int kPoolDecodeKeys = 32, kPoolDecodeWaves = 4;    // keys of a tile, a wavefront's; wavefronts of a workgroup
+constexpr int kPoolDecodeRows = 32;                          // most rows of one key head that pool_decode takes, in blocks of 16
+constexpr int kPoolDecodeWaves = 4;
+constexpr int pool_decode_keys(int d, int cb) { return d <= 128 && cb == 1 ? 64 : 32; }      // of a tile
 constexpr int kPoolBlock = 32;                               // rows of a wavefront
 template <int D> constexpr int kPoolChunkKeys = D <= 128 ? 64 : 32;
 template <int D> constexpr int kPoolChunkWaves = 8;
@@ -43,17 +44,19 @@ struct pool_attention_args {
     long long q_token, q_head, out_token, out_head;
     int bf16;
     float exponent, sign;                                    // |softmax_scale| log2 e, and its sign
-    const uint4 *q_table, *k_table, *v_table, *out_table;
+    const uint4 *q_table, *k_table, *v_table, *out_table, *out_table16;
     float q_unscale, k_unscale, v_unscale, out_unscale;
-    int q_tiles, q_grid;                                     // tiles of 32 query rows, workgroups that take them
+    int q_tiles, q_grid;                                     // passes of query rows in pool_rotate, workgroups that take them
     // workspace
     int *decode_before, *chunk_before;                       // [n_seq + 1]: units of work in front of a sequence
-    unsigned short* q_rows;                                  // [n_new][n_q_heads][D] fp16
+    unsigned short *q_rows, *q_rows_low;                     // [n_new][n_q_heads][D] fp16: q', and what its rounding leaves
     float* q_factor;                                         // [n_new][n_q_heads]: exponent * what q_rows are to be multiplied with
     unsigned short* tail_rows;                               // [K, V][n_seq][heads][R][D] fp16
     float* tail_factor;                                      // [K, V][n_seq][heads][R]
+    unsigned short* tail_columns;                            // V's [n_seq][heads][D channels][R]
     float *decode_parts, *chunk_parts;                       // sums of segments (pool_part)
     int decode_grid, chunk_grid;
+    int decode_rows, decode_block, decode_keys;              // rows that go to pool_decode, those of a workgroup, keys of its tiles
     int merge_blocks;                                        // of 32 rows, of a sequence and key head
 };
 // Sums of a block of 32 rows that a segment leaves: [D / 8 float4][64 lanes], then per lane maximum, sum of weights and V's exponent.
@@ -65,7 +68,7 @@ __device__ __forceinline__ int pool_tiles(int seen, int full, int keys) {
     const int pages = max(min(seen, full), 0), window = max(seen - full, 0);
     return (pages + keys - 1) / keys + (window + keys - 1) / keys;
 }
-__device__ __forceinline__ bool pool_is_decode(const pool_seq& q, int group) { return q.n_new * group <= kPoolDecodeRows; }
+__device__ __forceinline__ bool pool_is_decode(const pool_seq& q, int group, int rows) { return q.n_new * group <= rows; }
 // tokens that the rows of block rt (of `rows` rows) see at most
 __device__ __forceinline__ int pool_seen(const pool_seq& q, int group, int rows, int rt) {
     return q.before + (min((rt + 1) * rows, q.n_new * group) - 1) / group + 1;
@@ -241,6 +244,22 @@ __device__ __forceinline__ half8 pool_half8(const floatx16& s, int i) {
     return h;
 }
 
+// 16 channels next to each other of the lane's row, times three factors (a power of two for each part: together they may leave fp32's range
+// before the product does), to row dst from channel `first` on; nowhere if dst is null.
+__device__ __forceinline__ void pool_store16(const floatx16& acc, float down, float p0, float p1, char* dst, int first, int bf16) {
+    if (!dst) return;
+    uint32_t o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = acc[2 * i] * down * p0 * p1, y = acc[2 * i + 1] * down * p0 * p1;
+        typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+        o[i] = bf16 ? __builtin_bit_cast(uint32_t, bf2{(__bf16)x, (__bf16)y}) : pack_half2(x, y);
+    }
+    uint4* const p = reinterpret_cast<uint4*>(dst) + first / 8;
+    p[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    p[1] = make_uint4(o[4], o[5], o[6], o[7]);
+}
+
 // The end of 32 rows: division by the sum of weights (over both halves' keys already) and R_v.  The sums are taken as fp16 hi + lo
 // under a power of two per row, the matrix as hi + lo, so that nothing is lost here.  dst: the lane's row (l % 32), or null.
 template <int D>
@@ -253,7 +272,6 @@ __device__ __forceinline__ void pool_finish(pool_block<D>& b, const uint4* __res
     m = other_half_max(m);
     const int e = max((int)((__float_as_uint(m) >> 23) & 0xFF) - 127, -100);
     const float up = pool_power(14 - e);
-    // (a power of two for each part: together they may leave fp32's range before the product does)
     const float down = (b.den > 0.0f ? 1.0f / b.den : 0.0f) * unscale, p0 = pool_power(e - 14), p1 = pool_power(b.e);
     half8 hi[D / 16], lo[D / 16];
 #pragma unroll
@@ -276,23 +294,7 @@ __device__ __forceinline__ void pool_finish(pool_block<D>& b, const uint4* __res
             acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, hi[k], acc, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, lo[k], acc, 0, 0, 0);
         }
-        if (dst) {
-            uint4 w[2];
-            uint32_t* const o = reinterpret_cast<uint32_t*>(w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float x = acc[2 * i] * down * p0 * p1, y = acc[2 * i + 1] * down * p0 * p1;
-                if (bf16) {
-                    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-                    o[i] = __builtin_bit_cast(uint32_t, bf2{(__bf16)x, (__bf16)y});
-                } else {
-                    o[i] = pack_half2(x, y);
-                }
-            }
-            uint4* const p = reinterpret_cast<uint4*>(dst) + (32 * j + 16 * h) / 8;
-            p[0] = w[0];
-            p[1] = w[1];
-        }
+        pool_store16(acc, down, p0, p1, dst, 32 * j + 16 * h, bf16);
     }
 }
 
@@ -308,9 +310,13 @@ __device__ __forceinline__ pool_row pool_row_of(const pool_seq& q, int key_head,
 }
 
 typedef void (*pool_attention_kernel_t)(const pool_attention_args);
-pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits);
-pool_attention_kernel_t srft_pick_pool_decode(int d, int bits);
+// tiles of 32 rows of a pass of pool_rotate: with few rows one, so that they are spread over the compute units
+constexpr int pool_rotate_tiles(long long q_rows, int compute_units) { return q_rows >= 128LL * compute_units ? 4 : 1; }
+pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits, int tiles);
+pool_attention_kernel_t srft_pick_pool_decode_b4(int d, int cb, int gm);
+pool_attention_kernel_t srft_pick_pool_decode_b8(int d, int cb, int gm);
+pool_attention_kernel_t srft_pick_pool_decode_merge(int d, int cb);
 pool_attention_kernel_t srft_pick_pool_chunk(int d, int bits);
-pool_attention_kernel_t srft_pick_pool_merge(int d, bool chunk);
+pool_attention_kernel_t srft_pick_pool_merge(int d);
 
 #endif  // SRFT_POOL_ATTENTION_H

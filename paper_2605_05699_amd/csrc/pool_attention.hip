@@ -8,12 +8,25 @@ namespace {
 
 // Where each part of the workspace begins, and the grids that parts of it are counted by.
 struct workspace {
-    int64_t decode_before, chunk_before, q_rows, q_factor, tail_rows, tail_factor, decode_parts, chunk_parts, bytes;
+    int64_t decode_before, chunk_before, q_rows, q_rows_low, q_factor, tail_rows, tail_factor, tail_columns, decode_parts, chunk_parts, bytes;
     int decode_grid, chunk_grid;
 };
 int workgroups(const srft_pool* p, int per_unit) { return p->plan_k->max_wgs > 0 ? p->plan_k->max_wgs : p->plan_k->compute_units * per_unit; }
 int64_t row_blocks(const srft_paged_seqs* s, int64_t n_new, int group, int rows) {           // of one sequence and key head, at most
     return (std::min<int64_t>(s->max_new, n_new) * group + rows - 1) / rows;
+}
+// Sequences that bring few rows a key head go to pool_decode, cb blocks of 16 of them a workgroup, the others to pool_chunk.  Two blocks where
+// a sequence may bring 17 to 32 rows and none brings more, up to d = 128 (beyond it two blocks' sums do not fit the registers: there a
+// workgroup takes one block, and the keys are read twice); else one, and 17 rows are a chunk.
+struct split {
+    int cb, rows;
+    bool chunk, decode;
+};
+split split_of(const srft_paged_seqs* s, int64_t n_new, int group, int d) {
+    const int64_t most = std::min<int64_t>(s->max_new, n_new) * group;
+    const bool few = most > 16 && most <= kPoolDecodeRows;
+    const int rows = few ? kPoolDecodeRows : 16;
+    return {few && d <= 128 ? 2 : 1, rows, most > rows, most <= rows || s->n_seq > 1 || n_new * group <= rows};
 }
 workspace layout(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new, int q_heads) {
     const int d = p->plan_k->d, group = q_heads / p->heads;
@@ -25,18 +38,25 @@ workspace layout(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new, in
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    w.decode_grid = workgroups(p, 2);
+    const split s16 = split_of(s, n_new, group, d);
+    w.decode_grid = workgroups(p, p->decode_blocks[s16.cb - 1]);
     w.chunk_grid = workgroups(p, 1);
     w.decode_before = take(4LL * (s->n_seq + 1));
     w.chunk_before = take(4LL * (s->n_seq + 1));
     w.q_rows = take(2 * rows * d);
+    w.q_rows_low = take(2 * rows * d);
     w.q_factor = take(4 * rows);
     w.tail_rows = take(2 * tail * d);
     w.tail_factor = take(4 * tail);
-    w.decode_parts = take(2LL * w.decode_grid * pool_part(d) * 4);
-    w.chunk_parts = take(std::min<int64_t>(s->max_new, n_new) * group > kPoolDecodeRows ? 2LL * w.chunk_grid * pool_chunk_waves(d) * pool_part(d) * 4 : 0);
+    w.tail_columns = take(tail * d);
+    w.decode_parts = take(2LL * w.decode_grid * s16.cb * (16 * d + 3 * 64) * 4);
+    w.chunk_parts = take(s16.chunk ? 2LL * w.chunk_grid * pool_chunk_waves(d) * pool_part(d) * 4 : 0);
     w.bytes = at;
     return w;
+}
+
+pool_attention_kernel_t srft_pool_decode_kernel_of(const srft_plan* p, int cb) {
+    return p->bits == 8 ? srft_pick_pool_decode_b8(p->d, cb, p->gm) : srft_pick_pool_decode_b4(p->d, cb, p->gm);
 }
 
 int check(const srft_pool* pool, const srft_paged_seqs* seqs, int64_t n_new, int q_heads) {
@@ -45,9 +65,9 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, int64_t n_new, int
     if (q_heads < 1 || q_heads % pool->heads != 0 || q_heads > 64 * pool->heads || n_new * q_heads >= (1LL << 31) - 32) return SRFT_ERR_BAD_N;
     // units of work, tiles and workgroups are counted with 32 bits
     const int d = pool->plan_k->d, group = q_heads / pool->heads, rows = kPoolBlock * pool_chunk_waves(d);
-    const int64_t most = 1LL << 31, tiles = seqs->max_length / kPoolDecodeKeys + 2, heads = (int64_t)seqs->n_seq * pool->heads;
+    const int64_t most = 1LL << 31, tiles = seqs->max_length / 32 + 2, heads = (int64_t)seqs->n_seq * pool->heads;
     const int64_t blocks = row_blocks(seqs, n_new, group, rows), all_blocks = n_new * group / rows + seqs->n_seq;
-    if (heads * tiles >= most || all_blocks * pool->heads * tiles >= most || heads * std::max<int64_t>(blocks, 1) * pool_chunk_waves(d) >= most ||
+    if (2 * heads * tiles >= most || all_blocks * pool->heads * tiles >= most || heads * std::max<int64_t>(blocks, 1) * pool_chunk_waves(d) >= most ||
         heads * pool->R / kTileVecs * 2 >= most / 2)
         return SRFT_ERR_BAD_N;
     return SRFT_OK;
@@ -57,7 +77,8 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, int64_t n_new, int
 
 // Both tables are R_k^T and R_v as fp16 hi + lo fragments.  The queries': [D / 32 slabs][D / 16 k-steps][hi, lo][64 lanes], as on the
 // write path (lane l: row slab_output_of_row(l % 32), columns 16 t + 8 (l / 32) + e).  The outputs': the same with the columns
-// in the order that sums of values have them in a lane, 16 t + 8 (e / 4) + 4 (l / 32) + e % 4, positions instead of channels.
+// in the order that sums of values have them in a lane, 16 t + 8 (e / 4) + 4 (l / 32) + e % 4, positions instead of channels.  The
+// outputs' again for blocks of 16 rows, [D / 16][D / 32 k-steps][hi, lo][64 lanes]: row l % 16, channels 32 t + 16 (e / 4) + 4 (l / 16) + e % 4.
 int srft_pool_tables(srft_pool* p) {
     const int d = p->plan_k->d, G = d / 32, T = d / 16, bits = p->plan_k->bits;
     std::vector<float> rk((size_t)d * d), rv((size_t)d * d);                // [channel][n]
@@ -76,7 +97,7 @@ int srft_pool_tables(srft_pool* p) {
     p->q_unscale = (float)std::ldexp(1.0, -srft_split_hi_lo(q, qh, ql));
     p->out_unscale = (float)std::ldexp(1.0, -srft_split_hi_lo(o, oh, ol));
     const size_t units = (size_t)G * T * 2 * 64;
-    std::vector<uint16_t> image(2 * units * 8);
+    std::vector<uint16_t> image(3 * units * 8);
     static const int byte_order[8] = {0, 2, 1, 3, 4, 6, 5, 7};
     for (int w = 0; w < G; ++w)
         for (int t = 0; t < T; ++t)
@@ -90,6 +111,19 @@ int srft_pool_tables(srft_pool* p) {
                     image[units * 8 + at] = oh[(size_t)row * d + channel];
                     image[units * 8 + at + 64 * 8] = ol[(size_t)row * d + channel];
                 }
+    for (int n = 0; n < d / 16; ++n)
+        for (int t = 0; t < G; ++t)
+            for (int l = 0; l < 64; ++l)
+                for (int e = 0; e < 8; ++e) {
+                    const size_t at = 2 * units * 8 + (((size_t)n * G + t) * 2 * 64 + l) * 8 + e;
+                    const size_t src = (size_t)(16 * n + l % 16) * d + 32 * t + 16 * (e / 4) + 4 * (l / 16) + e % 4;
+                    image[at] = oh[src];
+                    image[at + 64 * 8] = ol[src];
+                }
+    for (int cb = 1; cb <= 2; ++cb) {
+        SRFT_HIP(hipOccupancyMaxActiveBlocksPerMultiprocessor(&p->decode_blocks[cb - 1], (const void*)srft_pool_decode_kernel_of(p->plan_k, cb), 64 * kPoolDecodeWaves, 0));
+        p->decode_blocks[cb - 1] = std::max(1, std::min(4, p->decode_blocks[cb - 1]));
+    }
     SRFT_HIP(hipMalloc((void**)&p->tables, image.size() * 2));
     SRFT_HIP(hipMemcpy(p->tables, image.data(), image.size() * 2, hipMemcpyHostToDevice));
     return SRFT_OK;
@@ -132,41 +166,44 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     a.exponent = std::fabs(softmax_scale) * 1.44269504088896340736f;
     a.sign = softmax_scale < 0 ? -1.0f : 1.0f;
     a.q_table = pool->tables;
-    a.out_table = pool->tables + (size_t)(d / 32) * (d / 16) * 2 * 64;
+    const size_t units = (size_t)(d / 32) * (d / 16) * 2 * 64;
+    a.out_table = pool->tables + units;
+    a.out_table16 = pool->tables + 2 * units;
     a.k_table = pk->wfrag;
     a.v_table = pv->wfrag;
     a.q_unscale = pool->q_unscale;
     a.out_unscale = pool->out_unscale;
     a.k_unscale = pk->unscale_w;
     a.v_unscale = pv->unscale_w;
-    a.q_tiles = (int)((n_new * n_q_heads + kTileVecs - 1) / kTileVecs);
+    const int pass = pool_rotate_tiles(n_new * n_q_heads, pk->compute_units);
+    a.q_tiles = (int)((n_new * n_q_heads + pass * kTileVecs - 1) / (pass * kTileVecs));
     a.q_grid = std::min(a.q_tiles, workgroups(pool, 2));
     a.decode_before = (int*)(base + w.decode_before);
     a.chunk_before = (int*)(base + w.chunk_before);
     a.q_rows = (unsigned short*)(base + w.q_rows);
+    a.q_rows_low = (unsigned short*)(base + w.q_rows_low);
     a.q_factor = (float*)(base + w.q_factor);
     a.tail_rows = (unsigned short*)(base + w.tail_rows);
     a.tail_factor = (float*)(base + w.tail_factor);
+    a.tail_columns = (unsigned short*)(base + w.tail_columns);
     a.decode_parts = (float*)(base + w.decode_parts);
     a.chunk_parts = (float*)(base + w.chunk_parts);
+    const split sp = split_of(seqs, n_new, group, d);
     a.decode_grid = w.decode_grid;
+    a.decode_rows = sp.rows;
+    a.decode_block = 16 * sp.cb;
+    a.decode_keys = pool_decode_keys(d, sp.cb);
     a.chunk_grid = w.chunk_grid;
     const hipStream_t st = (hipStream_t)hip_stream;
-    const int tail_tiles = 2 * seqs->n_seq * (pool->heads * pool->R / kTileVecs), heads = seqs->n_seq * pool->heads;
-    rc = srft_launch(srft_pick_pool_rotate(d, pk->bits), dim3((unsigned)(1 + a.q_grid + tail_tiles)), 2 * d, st, a);
-    // whatever few rows each sequence may bring there can be some that bring few, unless it is the only one
-    const int64_t most_rows = std::min<int64_t>(seqs->max_new, n_new) * group;
-    const bool chunk = most_rows > kPoolDecodeRows, decode = !chunk || seqs->n_seq > 1 || n_new * group <= kPoolDecodeRows;
-    if (rc == SRFT_OK && chunk) rc = srft_launch(srft_pick_pool_chunk(d, pk->bits), dim3((unsigned)a.chunk_grid), 64 * pool_chunk_waves(d), st, a);
-    if (rc == SRFT_OK && decode) rc = srft_launch(srft_pick_pool_decode(d, pk->bits), dim3((unsigned)a.decode_grid), 64 * kPoolDecodeWaves, st, a);
-    if (rc == SRFT_OK && chunk) {
+    const int tail_tiles = 2 * seqs->n_seq * ((pool->heads * pool->R + pass * kTileVecs - 1) / (pass * kTileVecs)), heads = seqs->n_seq * pool->heads;
+    rc = srft_launch(srft_pick_pool_rotate(d, pk->bits, pass), dim3((unsigned)(1 + a.q_grid + tail_tiles)), 2 * d, st, a);
+    if (rc == SRFT_OK && sp.chunk) rc = srft_launch(srft_pick_pool_chunk(d, pk->bits), dim3((unsigned)a.chunk_grid), 64 * pool_chunk_waves(d), st, a);
+    if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb), dim3((unsigned)a.decode_grid), 64 * kPoolDecodeWaves, st, a);
+    if (rc == SRFT_OK && sp.chunk) {
         a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * pool_chunk_waves(d)) * pool_chunk_waves(d);
-        rc = srft_launch(srft_pick_pool_merge(d, true), dim3((unsigned)(heads * a.merge_blocks)), 64, st, a);
+        rc = srft_launch(srft_pick_pool_merge(d), dim3((unsigned)(heads * a.merge_blocks)), 256, st, a);
     }
-    if (rc == SRFT_OK && decode) {
-        a.merge_blocks = 1;
-        rc = srft_launch(srft_pick_pool_merge(d, false), dim3((unsigned)heads), 64, st, a);
-    }
+    if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pick_pool_decode_merge(d, sp.cb), dim3((unsigned)(heads * ((sp.rows + a.decode_block - 1) / a.decode_block))), 64 * kPoolDecodeWaves, st, a);
     return rc;
 }
 
