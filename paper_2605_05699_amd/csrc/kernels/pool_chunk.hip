@@ -6,11 +6,16 @@
 // rows of the score product, so that scores, weights and the running softmax of a row stay in one lane and its neighbour across the
 // wavefront, and weights go into the second product as they are.
 //
-// A tile's exponent (of K's scales and of V's) has to be known before it is decoded.  Its scales are loaded with its codes two tiles ahead;
-// each wavefront brings its largest one to LDS at the end of the tile in between, one atomic maximum, in a ring of four.
+// A tile is decoded under powers of two of K's and of V's scales that all wavefronts share.  They are running: they change only where a scale
+// outgrows them (kRoom powers of two above what they were taken from), which a wavefront sees when its part of a tile arrives, one
+// comparison; only then it tells the others, through a ring in LDS that all look into before they decode.
+// Loads are straight-line, two tiles ahead of their use; a wavefront's part of a tile lies in one or two blocks of 16 keys, whose pages
+// make scalar addresses.
 #include "../pool_attention.h"
 
 namespace {
+
+constexpr int kRoom = 2;                                     // powers of two that scales may grow before the exponent changes
 
 template <int D, int BITS>
 __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_kernel(const pool_attention_args a) {
@@ -19,11 +24,11 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
     constexpr int KROW = 2 * D + 16, VROW = 2 * D + 32;      // bytes of a row in LDS: 16-byte reads of 32 rows, transposed reads of 8, on different banks
     constexpr int UNITS = KEYS * T;                          // of 16 channels, of K or of V
     constexpr int N = (2 * UNITS + NT - 1) / NT;             // a thread's
+    static_assert(UNITS % 64 == 0 && N <= 2, "a wavefront's units are of one kind, a thread has one or two");
     typedef typename pool_codes<BITS>::type code_t;
     __shared__ __align__(16) unsigned char k_lds[2][KEYS * KROW], v_lds[2][KEYS * VROW];
-    __shared__ unsigned int largest[4][2];                   // bits of the largest scale of a tile, K and V
-    __shared__ unsigned int unknown[4];                      // a key of the tile lies in a page that does not exist
-    __shared__ unsigned char known[2][KEYS];
+    __shared__ uint4 ring[4];                                // of tile t % 4: largest scales (bits) of K, of V where they outgrew the exponents; blocks of 16
+                                                             // keys whose pages do not exist
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
     const int total = a.chunk_before[a.s.n_seq];
@@ -36,16 +41,22 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
     const int R = 1 << a.s.log_R, n_scales = D / a.g;
 
     // a thread's units: K's first, then V's; which key of the tile, which 16 channels
-    int u_key[N], u_at[N], u_scale[N];
-    bool u_v[N];
+    bool u_v[N];                                             // (of the whole wavefront)
+    int u_block[N], u_key[N], u_at[N], off_code[N], off_scale[N];
+    unsigned char* dst[N];                                   // in the first buffer
+    bool second[N];                                          // the key is in the second block of 16 that the wavefront's units touch
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int u = min(tid + i * NT, 2 * UNITS - 1);      // (past the end: the last unit again)
-        u_v[i] = u >= UNITS;
-        const int r = u_v[i] ? u - UNITS : u;
+        const int u0 = min(wave * 64 + i * NT, 2 * UNITS - 64), u = u0 + lane;           // (past the end: the last units again)
+        u_v[i] = u0 >= UNITS;
+        const int r = u_v[i] ? u - UNITS : u, r0 = u_v[i] ? u0 - UNITS : u0;
         u_key[i] = r / T;
         u_at[i] = r - u_key[i] * T;
-        u_scale[i] = 16 * u_at[i] / a.g;
+        u_block[i] = r0 / T / 16;
+        second[i] = u_key[i] / 16 != u_block[i];
+        off_code[i] = (u_key[i] & 15) * CB + u_at[i] * (int)sizeof(code_t);
+        off_scale[i] = 4 * ((u_key[i] & 15) * n_scales + 16 * u_at[i] / a.g);
+        dst[i] = (u_v[i] ? v_lds[0] + u_key[i] * VROW : k_lds[0] + u_key[i] * KROW) + 32 * u_at[i];
     }
 
     for (bool at_begin = true; unit < end; at_begin = false) {
@@ -61,11 +72,10 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
         }
         const int t1 = min(tiles, t0 + end - unit);
         if (t1 <= t0) return;                                // (only if the device arrays were written during the call)
-        const int seen = pool_seen(q, a.group, ROWS, rt), page_keys = min(seen, q.full), page_tiles = (max(page_keys, 0) + KEYS - 1) / KEYS, tail = q.length - q.full;
+        const int seen = pool_seen(q, a.group, ROWS, rt), page_tiles = (max(min(seen, q.full), 0) + KEYS - 1) / KEYS, tail = q.length - q.full;
         const pool_row row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + l32);
         const long long q_row = (long long)row.token * (a.heads * a.group) + row.head;
         const int32_t* const table = a.s.table + seq * a.s.max_pages;
-        const bool window_there = pool_there(a.s.windows[2 * seq + 1], a.s.n_windows);
         // (the last token that any row of this wavefront sees; rows do not see less than those before them)
         int wave_last = row.last;
 #pragma unroll
@@ -81,153 +91,188 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
         const float factor = a.q_factor[q_row];
         pool_block<D> b;
         b.clear();
+        int ek = kPoolNoExponent, ev = kPoolNoExponent;      // of the tile decoded last
 
-        code_t code[N];
-        float scale[N];
-        bool there[N];
-        int page[N];
-        const auto pages = [&](int t) __attribute__((always_inline)) {
+        // ---- the rows of a decoded tile: buffer, its first token, the last that may count, missing blocks of 16 keys, exponents
+        const auto compute = [&](int buffer, int key0, int last_key, uint32_t missing, int ek_now, int ev_now) __attribute__((always_inline)) {
+            if (key0 > wave_last) return;                    // (uniform over the wavefront)
+            floatx16 s[KB];
+            const unsigned char* const kr = &k_lds[buffer][l32 * KROW + 16 * half];
 #pragma unroll
-            for (int i = 0; i < N; ++i) page[i] = q.full > 0 ? table[min(t * KEYS + u_key[i], q.full - 1) >> a.s.log_R] : -1;
+            for (int n = 0; n < KB; ++n) s[n] = floatx16{0};
+#pragma unroll
+            for (int i = 0; i < T; ++i)
+#pragma unroll
+                for (int n = 0; n < KB; ++n)
+                    s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, *reinterpret_cast<const uint4*>(kr + 32 * n * KROW + 32 * i)), qf[i], s[n], 0, 0, 0);
+            const int last = min(row.last, last_key) - key0;
+            if (__ballot(last < KEYS - 1) || missing) {
+#pragma unroll
+                for (int n = 0; n < KB; ++n)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int key = 32 * n + 8 * (v / 4) + 4 * half + v % 4;
+                        s[n][v] = key <= last && !(missing >> (key >> 4) & 1) ? s[n][v] : -__builtin_inff();
+                    }
+            }
+            pool_weights<D, KB>(b, s, fmaxf(factor * pool_power(ek_now), 1.17549435e-38f), ev_now, b.e == kPoolNoExponent);
+            const unsigned char* const vr = &v_lds[buffer][(4 * half + (lane & 15) / 4) * VROW + (16 * (lane >> 4 & 1) + 4 * (lane & 3)) * 2];
+#pragma unroll
+            for (int i = 0; i < 2 * KB; ++i) {
+                const half8 p = pool_half8(s[i / 2], i % 2);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c)
+                    b.sums[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pool_transposed(vr + 16 * i * VROW + 64 * c, vr + (16 * i + 8) * VROW + 64 * c), p, b.sums[c], 0, 0, 0);
+            }
         };
-        const auto fetch = [&](int t) __attribute__((always_inline)) {
-            if (t >= t1) return;                             // uniform, as below
-            if (t < page_tiles) {
+
+        const int last_page_tile = min(t1, page_tiles) - 1;
+        int t = t0;
+        __syncthreads();                                     // (the segment before has read its last tile)
+        if (tid < 4) ring[tid] = make_uint4(0, 0, 0, 0);
+        if (t <= last_page_tile) {
+            code_t code[N];
+            typedef float pair __attribute__((ext_vector_type(2)));
+            pair scale{0, 0};                                // (a native vector: an array ends up in LDS)
+            uint32_t there = 0;                              // of the tile fetched last: bits 2 i, 2 i + 1: the pages of unit i's two blocks
+            // the pages of a wavefront's blocks of 16 keys, unit i's in lanes 2 i and 2 i + 1; behind the last page, the last block again
+            const auto pages_of = [&](int tile) __attribute__((always_inline)) {
+                int block = u_block[0] + (lane & 1);
+                if constexpr (N > 1) block = (lane >> 1 & 1) == 1 ? u_block[1] + (lane & 1) : block;
+                return table[min(tile * KEYS + 16 * block, q.full - 16) >> a.s.log_R];
+            };
+            const auto fetch = [&](int tile, int pages) __attribute__((always_inline)) {
+                there = 0;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const srft_pool_buffers& of = u_v[i] ? a.vb : a.kb;
-                    there[i] = pool_there(page[i], a.s.n_pages);
-                    const long long at = ((long long)(there[i] ? page[i] : 0) * a.heads + head << a.s.log_R) + (min(t * KEYS + u_key[i], q.full - 1) & (R - 1));
-                    code[i] = reinterpret_cast<const code_t*>(of.codes_dev + at * CB)[u_at[i]];
-                    scale[i] = of.scales_dev[at * n_scales + u_scale[i]];
+                    uint64_t c0, c1, f0, f1;
+                    const auto address = [&](int k, uint64_t& c, uint64_t& f) __attribute__((always_inline)) {
+                        const int page = __builtin_amdgcn_readlane(pages, 2 * i + k), slot = min(tile * KEYS + 16 * (u_block[i] + k), q.full - 16) & (R - 1);
+                        const bool ok = pool_there(page, a.s.n_pages);
+                        there |= (ok ? 1u : 0u) << (2 * i + k);
+                        const uint64_t at = ((uint64_t)((ok ? page : 0) * (uint64_t)a.heads + head) << a.s.log_R) + slot;
+                        c = at * CB;
+                        f = at * (4 * n_scales);
+                        asm("" : "+s"(c), "+s"(f));
+                    };
+                    address(0, c0, f0);
+                    if constexpr (64 % T == 0 && 64 / T <= 16) {             // the wavefront's units lie in one block
+                        c1 = c0, f1 = f0;
+                        there |= (there >> (2 * i) & 1) << (2 * i + 1);
+                    } else {
+                        address(1, c1, f1);
+                    }
+                    const uint8_t* const codes = u_v[i] ? a.vb.codes_dev : a.kb.codes_dev;
+                    const char* const scales = (const char*)(u_v[i] ? a.vb.scales_dev : a.kb.scales_dev);
+                    code[i] = *reinterpret_cast<const code_t*>(codes + (second[i] ? c1 : c0) + off_code[i]);
+                    scale[i] = *reinterpret_cast<const float*>(scales + (second[i] ? f1 : f0) + off_scale[i]);
                 }
-            } else {                                         // the window's tokens: the row's factor (their rows are loaded where they are used)
-                constexpr float kUp = BITS == 4 ? 4096.0f : 256.0f;
+            };
+            // what of the fetched tile the others have to know: scales that outgrow the exponents, missing pages
+            const auto check = [&](int tile) __attribute__((always_inline)) {
+                const float most_k = pool_power(ek + 15 - kPoolAmp<BITS>), most_v = pool_power(ev + 15 - kPoolAmp<BITS>);
+                bool news = there != (1u << (2 * N)) - 1;    // uniform
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const long long at = ((long long)((u_v[i] ? a.s.n_seq : 0) + seq) * a.heads + head << a.s.log_R) + min((t - page_tiles) * KEYS + u_key[i], tail - 1);
-                    there[i] = window_there;
-                    scale[i] = there[i] ? a.tail_factor[at] * kUp : 0.0f;
+                for (int i = 0; i < N; ++i) news |= __ballot(!(scale[i] < (u_v[i] ? most_v : most_k))) != 0;
+                if (news) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const bool ok = there >> (2 * i + (second[i] ? 1 : 0)) & 1;
+                        scale[i] = ok ? scale[i] : 0.0f;
+                        const float m = pool_wave_max(scale[i]);
+                        uint32_t* const at = reinterpret_cast<uint32_t*>(&ring[tile & 3]);
+                        if (lane == 0) atomicMax(&at[u_v[i] ? 1 : 0], __float_as_uint(m));
+                        if (!ok) atomicOr(&at[2], 1u << (u_key[i] >> 4));
+                    }
                 }
-            }
-        };
-        // the largest scale of the tile that has been fetched
-        const auto publish = [&](int t) __attribute__((always_inline)) {
-            if (t >= t1) return;
-            float mk = 0.0f, mv = 0.0f;
-            bool all = true;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                scale[i] = there[i] ? scale[i] : 0.0f;
-                mk = fmaxf(mk, u_v[i] ? 0.0f : scale[i]);
-                mv = fmaxf(mv, u_v[i] ? scale[i] : 0.0f);
-                all &= there[i];
-            }
-            mk = pool_wave_max(mk);
-            mv = pool_wave_max(mv);
-            const bool some = __ballot(!all) != 0;
-            if (lane == 0) {
-                atomicMax(&largest[t & 3][0], __float_as_uint(mk));
-                atomicMax(&largest[t & 3][1], __float_as_uint(mv));
-                if (some) unknown[t & 3] = 1;
-            }
-        };
-        int ev = kPoolNoExponent;                            // of the tile decoded last
-        const auto decode = [&](int t) __attribute__((always_inline)) {
-            if (t >= t1) return;
-            const int ek = pool_exponent<BITS>(__uint_as_float(largest[t & 3][0]));
-            ev = max(ev, pool_exponent<BITS>(__uint_as_float(largest[t & 3][1])));
-            const float uk = pool_power(-ek), uv = pool_power(-ev);
-            if (t < page_tiles) {
+            };
+            const auto decode = [&](int tile) __attribute__((always_inline)) {
+                const float uk = pool_power(-ek), uv = pool_power(-ev);
+                const int buffer = tile & 1;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     half8 x, y;
                     pool_decode16(code[i], (_Float16)(scale[i] * (u_v[i] ? uv : uk)), x, y);
-                    unsigned char* const dst = u_v[i] ? &v_lds[t & 1][u_key[i] * VROW] : &k_lds[t & 1][u_key[i] * KROW];
-                    reinterpret_cast<uint4*>(dst)[2 * u_at[i]] = __builtin_bit_cast(uint4, x);
-                    reinterpret_cast<uint4*>(dst)[2 * u_at[i] + 1] = __builtin_bit_cast(uint4, y);
-                    if (!u_v[i] && u_at[i] == 0) known[t & 1][u_key[i]] = there[i];
+                    uint4* const to = reinterpret_cast<uint4*>(dst[i] + buffer * (u_v[i] ? KEYS * VROW : KEYS * KROW));
+                    to[0] = __builtin_bit_cast(uint4, x);
+                    to[1] = __builtin_bit_cast(uint4, y);
                 }
-            } else {
-                constexpr float kDown = BITS == 4 ? 1.0f / 4096.0f : 1.0f / 256.0f;
+            };
+            // exponents for tile t, from the ring: kept unless a scale has outgrown them, else with room to grow
+            uint32_t missing = 0;
+            const auto look = [&](int tile) __attribute__((always_inline)) {
+                const uint4 x = ring[tile & 3];
+                const uint32_t k = __builtin_amdgcn_readfirstlane(x.x), v = __builtin_amdgcn_readfirstlane(x.y);
+                missing = __builtin_amdgcn_readfirstlane(x.z);
+                if (k) ek = max(ek, pool_exponent<BITS>(__uint_as_float(k)) + (__uint_as_float(k) < pool_power(ek + 15 - kPoolAmp<BITS>) ? -1000 : kRoom));
+                if (v) ev = max(ev, pool_exponent<BITS>(__uint_as_float(v)) + (__uint_as_float(v) < pool_power(ev + 15 - kPoolAmp<BITS>) ? -1000 : kRoom));
+            };
+            fetch(t, pages_of(t));
+            int pages = pages_of(min(t + 1, last_page_tile));
+            __syncthreads();                                 // the ring is clear
+            check(t);
+            __syncthreads();
+            look(t);
+            ek = max(ek, -99 + kPoolAmp<BITS> - 14);         // (a tile of zeros)
+            ev = max(ev, -99 + kPoolAmp<BITS> - 14);
+            decode(t);
+            fetch(min(t + 1, last_page_tile), pages);
+            pages = pages_of(min(t + 2, last_page_tile));
+            check(t + 1);
+            for (; t <= last_page_tile; ++t) {
+                __syncthreads();                             // tile t is in LDS, what tile t + 1 has to say in the ring
+                const int ek_now = ek, ev_now = ev;
+                const uint32_t missing_now = missing;
+                if (tid == 0) ring[(t + 3) & 3] = make_uint4(0, 0, 0, 0);            // (last read before this barrier, next written behind the next one)
+                look(t + 1);
+                decode(t + 1);                               // (behind the last tile: that one again, which nobody reads)
+                fetch(min(t + 2, last_page_tile), pages);
+                pages = pages_of(min(t + 3, last_page_tile));
+                compute(t & 1, t * KEYS, q.full - 1, missing_now, ek_now, ev_now);
+                check(t + 2);
+            }
+        }
+        // ---- the window's tokens: rows in fp16 under a power of two each
+        if (t < t1 && pool_there(a.s.windows[2 * seq + 1], a.s.n_windows)) {             // (uniform)
+            for (; t < t1; ++t) {
+                const int key0 = (t - page_tiles) * KEYS;
+                constexpr float kUp = BITS == 4 ? 4096.0f : 256.0f;          // 2^(15 - AMP): a row's values are below 2^15, not 2^AMP
+                uint4 x[N][2];
+                float f[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const long long at = ((long long)((u_v[i] ? a.s.n_seq : 0) + seq) * a.heads + head << a.s.log_R) + min((t - page_tiles) * KEYS + u_key[i], tail - 1);
+                    const long long at = ((long long)((u_v[i] ? a.s.n_seq : 0) + seq) * a.heads + head << a.s.log_R) + min(key0 + u_key[i], tail - 1);
                     const uint4* const src = reinterpret_cast<const uint4*>(a.tail_rows + at * D) + 2 * u_at[i];
-                    const _Float16 f = (_Float16)(scale[i] * kDown * (u_v[i] ? uv : uk));
-                    const uint4 zero = make_uint4(0, 0, 0, 0);
-                    unsigned char* const dst = u_v[i] ? &v_lds[t & 1][u_key[i] * VROW] : &k_lds[t & 1][u_key[i] * KROW];
-                    reinterpret_cast<uint4*>(dst)[2 * u_at[i]] = __builtin_bit_cast(uint4, pool_times(there[i] ? src[0] : zero, f));
-                    reinterpret_cast<uint4*>(dst)[2 * u_at[i] + 1] = __builtin_bit_cast(uint4, pool_times(there[i] ? src[1] : zero, f));
-                    if (!u_v[i] && u_at[i] == 0) known[t & 1][u_key[i]] = there[i];
+                    x[i][0] = src[0];
+                    x[i][1] = src[1];
+                    f[i] = a.tail_factor[at];
                 }
+                __syncthreads();                             // (the tile before has been read, its ring entries too)
+                if (tid < 4) ring[tid] = make_uint4(0, 0, 0, 0);
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float m = pool_wave_max(f[i] * kUp);
+                    if (lane == 0) atomicMax(reinterpret_cast<uint32_t*>(&ring[0]) + (u_v[i] ? 1 : 0), __float_as_uint(m));
+                }
+                __syncthreads();
+                ek = pool_exponent<BITS>(__uint_as_float(ring[0].x));
+                ev = max(ev, pool_exponent<BITS>(__uint_as_float(ring[0].y)));
+                const float uk = pool_power(-ek), uv = pool_power(-ev);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const _Float16 up = (_Float16)(f[i] * (u_v[i] ? uv : uk));
+                    reinterpret_cast<uint4*>(dst[i])[0] = __builtin_bit_cast(uint4, pool_times(x[i][0], up));
+                    reinterpret_cast<uint4*>(dst[i])[1] = __builtin_bit_cast(uint4, pool_times(x[i][1], up));
+                }
+                __syncthreads();
+                compute(0, q.full + key0, q.length - 1, 0, __builtin_amdgcn_readfirstlane(ek), __builtin_amdgcn_readfirstlane(ev));
             }
-        };
-
-        // ---- the first tiles
-        __syncthreads();                                     // (the segment before has read its last tile)
-        if (tid < 8) largest[tid >> 1][tid & 1] = 0;
-        if (tid < 4) unknown[tid] = 0;
-        pages(t0);
-        fetch(t0);
-        pages(t0 + 1);
-        __syncthreads();
-        publish(t0);
-        __syncthreads();
-        decode(t0);
-        int ev_now = ev;
-        fetch(t0 + 1);
-        pages(t0 + 2);
-        publish(t0 + 1);
-
-        for (int t = t0; t < t1; ++t) {
-            __syncthreads();                                 // tile t is in LDS, tile t + 1's scales in the ring
-            const int ek_now = pool_exponent<BITS>(__uint_as_float(largest[t & 3][0]));
-            ev_now = ev;
-            const bool some_unknown = unknown[t & 3] != 0;
-            if (tid < 2) largest[(t + 3) & 3][tid] = 0;      // (last read before this barrier, next written behind the next one)
-            if (tid == 2) unknown[(t + 3) & 3] = 0;
-            decode(t + 1);
-            fetch(t + 2);
-            pages(t + 3);
-            const bool window = t >= page_tiles;
-            const int key0 = window ? q.full + (t - page_tiles) * KEYS : t * KEYS;
-            if (key0 <= wave_last) {                         // (uniform over the wavefront)
-                floatx16 s[KB];
-                const unsigned char* const kr = &k_lds[t & 1][l32 * KROW + 16 * half];
-#pragma unroll
-                for (int n = 0; n < KB; ++n) {
-                    s[n] = floatx16{0};
-#pragma unroll
-                    for (int i = 0; i < T; ++i)
-                        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, *reinterpret_cast<const uint4*>(kr + 32 * n * KROW + 32 * i)), qf[i], s[n], 0, 0, 0);
-                }
-                const int last = min(row.last, window ? q.length - 1 : q.full - 1) - key0;
-                if (__ballot(last < KEYS - 1) || some_unknown) {
-#pragma unroll
-                    for (int n = 0; n < KB; ++n)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const int key = 32 * n + 8 * (v / 4) + 4 * half + v % 4;
-                            s[n][v] = key <= last && known[t & 1][key] ? s[n][v] : -__builtin_inff();
-                        }
-                }
-                pool_weights<D, KB>(b, s, fmaxf(factor * pool_power(ek_now), 1.17549435e-38f), ev_now, b.e == kPoolNoExponent);
-                const unsigned char* const vr = &v_lds[t & 1][(4 * half + (lane & 15) / 4) * VROW + (16 * (lane >> 4 & 1) + 4 * (lane & 3)) * 2];
-#pragma unroll
-                for (int i = 0; i < 2 * KB; ++i) {
-                    const half8 p = pool_half8(s[i / 2], i % 2);
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c)
-                        b.sums[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pool_transposed(vr + 16 * i * VROW + 64 * c, vr + (16 * i + 8) * VROW + 64 * c), p, b.sums[c], 0, 0, 0);
-                }
-            }
-            publish(t + 2);
         }
         b.den = pool_halves_sum(b.den);
         if (t0 == 0 && t1 == tiles) {
-            char* const dst = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
-            pool_finish<D>(b, a.out_table, a.out_unscale, dst, a.bf16, lane);
+            char* const to = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
+            pool_finish<D>(b, a.out_table, a.out_unscale, to, a.bf16, lane);
         } else {
             b.put(a.chunk_parts + ((2LL * w + (at_begin ? 0 : 1)) * W + wave) * kPoolPart<D>, lane);
         }

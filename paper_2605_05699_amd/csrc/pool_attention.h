@@ -114,18 +114,18 @@ __device__ __forceinline__ float pool_power(int e) { return __uint_as_float((uin
 
 // ---- 16 codes of a row (two dwords at 4 bits, four at 8) -> two units of eight fp16 values times a scale
 template <int BITS> struct pool_codes;
-template <> struct pool_codes<4> { typedef uint2 type; };
-template <> struct pool_codes<8> { typedef uint4 type; };
+template <> struct pool_codes<4> { typedef u32x2 type; };
+template <> struct pool_codes<8> { typedef u32x4 type; };
 __device__ __forceinline__ half8 pool_times(uint4 x, _Float16 f) {
     const half8 s = {f, f, f, f, f, f, f, f};
     return __builtin_bit_cast(half8, x) * s;
 }
-__device__ __forceinline__ void pool_decode16(uint2 c, _Float16 f, half8& a, half8& b) {
-    a = pool_times(decode8(c.x), f);
-    b = pool_times(decode8(c.y), f);
+__device__ __forceinline__ void pool_decode16(u32x2 c, _Float16 f, half8& a, half8& b) {
+    a = pool_times(decode8(c[0]), f);
+    b = pool_times(decode8(c[1]), f);
 }
-__device__ __forceinline__ void pool_decode16(uint4 c, _Float16 f, half8& a, half8& b) {
-    const uint2 x = decode4_bytes(c.x), y = decode4_bytes(c.y), z = decode4_bytes(c.z), w = decode4_bytes(c.w);
+__device__ __forceinline__ void pool_decode16(u32x4 c, _Float16 f, half8& a, half8& b) {
+    const uint2 x = decode4_bytes(c[0]), y = decode4_bytes(c[1]), z = decode4_bytes(c[2]), w = decode4_bytes(c[3]);
     a = pool_times(make_uint4(x.x, x.y, y.x, y.y), f);
     b = pool_times(make_uint4(z.x, z.y, w.x, w.y), f);
 }

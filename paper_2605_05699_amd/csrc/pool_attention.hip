@@ -40,7 +40,7 @@ workspace layout(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new, in
     };
     const split s16 = split_of(s, n_new, group, d);
     w.decode_grid = workgroups(p, p->decode_blocks[s16.cb - 1]);
-    w.chunk_grid = workgroups(p, 1);
+    w.chunk_grid = workgroups(p, 8 / pool_chunk_waves(d));
     w.decode_before = take(4LL * (s->n_seq + 1));
     w.chunk_before = take(4LL * (s->n_seq + 1));
     w.q_rows = take(2 * rows * d);
