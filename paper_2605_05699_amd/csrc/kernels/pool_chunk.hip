@@ -15,6 +15,7 @@
 
 namespace {
 
+constexpr int kAhead = 2;                                    // reads of LDS ahead of the matrix instructions; 4 and 6 measure the same up to 128 dimensions, and spill above
 constexpr int kRoom = 2;                                     // powers of two that scales may grow before the exponent changes
 
 template <int D, int BITS>
@@ -98,32 +99,50 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
             if (key0 > wave_last) return;                    // (uniform over the wavefront)
             floatx16 s[KB];
             const unsigned char* const kr = &k_lds[buffer][l32 * KROW + 16 * half];
+            const unsigned char* const vr = &v_lds[buffer][(4 * half + (lane & 15) / 4) * VROW + (16 * (lane >> 4 & 1) + 4 * (lane & 3)) * 2];
+            // Both products read their operands kAhead matrix instructions ahead; the fences keep the compiler from moving the reads to their uses.
+            half8 f[kAhead];
+            const auto read_k = [&](int j) __attribute__((always_inline)) {          // of the scores' j-th: block of keys j % KB, channels from 16 (j / KB) on
+                return __builtin_bit_cast(half8, *reinterpret_cast<const uint4*>(kr + 32 * (j % KB) * KROW + 32 * (j / KB)));
+            };
+            const auto read_v = [&](int j) __attribute__((always_inline)) {          // of the sums': channels from 32 (j % (D / 32)) on, keys from 16 (j / (D / 32)) on
+                const unsigned char* const at = vr + 16 * (j / (D / 32)) * VROW + 64 * (j % (D / 32));
+                return pool_transposed(at, at + 8 * VROW);
+            };
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) f[j] = read_k(j);
 #pragma unroll
             for (int n = 0; n < KB; ++n) s[n] = floatx16{0};
 #pragma unroll
-            for (int i = 0; i < T; ++i)
+            for (int j = 0; j < T * KB; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                s[j % KB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[j % kAhead], qf[j / KB], s[j % KB], 0, 0, 0);
+                if (j + kAhead < T * KB) f[j % kAhead] = read_k(j + kAhead);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int n = 0; n < KB; ++n)
-                    s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, *reinterpret_cast<const uint4*>(kr + 32 * n * KROW + 32 * i)), qf[i], s[n], 0, 0, 0);
+            for (int j = 0; j < kAhead; ++j) f[j] = read_v(j);
             const int last = min(row.last, last_key) - key0;
             if (__ballot(last < KEYS - 1) || missing) {
+                const int limit = last - 4 * half;           // (compared with constants)
 #pragma unroll
                 for (int n = 0; n < KB; ++n)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
-                        const int key = 32 * n + 8 * (v / 4) + 4 * half + v % 4;
-                        s[n][v] = key <= last && !(missing >> (key >> 4) & 1) ? s[n][v] : -__builtin_inff();
+                        const int key = 32 * n + 8 * (v / 4) + v % 4;
+                        s[n][v] = key <= limit && !(missing >> (key >> 4) & 1) ? s[n][v] : -__builtin_inff();
                     }
             }
             pool_weights<D, KB>(b, s, fmaxf(factor * pool_power(ek_now), 1.17549435e-38f), ev_now, b.e == kPoolNoExponent);
-            const unsigned char* const vr = &v_lds[buffer][(4 * half + (lane & 15) / 4) * VROW + (16 * (lane >> 4 & 1) + 4 * (lane & 3)) * 2];
+            half8 p{};
 #pragma unroll
-            for (int i = 0; i < 2 * KB; ++i) {
-                const half8 p = pool_half8(s[i / 2], i % 2);
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c)
-                    b.sums[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pool_transposed(vr + 16 * i * VROW + 64 * c, vr + (16 * i + 8) * VROW + 64 * c), p, b.sums[c], 0, 0, 0);
+            for (int j = 0; j < 2 * KB * (D / 32); ++j) {
+                if (j % (D / 32) == 0) p = pool_half8(s[j / (D / 32) / 2], j / (D / 32) % 2);
+                __builtin_amdgcn_sched_barrier(0);
+                b.sums[j % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[j % kAhead], p, b.sums[j % (D / 32)], 0, 0, 0);
+                if (j + kAhead < 2 * KB * (D / 32)) f[j % kAhead] = read_v(j + kAhead);
             }
+            __builtin_amdgcn_sched_barrier(0);
         };
 
         const int last_page_tile = min(t1, page_tiles) - 1;
