@@ -1,19 +1,20 @@
-// Attention over a pool, the end of chunks: the sums of rows whose keys went to several workgroups are added in the order of the keys and
-// finished; rows of sequences without a tile are zero.  One workgroup of four wavefronts per 32 rows of a key head, each with every fourth
+// Attention over a pool, the end: the sums of rows whose keys went to several workgroups are added in the order of the keys and
+// finished; rows of sequences without a tile are zero.  The first a.decode_merges workgroups take the rows of the scan for few rows
+// (pool_decode_merge), the others those of chunks, in one launch: apart, the first took 17 us beside the 29 of the others (d = 256).
+// Chunks: one workgroup of four wavefronts per 32 rows of a key head, each with every fourth
 // run of 32 positions of the sums and then of the outputs (one wavefront per 32 rows read every part, and the matrix, one after
 // the other: 104 us at d = 256, 28 at d = 128).  Rows that their scan has finished have nothing to do here.
-#include "../pool_attention.h"
+#include "../pool_decode.h"
 
 namespace {
 
-constexpr int kTeam = 4;
+constexpr int kTeam = kPoolTeam;
 template <int D>
-__global__ void __launch_bounds__(64 * kTeam) srft_pool_merge_kernel(const pool_attention_args a) {
+__device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsigned workgroup, uint4* ops, float (*tops)[32]) {
     constexpr int BLOCKS = kPoolChunkWaves<D>, ROWS = kPoolBlock * BLOCKS, KEYS = kPoolChunkKeys<D>, G = D / 32, T = D / 16, OWN = (G + kTeam - 1) / kTeam, AHEAD = 2;
-    __shared__ uint4 ops[T * 2 * 64];                        // [k-step][hi, lo][lane]
-    __shared__ float tops[kTeam][32];
+    // ops: [k-step][hi, lo][lane]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int of = (int)(blockIdx.x / (unsigned)a.merge_blocks), at = (int)blockIdx.x - of * a.merge_blocks;
+    const int of = (int)(workgroup / (unsigned)a.merge_blocks), at = (int)workgroup - of * a.merge_blocks;
     const int seq = of / a.heads, head = of - seq * a.heads, rt = at / BLOCKS, block = at - rt * BLOCKS;
     const pool_seq q = pool_seq_of(a.s, seq);
     const int r0 = rt * ROWS + block * kPoolBlock;
@@ -32,14 +33,18 @@ __global__ void __launch_bounds__(64 * kTeam) srft_pool_merge_kernel(const pool_
     const pool_shares shares(before[a.s.n_seq], a.chunk_grid, 1);
     const int w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
     if (w0 == w1) return;
+    const int behind = shares.begin(w0) != first ? 1 : 0;    // the first part's workgroup began with other rows
     const auto part = [&](int w) __attribute__((always_inline)) {
-        return a.chunk_parts + ((2LL * w + (w == w0 && shares.begin(w) != first ? 1 : 0)) * BLOCKS + block) * kPoolPart<D>;
+        return a.chunk_parts + ((2LL * w + (w == w0 ? behind : 0)) * BLOCKS + block) * kPoolPart<D>;
     };
     float t_all = kPoolLowest, den = 0.0f;
     int e_all = kPoolNoExponent;
-    for (int w = w0; w <= w1; ++w) {
-        t_all = fmaxf(t_all, part(w)[32 * D + lane]);
-        e_all = max(e_all, (int)__float_as_uint(part(w)[32 * D + 128 + lane]));
+    for (int v = w0; v <= w1; v += 4) {
+        float t[4], e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = part(min(v + k, w1))[32 * D + lane], e[k] = part(min(v + k, w1))[32 * D + 128 + lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t_all = fmaxf(t_all, t[k]), e_all = max(e_all, (int)__float_as_uint(e[k]));
     }
     floatx16 sums[OWN];
 #pragma unroll
@@ -114,9 +119,23 @@ __global__ void __launch_bounds__(64 * kTeam) srft_pool_merge_kernel(const pool_
     }
 }
 
-template <int D> pool_attention_kernel_t pick() { return srft_pool_merge_kernel<D>; }
-pool_attention_kernel_t dispatch(int d) { SRFT_DISPATCH_D(d, pick) }
+template <int D, int CB>
+__global__ void __launch_bounds__(64 * kTeam) srft_pool_merge_kernel(const pool_attention_args a) {
+    constexpr int OPS = D / 16 * 2 * 64;
+    __shared__ __align__(16) unsigned char lds[std::max(kPoolFinishBytes<D>, OPS * 16 + kTeam * 32 * 4)];
+    if (blockIdx.x < (unsigned)a.decode_merges)              // uniform
+        pool_decode_merge<D, CB>(a, blockIdx.x, lds);
+    else
+        chunk_merge<D>(a, blockIdx.x - a.decode_merges, reinterpret_cast<uint4*>(lds), reinterpret_cast<float (*)[32]>(lds + OPS * 16));
+}
+
+template <int D> pool_attention_kernel_t pick(int cb) {
+    if constexpr (D <= 128)
+        if (cb == 2) return srft_pool_merge_kernel<D, 2>;
+    return srft_pool_merge_kernel<D, 1>;
+}
+pool_attention_kernel_t dispatch(int d, int cb) { SRFT_DISPATCH_D(d, pick, cb) }
 
 }  // namespace
 
-pool_attention_kernel_t srft_pick_pool_merge(int d) { return dispatch(d); }
+pool_attention_kernel_t srft_pick_pool_merge(int d, int cb) { return dispatch(d, cb); }

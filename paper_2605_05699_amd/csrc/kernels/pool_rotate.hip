@@ -51,7 +51,7 @@ __device__ __forceinline__ void count_units(const pool_attention_args& a) {
 template <int D, int BITS, int N>
 __global__ void __launch_bounds__(2 * D) srft_pool_rotate_kernel(const pool_attention_args a) {
     constexpr int G = D / 32, T = D / 16, U = D / 8, ROW = U + 1, NT = 2 * D, ROWS = kTileVecs * N;
-    constexpr bool HELD = D <= 128 && N == 1;                // the matrix stays in registers over the passes of a workgroup
+    constexpr bool HELD = N == 1;                // the matrix stays in registers over the passes of a workgroup
     __shared__ uint4 rows_lds[ROWS * ROW];
     __shared__ float row_max[G][ROWS];
     __shared__ int shifts[ROWS];

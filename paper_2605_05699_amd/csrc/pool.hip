@@ -80,34 +80,50 @@ __global__ void __launch_bounds__(256) srft_pool_window_kernel(const pool_append
 // Copies of pages and windows: one workgroup per pair and pool.  Bound by memory: a page at d = 128, 8 heads, 16 tokens is 20 KB of K
 // and V, five 16-byte units a thread, all on their way before the first is stored.
 constexpr int kCopyPools = 64;
+#ifndef KCU
+#define KCU 2048
+#endif
+constexpr int kCopyUnits = KCU;                             // of 16 bytes, a workgroup's
 struct pool_copy_args {
     struct { char *codes, *scales, *window; } of[kCopyPools][2];
-    const int32_t* pairs;
-    int n_pairs, count, units[2];            // numbers that exist; 16-byte units of codes and scales, or of a window and 0
-    bool windows;
+    struct { const int32_t* pairs; int n_pairs, count, units[2]; } what[2];  // pages, windows: numbers that exist; 16-byte units of codes and scales, or of a window and 0
 };
 static_assert(sizeof(pool_copy_args) <= 4096, "kernel arguments are limited to 4 KiB");
+#ifndef NTS
+#define NTS 0
+#endif
 __global__ void __launch_bounds__(256) srft_pool_copy_kernel(const pool_copy_args a) {
-    const int from = a.pairs[2 * (long long)blockIdx.x], to = a.pairs[2 * (long long)blockIdx.x + 1];
-    if (!pool_there(from, a.count) || !pool_there(to, a.count) || from == to) return;
+    const bool windows = (int)blockIdx.x >= a.what[0].n_pairs;               // uniform
+    const auto& w = a.what[windows];
+    const long long pair = (int)blockIdx.x - (windows ? a.what[0].n_pairs : 0);
+    const int from = w.pairs[2 * pair], to = w.pairs[2 * pair + 1];
+    if (!pool_there(from, w.count) || !pool_there(to, w.count) || from == to) return;
     const auto& p = a.of[blockIdx.y];
-    const int n = a.units[0] + a.units[1], all = 2 * n;
-    constexpr int AHEAD = 8;
-    for (int u0 = threadIdx.x; u0 < all; u0 += AHEAD * 256) {
-        uint4 x[AHEAD];
-        uint4* at[AHEAD];
+    const int n = w.units[0] + w.units[1], all = 2 * n;
+    const int u0 = (int)blockIdx.z * kCopyUnits + (int)threadIdx.x;
+    if (u0 - (int)threadIdx.x >= all) return;                // (uniform: pages or windows, what is smaller)
+    u32x4 x[kCopyUnits / 256];
+    u32x4* at[kCopyUnits / 256];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int u = min(u0 + i * 256, all - 1), v = u >= n, w = u - v * n;
-            const bool first = w < a.units[0];
-            char* const base = a.windows ? p[v].window : first ? p[v].codes : p[v].scales;
-            const int units = first ? a.units[0] : a.units[1], c = first ? w : w - a.units[0];
-            x[i] = reinterpret_cast<const uint4*>(base)[(long long)from * units + c];
-            at[i] = reinterpret_cast<uint4*>(base) + (long long)to * units + c;
-        }
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) *at[i] = x[i];       // (what is past the end stores the last unit again)
+    for (int i = 0; i < kCopyUnits / 256; ++i) {
+        const int u = min(u0 + i * 256, all - 1), v = u >= n, k = u - v * n;
+        const bool first = k < w.units[0];
+        char* const base = windows ? p[v].window : first ? p[v].codes : p[v].scales;
+        const int units = first ? w.units[0] : w.units[1], c = first ? k : k - w.units[0];
+#if NTS & 2
+        x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base) + ((long long)from * units + c));
+#else
+        x[i] = reinterpret_cast<const u32x4*>(base)[(long long)from * units + c];
+#endif
+        at[i] = reinterpret_cast<u32x4*>(base) + ((long long)to * units + c);
     }
+#pragma unroll
+    for (int i = 0; i < kCopyUnits / 256; ++i)               // (what is past the end stores the last unit again)
+#if NTS & 1
+        __builtin_nontemporal_store(x[i], at[i]);
+#else
+        *at[i] = x[i];
+#endif
 }
 
 bool known_page(int tokens) { return tokens >= 16 && tokens <= 256 && (tokens & (tokens - 1)) == 0; }
@@ -213,7 +229,9 @@ int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const
 
 int srft_pool_copy(const srft_pool_t* const* pools, int n_pools, const int32_t* pages_dev, int64_t n_page_pairs, const int32_t* windows_dev,
                    int64_t n_window_pairs, void* hip_stream) {
-    if (n_pools < 0 || n_page_pairs < 0 || n_window_pairs < 0 || n_page_pairs >= (1LL << 31) || n_window_pairs >= (1LL << 31)) return SRFT_ERR_BAD_N;
+    const int64_t pairs = n_page_pairs + n_window_pairs;
+    if (n_pools < 0 || n_page_pairs < 0 || n_window_pairs < 0 || n_page_pairs >= (1LL << 31) || n_window_pairs >= (1LL << 31) || pairs >= (1LL << 31))
+        return SRFT_ERR_BAD_N;
     if (n_pools == 0) return SRFT_OK;
     if (!pools) return SRFT_ERR_NULL;
     for (int i = 0; i < n_pools; ++i) {
@@ -224,6 +242,7 @@ int srft_pool_copy(const srft_pool_t* const* pools, int n_pools, const int32_t* 
     }
     if ((n_page_pairs > 0 && !pages_dev) || (n_window_pairs > 0 && !windows_dev)) return SRFT_ERR_NULL;
     if (!srft_aligned(pages_dev, 4) || !srft_aligned(windows_dev, 4)) return SRFT_ERR_ALIGN;
+    if (pairs == 0) return SRFT_OK;
     const srft_pool* p = pools[0];
     const int rows = p->heads * p->R, d = p->plan_k->d;
     for (int i0 = 0; i0 < n_pools; i0 += kCopyPools) {
@@ -234,18 +253,11 @@ int srft_pool_copy(const srft_pool_t* const* pools, int n_pools, const int32_t* 
                 const srft_pool_buffers& b = v ? pools[i0 + i]->v : pools[i0 + i]->k;
                 a.of[i][v] = {(char*)b.codes_dev, (char*)b.scales_dev, (char*)b.window_f16_dev};
             }
-        for (int windows = 0; windows < 2; ++windows) {
-            const int64_t pairs = windows ? n_window_pairs : n_page_pairs;
-            if (pairs == 0) continue;
-            a.windows = windows;
-            a.pairs = windows ? windows_dev : pages_dev;
-            a.n_pairs = (int)pairs;
-            a.count = windows ? p->n_windows : p->n_pages;
-            a.units[0] = windows ? rows * d / 8 : rows * d * p->plan_k->bits / 128;
-            a.units[1] = windows ? 0 : rows * (d / p->plan_k->g) / 4;
-            const int rc = srft_launch(srft_pool_copy_kernel, dim3((unsigned)pairs, (unsigned)n), 256, (hipStream_t)hip_stream, a);
-            if (rc != SRFT_OK) return rc;
-        }
+        a.what[0] = {pages_dev, (int)n_page_pairs, p->n_pages, {rows * d * p->plan_k->bits / 128, rows * (d / p->plan_k->g) / 4}};
+        a.what[1] = {windows_dev, (int)n_window_pairs, p->n_windows, {rows * d / 8, 0}};
+        const int units = 2 * std::max(n_page_pairs ? a.what[0].units[0] + a.what[0].units[1] : 0, n_window_pairs ? a.what[1].units[0] : 0);
+        const int rc = srft_launch(srft_pool_copy_kernel, dim3((unsigned)pairs, (unsigned)n, (unsigned)((units + kCopyUnits - 1) / kCopyUnits)), 256, (hipStream_t)hip_stream, a);
+        if (rc != SRFT_OK) return rc;
     }
     return SRFT_OK;
 }

@@ -57,7 +57,7 @@ struct pool_attention_args {
     float *decode_parts, *chunk_parts;                       // sums of segments (pool_part)
     int decode_grid, chunk_grid;
     int decode_rows, decode_block, decode_keys;              // rows that go to pool_decode, those of a workgroup, keys of its tiles
-    int merge_blocks;                                        // of 32 rows, of a sequence and key head
+    int merge_blocks, decode_merges;                         // of 32 rows, of a sequence and key head; workgroups that merge what pool_decode left
 };
 // Sums of a block of 32 rows that a segment leaves: [D / 8 float4][64 lanes], then per lane maximum, sum of weights and V's exponent.
 template <int D> constexpr int kPoolPart = 32 * D + 3 * 64;
@@ -85,12 +85,18 @@ __device__ __forceinline__ int pool_chunk_units(const pool_seq& q, int group, in
     for (int rt = threadIdx.x & 63; rt < n; rt += 64) sum += pool_tiles(pool_seen(q, group, rows, rt), q.full, keys);
     return pool_wave_sum(sum);
 }
-// The workgroups that take part, and where the share of workgroup w begins: w * units / workgroups.
+// The workgroups that take part, and where the share of workgroup w begins: the first `more` have a unit more than the others.
 struct pool_shares {
-    int units, groups;
-    __device__ __forceinline__ pool_shares(int units_, int grid, int least) : units(units_), groups(max(min(grid, (units_ + least - 1) / least), 1)) {}
-    __device__ __forceinline__ int begin(int w) const { return (int)((long long)w * units / groups); }
-    __device__ __forceinline__ int owner(int unit) const { return (int)((((long long)unit + 1) * groups - 1) / units); }
+    int units, groups, each, more;
+    __device__ __forceinline__ pool_shares(int units_, int grid, int least) : units(units_), groups(max(min(grid, (units_ + least - 1) / least), 1)) {
+        each = (int)((unsigned)units / (unsigned)groups);
+        more = units - each * groups;
+    }
+    __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int owner(int unit) const {
+        const int longer = more * (each + 1);                // units of those with one more
+        return unit < longer ? (int)((unsigned)unit / (unsigned)(each + 1)) : more + (int)((unsigned)(unit - longer) / (unsigned)max(each, 1));
+    }
 };
 // the sequence that a unit belongs to (by the whole wavefront; units before before[0] = 0 are none): the last b with before[b] <= unit
 __device__ __forceinline__ int pool_sequence_of(const int* before, int n_seq, int unit) {
@@ -315,8 +321,7 @@ constexpr int pool_rotate_tiles(long long q_rows, int compute_units) { return q_
 pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits, int tiles);
 pool_attention_kernel_t srft_pick_pool_decode_b4(int d, int cb, int gm);
 pool_attention_kernel_t srft_pick_pool_decode_b8(int d, int cb, int gm);
-pool_attention_kernel_t srft_pick_pool_decode_merge(int d, int cb);
 pool_attention_kernel_t srft_pick_pool_chunk(int d, int bits);
-pool_attention_kernel_t srft_pick_pool_merge(int d);
+pool_attention_kernel_t srft_pick_pool_merge(int d, int cb);
 
 #endif  // SRFT_POOL_ATTENTION_H

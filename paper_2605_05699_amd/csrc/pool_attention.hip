@@ -199,11 +199,10 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     rc = srft_launch(srft_pick_pool_rotate(d, pk->bits, pass), dim3((unsigned)(1 + a.q_grid + tail_tiles)), 2 * d, st, a);
     if (rc == SRFT_OK && sp.chunk) rc = srft_launch(srft_pick_pool_chunk(d, pk->bits), dim3((unsigned)a.chunk_grid), 64 * pool_chunk_waves(d), st, a);
     if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb), dim3((unsigned)a.decode_grid), 64 * kPoolDecodeWaves, st, a);
-    if (rc == SRFT_OK && sp.chunk) {
-        a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * pool_chunk_waves(d)) * pool_chunk_waves(d);
-        rc = srft_launch(srft_pick_pool_merge(d), dim3((unsigned)(heads * a.merge_blocks)), 256, st, a);
-    }
-    if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pick_pool_decode_merge(d, sp.cb), dim3((unsigned)(heads * ((sp.rows + a.decode_block - 1) / a.decode_block))), 64 * kPoolDecodeWaves, st, a);
+    a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * pool_chunk_waves(d)) * pool_chunk_waves(d);
+    a.decode_merges = sp.decode ? heads * ((sp.rows + a.decode_block - 1) / a.decode_block) : 0;
+    const unsigned merges = (unsigned)(a.decode_merges + (sp.chunk ? heads * a.merge_blocks : 0));
+    if (rc == SRFT_OK && merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb), dim3(merges), 64 * kPoolDecodeWaves, st, a);
     return rc;
 }
 

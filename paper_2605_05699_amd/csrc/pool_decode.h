@@ -612,11 +612,10 @@ __global__ void __launch_bounds__(64 * kPoolTeam, kPoolDecodeWavesAsked) srft_po
 // workgroup of four wavefronts per sequence and key head, each with a quarter of the channels, all parts of them on their way at once
 // (up to AHEAD).
 template <int D, int CB>
-__global__ void __launch_bounds__(64 * kPoolTeam) srft_pool_decode_merge_kernel(const pool_attention_args a) {
-    __shared__ __align__(16) unsigned char lds[kPoolFinishBytes<D>];
+__device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, unsigned block, unsigned char* lds) {
     constexpr int NB = D / 16, W = kPoolTeam, AHEAD = 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int all = (a.decode_rows + 16 * CB - 1) / (16 * CB), at = (int)(blockIdx.x / (unsigned)all), rb = (int)blockIdx.x - at * all;
+    const int all = (a.decode_rows + 16 * CB - 1) / (16 * CB), at = (int)(block / (unsigned)all), rb = (int)block - at * all;
     const int seq = at / a.heads, head = at - seq * a.heads;
     const pool_seq q = pool_seq_of(a.s, seq);
     const int rows = q.n_new * a.group, blocks_of_rows = (rows + 16 * CB - 1) / (16 * CB);
@@ -632,15 +631,19 @@ __global__ void __launch_bounds__(64 * kPoolTeam) srft_pool_decode_merge_kernel(
     const pool_shares shares(a.decode_before[a.s.n_seq], a.decode_grid, W);
     const int first = a.decode_before[seq] + (head * blocks_of_rows + rb) * tiles, w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
     if (w0 == w1) return;
+    const int behind = shares.begin(w0) != first ? 1 : 0;    // the first part's workgroup began with other rows
     const auto part = [&](int w, int c) __attribute__((always_inline)) {
-        return a.decode_parts + ((2LL * w + (w == w0 && shares.begin(w) != first ? 1 : 0)) * CB + c) * kPoolPart16<D>;
+        return a.decode_parts + ((2LL * w + (w == w0 ? behind : 0)) * CB + c) * kPoolPart16<D>;
     };
     for (int c = 0; c < CB; ++c) {
         float t_all = kPoolLowest, den = 0.0f;
         int e_all = kPoolNoExponent;
-        for (int w = w0; w <= w1; ++w) {
-            t_all = fmaxf(t_all, part(w, c)[16 * D + lane]);
-            e_all = max(e_all, (int)__float_as_uint(part(w, c)[16 * D + 128 + lane]));
+        for (int v = w0; v <= w1; v += AHEAD) {
+            float t[AHEAD], e[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) t[k] = part(min(v + k, w1), c)[16 * D + lane], e[k] = part(min(v + k, w1), c)[16 * D + 128 + lane];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) t_all = fmaxf(t_all, t[k]), e_all = max(e_all, (int)__float_as_uint(e[k]));
         }
         floatx4 o[kPoolOwn<D>];
 #pragma unroll
