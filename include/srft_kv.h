@@ -283,13 +283,13 @@ int srft_lambda_from_absmax(const float* amax_host, int d, float* lambda_host);
  * The first `rot` channels of a row are rot / 2 pairs (a, b); with t = positions[token] * freq[pair]
  *     a' = factor (a cos t - b sin t),   b' = factor (a sin t + b cos t);   the channels from rot on are copied.
  * inverse != 0 turns by -t: with the same factor that is the gradient of the call with inverse = 0.
- *   rows        HOST array of `count` tensors (1 .. SRFT_ROTARY_MAX), each [n_tokens][n_heads][d] in in_dev and out_dev with the
+ *   rows        HOST array of `count` tensors (0 .. SRFT_ROTARY_MAX), each [n_tokens][n_heads][d] in in_dev and out_dev with the
  *               given strides in elements (the channels next to each other).  out_dev == in_dev with the same strides and type
  *               turns in place; overlapping otherwise is not allowed.  Every pointer is aligned to its element.
  *   layout      SRFT_ROTARY_HALF: pair i is channels i and i + rot / 2.  SRFT_ROTARY_PAIRS: channels 2 i and 2 i + 1.
  *   positions_dev  [n_tokens] int32;  freq_dev [rot / 2] fp64, radians per token (of a long context: whatever scaling the
  *               model takes, srft_rotary knows of none).  Angles are formed and reduced in 64 bits.
- * d even, 2 <= d <= 1024, rot even, 0 <= rot <= d, types of srft_dtype, n_tokens * n_heads < 2^31 (else SRFT_ERR_BAD_N).  n_tokens == 0 is
+ * d even, 2 <= d <= 1024, rot even, 0 <= rot <= d, types of srft_dtype, n_tokens * n_heads < 2^31 (else SRFT_ERR_BAD_N).  n_tokens == 0 or count == 0 is
  * a successful no-op.  One kernel.
  */
 typedef enum srft_dtype { SRFT_F32 = 0, SRFT_F16 = 1, SRFT_BF16 = 2 } srft_dtype;

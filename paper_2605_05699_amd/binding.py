@@ -131,7 +131,8 @@ def lib() -> C.CDLL:
     if _marshal is not None:
         entries = ("srft_kv_quantize", "srft_kv_dequantize", "srft_kv_quantize_batched", "srft_kv_dequantize_batched", "srft_kv_scores",
                    "srft_kv_decode_attention", "srft_kv_channel_absmax", "srft_cache_append", "srft_scores_workspace_bytes",
-                   "srft_decode_attention_workspace_bytes", "srft_plan_d")
+                   "srft_decode_attention_workspace_bytes", "srft_plan_d", "srft_rotary", "srft_pool_append", "srft_pool_attention",
+                   "srft_pool_copy", "srft_pool_append_workspace_bytes", "srft_pool_attention_workspace_bytes")
         if _marshal.bind(*[C.cast(getattr(L, name), vp).value for name in entries], vp, C.Array):
             _native_append(L)
             _native_calls()
@@ -149,10 +150,12 @@ def _not_made(*args):
 
 
 _fast_quantize = _fast_dequantize = _fast_scores = _fast_attention = _fast_absmax = _fast_quantize_batched = _fast_dequantize_batched = _not_made
+_fast_rotary = _fast_pool_append = _fast_pool_attention = _fast_pool_copy = _not_made
 
 
 def _native_calls() -> None:
-    for name in ("quantize", "dequantize", "scores", "attention", "absmax", "quantize_batched", "dequantize_batched"):
+    for name in ("quantize", "dequantize", "scores", "attention", "absmax", "quantize_batched", "dequantize_batched", "rotary",
+                 "pool_append", "pool_attention", "pool_copy"):
         globals()["_fast_" + name] = getattr(_marshal, name)
 
 
@@ -484,6 +487,10 @@ def srft_rotary(items, positions: torch.Tensor, freq: torch.Tensor, layout: str 
     items = list(items)
     if not items:
         return
+    if stream is None:
+        status = _fast_rotary(items, positions, freq, ROTARY_LAYOUTS[layout], factor, inverse)
+        if status is not None:
+            return _check(status, "srft_rotary") if status else None
     n, _, d = items[0][0].shape
     if positions.shape != (n,) or freq.dim() != 1:
         raise ValueError("positions must be [tokens], freq one-dimensional")
@@ -573,6 +580,7 @@ class PoolTable:
     def __init__(self, pools):
         self.pools = list(pools)
         self.handles = (C.c_void_p * len(self.pools))(*[int(p.handle) for p in self.pools])
+        self.address = C.addressof(self.handles)
 
 
 def _sized(bytes_: int, where: str) -> int:
@@ -593,6 +601,10 @@ def srft_pool_append_workspace_bytes(pool: PagePool, seqs: PagedSeqs, n_new: int
 
 def srft_pool_append(pool: PagePool, seqs: PagedSeqs, k: torch.Tensor, v: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """New tokens k, v [n_new, heads, d] fp16 into the pages and windows of their sequences."""
+    if stream is None:
+        status = _fast_pool_append(pool.handle, seqs.address, pool.heads, pool.d, k, v, workspace)
+        if status is not None:
+            return _check(status, "srft_pool_append") if status else None
     n = k.shape[0]
     if k.dtype != torch.float16 or v.dtype != torch.float16 or k.shape != (n, pool.heads, pool.d) or v.shape != k.shape:
         raise ValueError("k and v must be float16 [n_new, heads, d]")
@@ -609,6 +621,10 @@ def srft_pool_attention_workspace_bytes(pool: PagePool, seqs: PagedSeqs, n_new: 
 def srft_pool_attention(pool: PagePool, seqs: PagedSeqs, q: torch.Tensor, softmax_scale: float, out: torch.Tensor, workspace: torch.Tensor,
                         stream=None) -> None:
     """out <- causal attention of q [n_new, q heads, d] (float16 or bfloat16) over the tokens that the pool holds."""
+    if stream is None:
+        status = _fast_pool_attention(pool.handle, seqs.address, pool.d, q, softmax_scale, out, workspace)
+        if status is not None:
+            return _check(status, "srft_pool_attention") if status else None
     n, heads, d = q.shape
     if q.dtype not in (torch.float16, torch.bfloat16) or out.dtype != q.dtype or out.shape != q.shape or d != pool.d:
         raise ValueError("q and out must be [n_new, q heads, d], both float16 or both bfloat16")
@@ -620,6 +636,10 @@ def srft_pool_attention(pool: PagePool, seqs: PagedSeqs, q: torch.Tensor, softma
 
 def srft_pool_copy(table: PoolTable, pages: torch.Tensor, windows: torch.Tensor, stream=None) -> None:
     """Pages pages[i, 0] -> pages[i, 1] and windows windows[i, 0] -> windows[i, 1] (int32 [n, 2] on the device) in every pool of the table."""
+    if stream is None:
+        status = _fast_pool_copy(table.address, len(table.pools), pages, windows)
+        if status is not None:
+            return _check(status, "srft_pool_copy") if status else None
     for t, name in ((pages, "pages"), (windows, "windows")):
         if t.dim() != 2 or t.shape[1] != 2:
             raise ValueError(f"{name} must be [n, 2]")

@@ -34,6 +34,12 @@ struct {
     decltype(&srft_scores_workspace_bytes) scores_bytes;
     decltype(&srft_decode_attention_workspace_bytes) attention_bytes;
     decltype(&srft_plan_d) plan_d;
+    decltype(&srft_rotary) rotary;
+    decltype(&srft_pool_append) pool_append;
+    decltype(&srft_pool_attention) pool_attention;
+    decltype(&srft_pool_copy) pool_copy;
+    decltype(&srft_pool_append_workspace_bytes) pool_append_bytes;
+    decltype(&srft_pool_attention_workspace_bytes) pool_attention_bytes;
     bool bound;
 } g;
 
@@ -80,6 +86,7 @@ PyObject* made(F body) {
     } catch (...) {
     }
     if (done) return PyLong_FromLong(rc);
+    PyErr_Clear();                                           // (an int past 64 bits)
     Py_RETURN_NONE;
 }
 template <class F>
@@ -206,6 +213,110 @@ PyObject* absmax(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- rotary positions and the paged cache
+// a plain tensor [tokens, heads, channels] on the device whose channels lie next to each other
+const at::Tensor* rows_of(PyObject* o) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.defined() && t.is_cuda() && t.layout() == at::kStrided && t.unsafeGetTensorImpl()->has_storage() && t.dim() == 3 &&
+                   (t.size(2) <= 1 || t.stride(2) == 1)
+               ? &t
+               : nullptr;
+}
+int type_of(const at::Tensor& t) {                           // srft_dtype, or -1
+    return t.scalar_type() == at::kFloat ? SRFT_F32 : t.scalar_type() == at::kHalf ? SRFT_F16 : t.scalar_type() == at::kBFloat16 ? SRFT_BF16 : -1;
+}
+// a plain contiguous tensor of any type
+const at::Tensor* space_of(PyObject* o) { return THPVariable_CheckExact(o) ? tensor_of(o, THPVariable_Unpack(o).scalar_type()) : nullptr; }
+
+// rotary(items, positions, freq, layout, factor, inverse)
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return made([&](int* rc) {
+        if (n != 6 || !PyList_CheckExact(a[0]) || !PyLong_CheckExact(a[3]) || !PyFloat_CheckExact(a[4]) || !PyBool_Check(a[5])) return false;
+        const int items = (int)PyList_GET_SIZE(a[0]);
+        if (items < 1 || items > SRFT_ROTARY_MAX) return false;
+        const at::Tensor *pos = tensor_of(a[1], at::kInt), *freq = tensor_of(a[2], at::kDouble);
+        if (!pos || !freq || pos->dim() != 1 || freq->dim() != 1) return false;
+        srft_rotary_rows rows[SRFT_ROTARY_MAX] = {};
+        const int64_t tokens = pos->size(0);
+        int64_t d = 0;
+        for (int i = 0; i < items; ++i) {
+            PyObject* const pair = PyList_GET_ITEM(a[0], i);
+            if (!PyTuple_CheckExact(pair) || PyTuple_GET_SIZE(pair) != 2) return false;
+            const at::Tensor *x = rows_of(PyTuple_GET_ITEM(pair, 0)), *y = rows_of(PyTuple_GET_ITEM(pair, 1));
+            if (!x || !y || !x->sizes().equals(y->sizes()) || x->size(0) != tokens || type_of(*x) < 0 || type_of(*y) < 0) return false;
+            if (i == 0) d = x->size(2);
+            if (x->size(2) != d || d > INT32_MAX || x->size(1) > INT32_MAX) return false;
+            rows[i].in_dev = x->data_ptr(), rows[i].in_token = x->stride(0), rows[i].in_head = x->stride(1);
+            rows[i].out_dev = y->data_ptr(), rows[i].out_token = y->stride(0), rows[i].out_head = y->stride(1);
+            rows[i].n_heads = (int32_t)x->size(1), rows[i].in_type = type_of(*x), rows[i].out_type = type_of(*y);
+        }
+        const long layout = PyLong_AsLong(a[3]);
+        const double factor = PyFloat_AS_DOUBLE(a[4]);
+        const bool inverse = a[5] == Py_True;
+        const int32_t* const pp = static_cast<const int32_t*>(pos->data_ptr());
+        const double* const fp = static_cast<const double*>(freq->data_ptr());
+        if (freq->size(0) > INT32_MAX / 2) return false;
+        const int rot = 2 * (int)freq->size(0);
+        void* const st = current_stream();
+        *rc = without_gil([&] { return g.rotary(rows, items, tokens, (int)d, rot, (int)layout, pp, fp, factor, inverse, st); });
+        return true;
+    });
+}
+// pool_append(pool, sequences, heads, d, k, v, workspace)
+PyObject* pool_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return made([&](int* rc) {
+        const srft_pool_t* pool;
+        const srft_paged_seqs* seqs;
+        if (n != 7 || !handle_of(a[0], &pool) || !handle_of(a[1], &seqs) || !pool || !seqs || !PyLong_CheckExact(a[2]) || !PyLong_CheckExact(a[3])) return false;
+        const at::Tensor *k = rows_of(a[4]), *v = rows_of(a[5]), *w = space_of(a[6]);
+        if (!k || !v || !w || k->scalar_type() != at::kHalf || v->scalar_type() != at::kHalf || !k->sizes().equals(v->sizes()) ||
+            k->size(1) != PyLong_AsLong(a[2]) || k->size(2) != PyLong_AsLong(a[3]))
+            return false;
+        const int64_t tokens = k->size(0), need = g.pool_append_bytes(pool, seqs, tokens);
+        if (need < 0 || bytes_of(*w) < need) return false;
+        void *const kp = k->data_ptr(), *const vp = v->data_ptr(), *const wp = w->data_ptr(), *const st = current_stream();
+        const int64_t kt = k->stride(0), kh = k->stride(1), vt = v->stride(0), vh = v->stride(1);
+        *rc = without_gil([&] { return g.pool_append(pool, seqs, kp, vp, tokens, kt, kh, vt, vh, wp, st); });
+        return true;
+    });
+}
+// pool_attention(pool, sequences, d, q, softmax_scale, out, workspace)
+PyObject* pool_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return made([&](int* rc) {
+        const srft_pool_t* pool;
+        const srft_paged_seqs* seqs;
+        if (n != 7 || !handle_of(a[0], &pool) || !handle_of(a[1], &seqs) || !pool || !seqs || !PyLong_CheckExact(a[2]) || !PyFloat_CheckExact(a[4])) return false;
+        const at::Tensor *q = rows_of(a[3]), *o = rows_of(a[5]), *w = space_of(a[6]);
+        if (!q || !o || !w || type_of(*q) <= SRFT_F32 || o->scalar_type() != q->scalar_type() || !q->sizes().equals(o->sizes()) ||
+            q->size(2) != PyLong_AsLong(a[2]) || q->size(1) > INT32_MAX)
+            return false;
+        const int64_t tokens = q->size(0), need = g.pool_attention_bytes(pool, seqs, tokens, (int)q->size(1));
+        if (need < 0 || bytes_of(*w) < need) return false;
+        void *const qp = q->data_ptr(), *const op = o->data_ptr(), *const wp = w->data_ptr(), *const st = current_stream();
+        const int64_t qt = q->stride(0), qh = q->stride(1), ot = o->stride(0), oh = o->stride(1);
+        const int heads = (int)q->size(1), type = type_of(*q);
+        const float scale = (float)PyFloat_AS_DOUBLE(a[4]);
+        *rc = without_gil([&] { return g.pool_attention(pool, seqs, qp, type, tokens, heads, qt, qh, scale, op, ot, oh, wp, st); });
+        return true;
+    });
+}
+// pool_copy(handles, count, pages, windows)
+PyObject* pool_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return made([&](int* rc) {
+        const srft_pool_t* const* pools;
+        if (n != 4 || !handle_of(a[0], &pools) || !PyLong_CheckExact(a[1])) return false;
+        const at::Tensor *p = tensor_of(a[2], at::kInt), *w = tensor_of(a[3], at::kInt);
+        if (!p || !w || p->dim() != 2 || w->dim() != 2 || p->size(1) != 2 || w->size(1) != 2) return false;
+        const int32_t *const pp = static_cast<const int32_t*>(p->data_ptr()), *const wp = static_cast<const int32_t*>(w->data_ptr());
+        const int64_t pages = p->size(0), windows = w->size(0);
+        const int count = (int)PyLong_AsLong(a[1]);
+        void* const st = current_stream();
+        *rc = without_gil([&] { return g.pool_copy(pools, count, pp, pages, wp, windows, st); });
+        return true;
+    });
+}
+
 // ---- lib().srft_cache_append, a ctypes function of a type of its own whose calls come here first: those with other arguments than
 // None, ints, c_void_p and arrays of them go on to ctypes.  (As the type's slot: by way of a __call__ in Python's sight a call took 0.03 us
 // more.)
@@ -253,10 +364,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // bind(addresses, c_void_p, Array): of the entry points, in the order of the struct above.  True: they are the ones called here; False: those
 // of another library are, which came first.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    constexpr int kCount = 11;
+    constexpr int kCount = 17;
     void* p[kCount];
     if (n != kCount + 2 || !PyType_Check(a[kCount]) || !PyType_Check(a[kCount + 1])) {
-        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of 11 entry points, c_void_p and Array");
+        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of 17 entry points, c_void_p and Array");
         return nullptr;
     }
     for (int i = 0; i < kCount; ++i) {
@@ -273,10 +384,11 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g.bound = true;
     Py_RETURN_TRUE;
 }
-static_assert(offsetof(decltype(g), bound) == 11 * sizeof(void*), "bind fills the pointers in order");
+static_assert(offsetof(decltype(g), bound) == 17 * sizeof(void*), "bind fills the pointers in order");
 
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(quantize), FAST(dequantize), FAST(scores), FAST(attention), FAST(absmax), FAST(append), FAST(bind),
+                         FAST(rotary), FAST(pool_append), FAST(pool_attention), FAST(pool_copy),
                          {"quantize_batched", quantize_batched, METH_O, nullptr},
                          {"dequantize_batched", dequantize_batched, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
