@@ -23,9 +23,9 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
     constexpr int W = kPoolChunkWaves<D>, NT = 64 * W, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * W, KB = KEYS / 32;
     constexpr int T = D / 16, CB = D * BITS / 8;
     constexpr int KROW = 2 * D + 16, VROW = 2 * D + 32;      // bytes of a row in LDS: 16-byte reads of 32 rows, transposed reads of 8, on different banks
-    constexpr int UNITS = KEYS * T;                          // of 16 channels, of K or of V
-    constexpr int N = (2 * UNITS + NT - 1) / NT;             // a thread's
-    static_assert(UNITS % 64 == 0 && N <= 2, "a wavefront's units are of one kind, a thread has one or two");
+    constexpr int UNITS = KEYS * T;                          // of 16 channels, of K and of V each
+    constexpr int N = 2 * UNITS <= NT ? 1 : 2;               // a thread's: one of K or of V (then all of the wavefront's), or one place of both
+    static_assert(UNITS % 64 == 0 && UNITS <= NT && (N == 2 || 64 * W % UNITS == 0), "whole wavefronts");
     typedef typename pool_codes<BITS>::type code_t;
     __shared__ __align__(16) unsigned char k_lds[2][KEYS * KROW], v_lds[2][KEYS * VROW];
     __shared__ uint4 ring[4];                                // of tile t % 4: largest scales (bits) of K, of V where they outgrew the exponents; blocks of 16
@@ -41,24 +41,14 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
     int seq = __builtin_amdgcn_readfirstlane(pool_sequence_of(a.chunk_before, a.s.n_seq, unit));
     const int R = 1 << a.s.log_R, n_scales = D / a.g;
 
-    // a thread's units: K's first, then V's; which key of the tile, which 16 channels
-    bool u_v[N];                                             // (of the whole wavefront)
-    int u_block[N], u_key[N], u_at[N], off_code[N], off_scale[N];
-    unsigned char* dst[N];                                   // in the first buffer
-    bool second[N];                                          // the key is in the second block of 16 that the wavefront's units touch
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int u0 = min(wave * 64 + i * NT, 2 * UNITS - 64), u = u0 + lane;           // (past the end: the last units again)
-        u_v[i] = u0 >= UNITS;
-        const int r = u_v[i] ? u - UNITS : u, r0 = u_v[i] ? u0 - UNITS : u0;
-        u_key[i] = r / T;
-        u_at[i] = r - u_key[i] * T;
-        u_block[i] = r0 / T / 16;
-        second[i] = u_key[i] / 16 != u_block[i];
-        off_code[i] = (u_key[i] & 15) * CB + u_at[i] * (int)sizeof(code_t);
-        off_scale[i] = 4 * ((u_key[i] & 15) * n_scales + 16 * u_at[i] / a.g);
-        dst[i] = (u_v[i] ? v_lds[0] + u_key[i] * VROW : k_lds[0] + u_key[i] * KROW) + 32 * u_at[i];
-    }
+    // a thread's units: which key of the tile, which 16 channels (wavefronts beyond the last unit take units that others have too)
+    const int r0 = N == 1 ? wave * 64 % UNITS : min(wave * 64, UNITS - 64), r = r0 + lane;
+    const bool only_v = N == 1 && (wave * 64 / UNITS & 1) == 1;
+    const auto is_v = [&](int i) __attribute__((always_inline)) { return N == 2 ? i == 1 : only_v; };
+    const int u_key = r / T, u_at = r - u_key * T, u_block = r0 / T / 16;
+    const bool second = u_key / 16 != u_block;               // the key is in the second block of 16 that the wavefront's units touch
+    const uint32_t off_code = (u_key & 15) * CB + u_at * (int)sizeof(code_t), off_scale = 4 * ((u_key & 15) * n_scales + 16 * u_at / a.g);
+    unsigned char *const k_dst = k_lds[0] + u_key * KROW + 32 * u_at, *const v_dst = v_lds[0] + u_key * VROW + 32 * u_at;    // in the first buffer
 
     for (bool at_begin = true; unit < end; at_begin = false) {
         while (seq + 1 < a.s.n_seq && a.chunk_before[seq + 1] <= unit) ++seq;
@@ -74,11 +64,12 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
         const int t1 = min(tiles, t0 + end - unit);
         if (t1 <= t0) return;                                // (only if the device arrays were written during the call)
         const int seen = pool_seen(q, a.group, ROWS, rt), page_tiles = (max(min(seen, q.full), 0) + KEYS - 1) / KEYS, tail = q.length - q.full;
-        const pool_row row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + l32);
+        pool_row row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + l32);
         const long long q_row = (long long)row.token * (a.heads * a.group) + row.head;
+        const int row_last = row.last;
         const int32_t* const table = a.s.table + seq * a.s.max_pages;
         // (the last token that any row of this wavefront sees; rows do not see less than those before them)
-        int wave_last = row.last;
+        int wave_last = row_last;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) wave_last = max(wave_last, __shfl_xor(wave_last, d));
         wave_last = __builtin_amdgcn_readfirstlane(wave_last);
@@ -122,7 +113,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) f[j] = read_v(j);
-            const int last = min(row.last, last_key) - key0;
+            const int last = min(row_last, last_key) - key0;
             if (__ballot(last < KEYS - 1) || missing) {
                 const int limit = last - 4 * half;           // (compared with constants)
 #pragma unroll
@@ -153,56 +144,56 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
             code_t code[N];
             typedef float pair __attribute__((ext_vector_type(2)));
             pair scale{0, 0};                                // (a native vector: an array ends up in LDS)
-            uint32_t there = 0;                              // of the tile fetched last: bits 2 i, 2 i + 1: the pages of unit i's two blocks
-            // the pages of a wavefront's blocks of 16 keys, unit i's in lanes 2 i and 2 i + 1; behind the last page, the last block again
+            uint32_t there = 0;                              // of the tile fetched last: the pages of its two blocks (bits)
+            // the pages of the wavefront's blocks of 16 keys, in lanes 0 and 1; behind the last page, the last block again
             const auto pages_of = [&](int tile) __attribute__((always_inline)) {
-                int block = u_block[0] + (lane & 1);
-                if constexpr (N > 1) block = (lane >> 1 & 1) == 1 ? u_block[1] + (lane & 1) : block;
-                return table[min(tile * KEYS + 16 * block, q.full - 16) >> a.s.log_R];
+                return table[min(tile * KEYS + 16 * (u_block + (lane & 1)), q.full - 16) >> a.s.log_R];
             };
             const auto fetch = [&](int tile, int pages) __attribute__((always_inline)) {
                 there = 0;
+                constexpr bool ONE = 64 % T == 0 && 64 / T <= 16;            // the wavefront's units lie in one block
+                uint64_t at[2];
+#pragma unroll
+                for (int k = 0; k < (ONE ? 1 : 2); ++k) {
+                    const int page = __builtin_amdgcn_readlane(pages, k), slot = min(tile * KEYS + 16 * (u_block + k), q.full - 16) & (R - 1);
+                    const bool ok = pool_there(page, a.s.n_pages);
+                    there |= (ok ? 1u : 0u) << k;
+                    at[k] = ((uint64_t)((ok ? page : 0) * (uint64_t)a.heads + head) << a.s.log_R) + slot;
+                }
+                if (ONE) there |= there << 1;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    uint64_t c0, c1, f0, f1;
-                    const auto address = [&](int k, uint64_t& c, uint64_t& f) __attribute__((always_inline)) {
-                        const int page = __builtin_amdgcn_readlane(pages, 2 * i + k), slot = min(tile * KEYS + 16 * (u_block[i] + k), q.full - 16) & (R - 1);
-                        const bool ok = pool_there(page, a.s.n_pages);
-                        there |= (ok ? 1u : 0u) << (2 * i + k);
-                        const uint64_t at = ((uint64_t)((ok ? page : 0) * (uint64_t)a.heads + head) << a.s.log_R) + slot;
-                        c = at * CB;
-                        f = at * (4 * n_scales);
-                        asm("" : "+s"(c), "+s"(f));
+                    typedef __attribute__((address_space(1))) const char* global_t;
+                    const auto load = [&](const void* base, uint64_t bytes, uint32_t off, auto* to) __attribute__((always_inline)) {
+                        // a scalar address for each block (the asm keeps the compiler from adding a lane's offset to the base, a pair of registers for each array)
+                        global_t p0 = (global_t)base + at[0] * bytes, p1 = p0;
+                        if constexpr (!ONE) p1 = (global_t)base + at[1] * bytes;
+                        asm("" : "+s"(p0));
+                        if constexpr (!ONE) asm("" : "+s"(p1));
+                        *to = *(__attribute__((address_space(1))) const std::remove_reference_t<decltype(*to)>*)((ONE || !second ? p0 : p1) + off);
                     };
-                    address(0, c0, f0);
-                    if constexpr (64 % T == 0 && 64 / T <= 16) {             // the wavefront's units lie in one block
-                        c1 = c0, f1 = f0;
-                        there |= (there >> (2 * i) & 1) << (2 * i + 1);
-                    } else {
-                        address(1, c1, f1);
-                    }
-                    const uint8_t* const codes = u_v[i] ? a.vb.codes_dev : a.kb.codes_dev;
-                    const char* const scales = (const char*)(u_v[i] ? a.vb.scales_dev : a.kb.scales_dev);
-                    code[i] = *reinterpret_cast<const code_t*>(codes + (second[i] ? c1 : c0) + off_code[i]);
-                    scale[i] = *reinterpret_cast<const float*>(scales + (second[i] ? f1 : f0) + off_scale[i]);
+                    float f;
+                    load(is_v(i) ? (const void*)a.vb.codes_dev : a.kb.codes_dev, CB, off_code, &code[i]);
+                    load(is_v(i) ? (const void*)a.vb.scales_dev : a.kb.scales_dev, 4 * n_scales, off_scale, &f);
+                    scale[i] = f;
                 }
             };
             // what of the fetched tile the others have to know: scales that outgrow the exponents, missing pages
             const auto check = [&](int tile) __attribute__((always_inline)) {
                 const float most_k = pool_power(ek + 15 - kPoolAmp<BITS>), most_v = pool_power(ev + 15 - kPoolAmp<BITS>);
-                bool news = there != (1u << (2 * N)) - 1;    // uniform
+                bool news = there != 3;                      // uniform
 #pragma unroll
-                for (int i = 0; i < N; ++i) news |= __ballot(!(scale[i] < (u_v[i] ? most_v : most_k))) != 0;
+                for (int i = 0; i < N; ++i) news |= __ballot(!(scale[i] < (is_v(i) ? most_v : most_k))) != 0;
                 if (news) {
+                    const bool ok = there >> (second ? 1 : 0) & 1;
+                    uint32_t* const at = reinterpret_cast<uint32_t*>(&ring[tile & 3]);
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const bool ok = there >> (2 * i + (second[i] ? 1 : 0)) & 1;
                         scale[i] = ok ? scale[i] : 0.0f;
                         const float m = pool_wave_max(scale[i]);
-                        uint32_t* const at = reinterpret_cast<uint32_t*>(&ring[tile & 3]);
-                        if (lane == 0) atomicMax(&at[u_v[i] ? 1 : 0], __float_as_uint(m));
-                        if (!ok) atomicOr(&at[2], 1u << (u_key[i] >> 4));
+                        if (lane == 0) atomicMax(&at[is_v(i) ? 1 : 0], __float_as_uint(m));
                     }
+                    if (!ok) atomicOr(&at[2], 1u << (u_key >> 4));
                 }
             };
             const auto decode = [&](int tile) __attribute__((always_inline)) {
@@ -211,8 +202,8 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     half8 x, y;
-                    pool_decode16(code[i], (_Float16)(scale[i] * (u_v[i] ? uv : uk)), x, y);
-                    uint4* const to = reinterpret_cast<uint4*>(dst[i] + buffer * (u_v[i] ? KEYS * VROW : KEYS * KROW));
+                    pool_decode16(code[i], (_Float16)(scale[i] * (is_v(i) ? uv : uk)), x, y);
+                    uint4* const to = reinterpret_cast<uint4*>((is_v(i) ? v_dst : k_dst) + buffer * (is_v(i) ? KEYS * VROW : KEYS * KROW));
                     to[0] = __builtin_bit_cast(uint4, x);
                     to[1] = __builtin_bit_cast(uint4, y);
                 }
@@ -260,8 +251,8 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
                 float f[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const long long at = ((long long)((u_v[i] ? a.s.n_seq : 0) + seq) * a.heads + head << a.s.log_R) + min(key0 + u_key[i], tail - 1);
-                    const uint4* const src = reinterpret_cast<const uint4*>(a.tail_rows + at * D) + 2 * u_at[i];
+                    const long long at = ((long long)((is_v(i) ? a.s.n_seq : 0) + seq) * a.heads + head << a.s.log_R) + min(key0 + u_key, tail - 1);
+                    const uint4* const src = reinterpret_cast<const uint4*>(a.tail_rows + at * D) + 2 * u_at;
                     x[i][0] = src[0];
                     x[i][1] = src[1];
                     f[i] = a.tail_factor[at];
@@ -272,7 +263,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const float m = pool_wave_max(f[i] * kUp);
-                    if (lane == 0) atomicMax(reinterpret_cast<uint32_t*>(&ring[0]) + (u_v[i] ? 1 : 0), __float_as_uint(m));
+                    if (lane == 0) atomicMax(reinterpret_cast<uint32_t*>(&ring[0]) + (is_v(i) ? 1 : 0), __float_as_uint(m));
                 }
                 __syncthreads();
                 ek = pool_exponent<BITS>(__uint_as_float(ring[0].x));
@@ -280,9 +271,10 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
                 const float uk = pool_power(-ek), uv = pool_power(-ev);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const _Float16 up = (_Float16)(f[i] * (u_v[i] ? uv : uk));
-                    reinterpret_cast<uint4*>(dst[i])[0] = __builtin_bit_cast(uint4, pool_times(x[i][0], up));
-                    reinterpret_cast<uint4*>(dst[i])[1] = __builtin_bit_cast(uint4, pool_times(x[i][1], up));
+                    const _Float16 up = (_Float16)(f[i] * (is_v(i) ? uv : uk));
+                    uint4* const to = reinterpret_cast<uint4*>(is_v(i) ? v_dst : k_dst);
+                    to[0] = __builtin_bit_cast(uint4, pool_times(x[i][0], up));
+                    to[1] = __builtin_bit_cast(uint4, pool_times(x[i][1], up));
                 }
                 __syncthreads();
                 compute(0, q.full + key0, q.length - 1, 0, __builtin_amdgcn_readfirstlane(ek), __builtin_amdgcn_readfirstlane(ev));
@@ -290,6 +282,9 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_ke
         }
         b.den = pool_halves_sum(b.den);
         if (t0 == 0 && t1 == tiles) {
+            int again = lane;                                // (computed again: kept, the row took registers that the loop lacks at 256 dimensions)
+            asm("" : "+v"(again));
+            row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + (again & 31));
             char* const to = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
             pool_finish<D>(b, a.out_table, a.out_unscale, to, a.bf16, lane);
         } else {
