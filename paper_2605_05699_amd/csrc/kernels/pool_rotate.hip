@@ -2,7 +2,8 @@
 //
 // Three products of rows with a D x D matrix, on the matrix cores with the matrix as fp16 hi + lo: q' = R_k^T q, w = W_k k and w = W_v v.
 // A workgroup has D / 32 wavefronts, each with 32 rows of the matrix; a pass is N tiles of 32 rows.  The results are stored as fp16 under a
-// power of two per row (the exponent of its largest value), in the order of positions; of the queries also what that rounding leaves.
+// power of two per row (the exponent of its largest value), in the order of positions; of the queries also what that rounding leaves,
+// where rows may go to pool_decode.
 // Bound by the matrix, 4 D^2 bytes a pass out of the L2 (256 KB at d = 256), and by the rows: many rows are taken four tiles a pass, few
 // are spread over the compute units, one tile each (pool_rotate_tiles).
 // Workgroups: 0 counts the units of work; 1 .. q_grid take the passes of the queries in turn; the others a part of a window each.
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(2 * D) srft_pool_rotate_kernel(const pool_atte
                 uint4* const dst = reinterpret_cast<uint4*>((queries ? a.q_rows : a.tail_rows) + row * D) + 4 * wave + 2 * half;
                 dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
                 dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
-                if (queries) {
+                if (queries && a.q_rows_low) {               // uniform
                     uint4* const dst_low = reinterpret_cast<uint4*>(a.q_rows_low + row * D) + 4 * wave + 2 * half;
                     dst_low[0] = make_uint4(low[0], low[1], low[2], low[3]);
                     dst_low[1] = make_uint4(low[4], low[5], low[6], low[7]);

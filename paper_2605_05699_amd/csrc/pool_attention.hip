@@ -181,7 +181,6 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     a.decode_before = (int*)(base + w.decode_before);
     a.chunk_before = (int*)(base + w.chunk_before);
     a.q_rows = (unsigned short*)(base + w.q_rows);
-    a.q_rows_low = (unsigned short*)(base + w.q_rows_low);
     a.q_factor = (float*)(base + w.q_factor);
     a.tail_rows = (unsigned short*)(base + w.tail_rows);
     a.tail_factor = (float*)(base + w.tail_factor);
@@ -189,8 +188,9 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     a.decode_parts = (float*)(base + w.decode_parts);
     a.chunk_parts = (float*)(base + w.chunk_parts);
     const split sp = split_of(seqs, n_new, group, d);
+    a.q_rows_low = sp.decode ? (unsigned short*)(base + w.q_rows_low) : nullptr;     // (chunks do not read them)
     a.decode_grid = w.decode_grid;
-    a.decode_rows = sp.rows;
+    a.decode_rows = sp.decode ? sp.rows : 0;                 // (0: the one sequence there is goes to pool_chunk, however few tokens it brings)
     a.decode_block = 16 * sp.cb;
     a.decode_keys = pool_decode_keys(d, sp.cb);
     a.chunk_grid = w.chunk_grid;
@@ -200,7 +200,7 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     if (rc == SRFT_OK && sp.chunk) rc = srft_launch(srft_pick_pool_chunk(d, pk->bits), dim3((unsigned)a.chunk_grid), 64 * pool_chunk_waves(d), st, a);
     if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb), dim3((unsigned)a.decode_grid), 64 * kPoolDecodeWaves, st, a);
     a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * pool_chunk_waves(d)) * pool_chunk_waves(d);
-    a.decode_merges = sp.decode ? heads * ((sp.rows + a.decode_block - 1) / a.decode_block) : 0;
+    a.decode_merges = sp.decode ? heads * ((a.decode_rows + a.decode_block - 1) / a.decode_block) : 0;
     const unsigned merges = (unsigned)(a.decode_merges + (sp.chunk ? heads * a.merge_blocks : 0));
     if (rc == SRFT_OK && merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb), dim3(merges), 64 * kPoolDecodeWaves, st, a);
     return rc;

@@ -244,6 +244,22 @@ def test_pages_and_windows_that_do_not_exist_count_for_nothing_and_rows_that_see
     s.close()
 
 
+@pytest.mark.parametrize("n", [1, 2])
+@pytest.mark.parametrize("group,bound", [(4, 40), (4, 8), (1, 300)])
+def test_fewer_new_tokens_than_the_bound(B, n, group, bound):
+    """What a replayed graph does: launches for `bound` new tokens, and one of them (or none) in the device arrays."""
+    s = Serving(B, 128, 32, 4, 16, 2, n=n, max_length=400, seed=60 + n)
+    s.append([70] * n)
+    new = [1] + [0] * (n - 1)
+    q = queries(s, bound, group, F16)
+    out = s.run(q, new, 0.1, seqs=s.seqs(new, max_new=bound))
+    check(s, q[:1], new, 0.1, out[:1], group)
+    assert out[1:].isnan().all()
+    none = s.run(q, new, 0.1, seqs=s.seqs([0] * n, max_new=bound))
+    assert none.isnan().all()
+    s.close()
+
+
 def test_sequences_without_tokens_and_bounds_that_cut(B):
     s = Serving(B, 64, 32, 4, 16, 2, n=4, max_length=100, seed=43)
     s.append([40, 0, 17, 3])
