@@ -12,6 +12,7 @@ namespace {
 // windows.  A window that is read for a filled page is never the one that tokens are copied into (the caller's two windows), so the
 // two kernels need no order between their parts.  The list is in no fixed order (a counter in LDS); every page is quantized by itself, so the
 // results do not depend on it.
+constexpr int kWindowUnits = 1024;                           // of 16 bytes: what a workgroup copies at a time
 __global__ void __launch_bounds__(256) srft_pool_window_kernel(const pool_append_args a, int U, int split) {
     const pool_seqs& s = a.s;
     const int R = 1 << s.log_R;
@@ -71,9 +72,18 @@ __global__ void __launch_bounds__(256) srft_pool_window_kernel(const pool_append
     const char* const from = v ? a.v : a.k;
     const long long token = v ? a.v_token : a.k_token, head = v ? a.v_head : a.k_head;
     uint4* const to = (uint4*)(v ? a.vb.window_f16_dev : a.kb.window_f16_dev) + (long long)window * a.heads * R * U;
-    for (int u = part * 256 + threadIdx.x; u < n * a.heads * U; u += split * 256) {
-        const int row = u / U, c = u - row * U, j = row / a.heads, h = row - j * a.heads;
-        to[(h * R + first - q.full + j) * U + c] = reinterpret_cast<const uint4*>(from + (q.start + first - q.before + j) * token + h * head)[c];
+    const int all = n * a.heads * U;
+    for (int u0 = part * kWindowUnits + threadIdx.x; u0 < all; u0 += split * kWindowUnits) {
+        uint4 x[kWindowUnits / 256];
+        uint4* at[kWindowUnits / 256];
+#pragma unroll
+        for (int k = 0; k < kWindowUnits / 256; ++k) {       // (past the end the last unit again)
+            const int u = min(u0 + 256 * k, all - 1), row = u / U, c = u - row * U, j = row / a.heads, h = row - j * a.heads;
+            x[k] = reinterpret_cast<const uint4*>(from + (q.start + first - q.before + j) * token + h * head)[c];
+            at[k] = to + ((h * R + first - q.full + j) * U + c);
+        }
+#pragma unroll
+        for (int k = 0; k < kWindowUnits / 256; ++k) *at[k] = x[k];
     }
 }
 
@@ -204,7 +214,10 @@ int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const
     a.tiles_magic = srft_even_magic((int)page_tiles);
     a.list = (int*)workspace_dev;
     const hipStream_t st = (hipStream_t)hip_stream;
-    const int split = std::max(1, std::min(pool->R / 32, std::max(1, 1024 / (2 * seqs->n_seq))));
+    // a workgroup for 16 KB of a window's new tokens, up to 4096 in all (with one for 32 tokens of it, 6 windows of up to 64 tokens at
+    // d = 256 took 9.7 us, now 4.1)
+    const int64_t units = (int64_t)std::min<int64_t>(seqs->max_new, pool->R) * pool->heads * pool->units();
+    const int split = (int)std::max<int64_t>(1, std::min<int64_t>((units + kWindowUnits - 1) / kWindowUnits, 4096 / (2 * seqs->n_seq)));
     rc = srft_launch(srft_pool_window_kernel, dim3((unsigned)(1 + 2 * seqs->n_seq * split)), 256, st, a, pool->units(), split);
     if (rc != SRFT_OK) return rc;
     int threads = 0;
