@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(64 * kPoolTeam, kPoolDecodeWavesAsked) srft_po
             };
             const auto fetch_values = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) vc[i] = *reinterpret_cast<const u32x4*>(a.vb.codes_dev + (code_of(piece_block[i]) + piece_off[i]));
+                for (int i = 0; i < NV; ++i) vc[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.vb.codes_dev + (code_of(piece_block[i]) + piece_off[i])));
             };
             const auto fetch = [&](int tile, int pages) __attribute__((always_inline)) {
                 // Blocks' addresses in scalar registers: in bytes of codes, and of scales.  (The empty asm keeps the choice between them a
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(64 * kPoolTeam, kPoolDecodeWavesAsked) srft_po
                     vf = *reinterpret_cast<const pool_floats<NH>*>(sv);
                 }
 #pragma unroll
-                for (int i = 0; i < NV; ++i) kc[i] = *reinterpret_cast<const u32x4*>(a.kb.codes_dev + (code_of(piece_block[i]) + piece_off[i]));
+                for (int i = 0; i < NV; ++i) kc[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.kb.codes_dev + (code_of(piece_block[i]) + piece_off[i])));
             };
             fetch(t, page_of(t));
             fetch_values();
