@@ -1,8 +1,14 @@
 // Attention over a pool for many rows a key head (a chunk of a prompt): 256 rows (tokens x query heads of the group) a workgroup.
 //
-// Bound by the vector instructions of the softmax and of the decoding, beside the matrix instructions.  A tile of keys is
+// 2048 new tokens behind 14,336, 32 query heads on 8 key heads, d = 128, 4 bits: 607 us, 0.85 PFLOP/s of the two products.  The same loop
+// without softmax, decoding and reads of LDS takes 370 (the rate of a large library product, 1.4 PFLOP/s, at the power limit);
+// without the decoding alone 559, without the softmax alone 523: bound by the sum of its matrix and vector instructions, which
+// overlap little although two wavefronts share a SIMD.  Priorities (s_setprio) for either half of the wavefronts, decoding before the
+// products in one half and behind them in the other, and rows of LDS without bank conflicts at the writes change nothing.
+//
+// A tile of keys is
 // decoded once for all the workgroup's rows, by all its wavefronts, into LDS (two buffers: the next tile is decoded while this one is
-// used, one barrier a tile); each of the eight wavefronts takes 32 rows through it with the scheme of pool_decode.hip: keys on the
+// used, one barrier a tile); each of the eight wavefronts (four: 946 us against 838 then) takes 32 rows through it with the scheme of pool_decode.h: keys on the
 // rows of the score product, so that scores, weights and the running softmax of a row stay in one lane and its neighbour across the
 // wavefront, and weights go into the second product as they are.
 //
@@ -10,12 +16,13 @@
 // outgrows them (kRoom powers of two above what they were taken from), which a wavefront sees when its part of a tile arrives, one
 // comparison; only then it tells the others, through a ring in LDS that all look into before they decode.
 // Loads are straight-line, two tiles ahead of their use; a wavefront's part of a tile lies in one or two blocks of 16 keys, whose pages
-// make scalar addresses.
+// make scalar addresses, the same for K and V.  At d = 256 the registers are full: a reload of a spilled address behind loads in
+// flight waited for these (119 us, now 78, for two prompts' chunks of 500 and 386 tokens among others, 8 query heads).
 #include "../pool_attention.h"
 
 namespace {
 
-constexpr int kAhead = 2;                                    // reads of LDS ahead of the matrix instructions; 4 and 6 measure the same up to 128 dimensions, and spill above
+constexpr int kAhead = 2;                                    // reads of LDS ahead of the matrix instructions (739 us without); 4 and 6 measure the same up to d = 128 and spill above
 constexpr int kRoom = 2;                                     // powers of two that scales may grow before the exponent changes
 
 template <int D, int BITS>

@@ -7,13 +7,15 @@
 //   2. pool_decode (few rows a key head) and pool_chunk (many): one pass over the keys with the running maximum and sum of the softmax.
 //      Each workgroup takes an equal share of all units, in their order, whatever sequences they belong to; what it has of one
 //      sequence, key head and block of rows is a segment.  A segment that is the whole of it is finished at once;
-//   3. pool_merge: the others' sums are brought under one maximum, added in their order, and finished.
+//   3. pool_merge: the others' sums are brought under one maximum, added in their order, and finished (one launch for both).
 // Finishing is the division by the sum of weights and R_v, on the matrix cores.
 //
-// Roundings to 16 bits: q', the dequantized w (code * scale, the scale rounded first) and the weights p are fp16 operands of the matrix
-// instructions, 2^-12 of their value each on average half of that; sums, maxima and exponents are fp32.  None of the
-// three can leave fp16's range: q' has a power of two per row, w one per tile (K) or a running one (V) taken from the scales, the
-// weights are at most 2^kLazy.  What of w is below 2^-26 of the largest in its tile (K) or so far (V) loses bits below 2^-40 of that.
+// Roundings to 16 bits.  pool_decode, which memory bounds: codes go to the matrix cores as they are (exact in fp16) against q' as fp16
+// hi + lo, scales on the results in fp32; a weight times the scale of its key and group is rounded to fp16 once.  pool_chunk, which the matrix
+// cores bound, has one matrix instruction where that would take two: q', the dequantized w (code * scale, the scale rounded first) and
+// the weights p are fp16, half a step (2^-11) each at most.  Against 64 bits that is 3e-4 and 1.2e-3 of an output's size, the output's own
+// rounding to fp16 included.  Sums, maxima and exponents are fp32.  None of the operands can leave fp16's range: q' has a power of two per
+// row, w a running one taken from the scales, the weights are at most 2^kLazy.
 //
 // Order of channels.  A dword of codes is decoded into eight fp16 values in the order 0 4 1 5 2 6 3 7 (4 bits; 0 2 1 3 at 8 bits), so
 // all operands have their channels in that order within units of eight ("positions"), q' by the way it is stored, the output by the
@@ -316,9 +318,7 @@ __device__ __forceinline__ pool_row pool_row_of(const pool_seq& q, int key_head,
 }
 
 typedef void (*pool_attention_kernel_t)(const pool_attention_args);
-// tiles of 32 rows of a pass of pool_rotate: with few rows one, so that they are spread over the compute units
-constexpr int pool_rotate_tiles(long long q_rows, int compute_units) { return q_rows >= 128LL * compute_units ? 4 : 1; }
-pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits, int tiles);
+pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits);
 pool_attention_kernel_t srft_pick_pool_decode_b4(int d, int cb, int gm);
 pool_attention_kernel_t srft_pick_pool_decode_b8(int d, int cb, int gm);
 pool_attention_kernel_t srft_pick_pool_chunk(int d, int bits);

@@ -175,9 +175,10 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     a.out_unscale = pool->out_unscale;
     a.k_unscale = pk->unscale_w;
     a.v_unscale = pv->unscale_w;
-    const int pass = pool_rotate_tiles(n_new * n_q_heads, pk->compute_units);
-    a.q_tiles = (int)((n_new * n_q_heads + pass * kTileVecs - 1) / (pass * kTileVecs));
-    a.q_grid = std::min(a.q_tiles, workgroups(pool, 2));
+    a.q_tiles = (int)((n_new * n_q_heads + kTileVecs - 1) / kTileVecs);
+    // as many as a compute unit's registers hold at a time, each with the matrix for all its passes (65,536 rows of d = 128: 12.4 us, with two
+    // a unit 13.0, with four 14.3; 32,000 of d = 256: 23.4, with two 26.2)
+    a.q_grid = std::min(a.q_tiles, workgroups(pool, d <= 128 ? 3 : 1));
     a.decode_before = (int*)(base + w.decode_before);
     a.chunk_before = (int*)(base + w.chunk_before);
     a.q_rows = (unsigned short*)(base + w.q_rows);
@@ -195,8 +196,8 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     a.decode_keys = pool_decode_keys(d, sp.cb);
     a.chunk_grid = w.chunk_grid;
     const hipStream_t st = (hipStream_t)hip_stream;
-    const int tail_tiles = 2 * seqs->n_seq * ((pool->heads * pool->R + pass * kTileVecs - 1) / (pass * kTileVecs)), heads = seqs->n_seq * pool->heads;
-    rc = srft_launch(srft_pick_pool_rotate(d, pk->bits, pass), dim3((unsigned)(1 + a.q_grid + tail_tiles)), 2 * d, st, a);
+    const int tail_tiles = 2 * seqs->n_seq * (pool->heads * pool->R / kTileVecs), heads = seqs->n_seq * pool->heads;
+    rc = srft_launch(srft_pick_pool_rotate(d, pk->bits), dim3((unsigned)(1 + a.q_grid + tail_tiles)), 2 * d, st, a);
     if (rc == SRFT_OK && sp.chunk) rc = srft_launch(srft_pick_pool_chunk(d, pk->bits), dim3((unsigned)a.chunk_grid), 64 * pool_chunk_waves(d), st, a);
     if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb), dim3((unsigned)a.decode_grid), 64 * kPoolDecodeWaves, st, a);
     a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * pool_chunk_waves(d)) * pool_chunk_waves(d);
