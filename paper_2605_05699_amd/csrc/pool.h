@@ -28,15 +28,16 @@ struct pool_seqs {
 struct pool_seq {
     int start, n_new, length, before, full;                  // rows of the new tokens; tokens with and without them; tokens in full pages
 };
-__device__ __forceinline__ pool_seq pool_seq_of(const pool_seqs& s, int b) {
+__device__ __forceinline__ pool_seq pool_seq_from(const pool_seqs& s, int start, int next_start, int length) {
     pool_seq q;
-    q.start = min(max(s.starts[b], 0), s.n_new);
-    q.n_new = min(min(max(s.starts[b + 1], q.start), s.n_new) - q.start, s.max_new);
-    q.length = min(max(s.lengths[b], 0), s.max_length);
+    q.start = min(max(start, 0), s.n_new);
+    q.n_new = min(min(max(next_start, q.start), s.n_new) - q.start, s.max_new);
+    q.length = min(max(length, 0), s.max_length);
     q.before = q.length - q.n_new;                           // (negative where there are more new tokens than tokens: those have no place)
     q.full = q.length >> s.log_R << s.log_R;
     return q;
 }
+__device__ __forceinline__ pool_seq pool_seq_of(const pool_seqs& s, int b) { return pool_seq_from(s, s.starts[b], s.starts[b + 1], s.lengths[b]); }
 __device__ __forceinline__ bool pool_there(int number, int count) { return (unsigned)number < (unsigned)count; }
 
 inline pool_seqs pool_seqs_of(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new) {

@@ -2,8 +2,8 @@
 // tokens of them): the scan over the keys, and the merge of what its workgroups leave.
 //
 // Bound by the records' bytes where there are enough of them, with the vector instructions that decode them close behind: 24 sequences up
-// to 32,768 tokens, 8 key heads of 128 channels, 4 bits: 388 MB in 117 us, 3.3 TB/s (loads and addresses alone, nothing decoded: 104; a
-// sum over 2 GiB reads 4.0 TB/s here).  Codes are loaded past the L2, where nobody reads them again: 124 without that.  A wavefront has
+// to 32,768 tokens, 8 key heads of 128 channels, 4 bits: 388 MB in 110 us, 3.5 TB/s (a sum over 2 GiB reads 4.0 here; the vector ALU is busy 59 %
+// of the time).  Codes are loaded past the L2, where nobody reads them again: 6 % slower without that.  A wavefront has
 // a tile of KEYS keys to itself, keys on the rows of the score product and 16 query rows on its columns (16x16x32; CB blocks of
 // them): a lane holds, for ITS row (lane % 16), the keys of its quarter of the wavefront (lane / 16), which is what the running maximum
 // and sum want and what the product with the values takes as its B operand.  Scores and weights stay in registers.
@@ -149,12 +149,23 @@ __device__ __forceinline__ uint32_t pool_product2(float a, float f, float b, flo
     return r;
 }
 
-// Wavefronts per SIMD asked of the compiler.  Two fit (LDS, and some 250 registers).  Asked for two it orders the instructions to save
-// registers that nobody needs: 133 us (24 sequences up to 32,768 tokens at d = 128); asked for four, which the LDS rules out, it gives that up
-// and fills the latencies: 120.
-constexpr int kPoolDecodeWavesAsked = 4;
+// Wavefronts per SIMD asked of the compiler.  Two fit (LDS, and 256 registers each).  Asked for one it fills the latencies with what registers there
+// are, and mostly ends below 256: us of the scan of 24 sequences up to 32,768 tokens, 8 rows a key head, asked for one / two: d = 64 73 / 78, d = 128
+// 109 / 121, 256 at 4 bits 209 / 247, 192 at 8 bits 201 / 227.  Where it ends above (one wavefront a SIMD), asking for two costs some spilled registers and
+// is faster up to 40 of them: at 8 bits d = 96 146 / 130, 128 189 / 160, 224 342 / 284, 256 389 / 326, 24 rows of d = 128 at 4 bits 261 / 187 (but at 8 bits,
+// with 69 spilled, 258 / 299).
+constexpr int pool_decode_waves(int d, int bits, int cb, int gm) {
+    if (bits == 8) return d == 96 || (cb == 1 && (d == 128 || d >= 224 || (d == 192 && gm == kGroupWide))) || (cb == 2 && d == 64 && gm == kGroup16) ? 2 : 1;
+    if (cb == 2) return (d == 128 && gm != kGroup16) || (d == 96 && gm != kGroup32) ? 2 : 1;
+    return d == 224 && gm == kGroupWide ? 2 : 1;
+}
+// Whether a segment's first tile is asked for before its queries are in LDS: 115 us -> 109 at d = 128, 142 -> 135 at 160; where the registers are full
+// (256: 209 -> 291) it is not.
+constexpr bool pool_decode_early(int d, int bits, int cb, int gm) {
+    return pool_decode_waves(d, bits, cb, gm) == 1 && d <= 160 && !(d == 128 && gm == kGroup16);
+}
 template <int D, int BITS, int CB, int GM>
-__global__ void __launch_bounds__(64 * kPoolTeam, kPoolDecodeWavesAsked) srft_pool_decode_kernel(const pool_attention_args a) {
+__global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB, GM)) srft_pool_decode_kernel(const pool_attention_args a) {
     using P = pool_decode<D, BITS, CB, GM>;
     constexpr bool FINE = P::FINE;
     constexpr int G = P::G, NS = P::NS, KEYS = P::KEYS, KQ = P::KQ, BK = P::BK, W = P::W, CBY = P::CBY, NV = P::NV, NH = P::NH, NB = D / 16;
@@ -162,13 +173,32 @@ __global__ void __launch_bounds__(64 * kPoolTeam, kPoolDecodeWavesAsked) srft_po
     __shared__ __align__(16) unsigned char lds[P::LDS];
     __shared__ uint4 qs[CB * G * 2 * 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quarter = lane >> 4;
-    const int total = a.decode_before[a.s.n_seq];
+    // The first segment's sequence: where the sequences fit the lanes, all that it takes comes with one round of loads (a step of 4
+    // sequences up to 1000 tokens: 12.6 us with this and with the first tile's loads before the queries are in LDS, 13.5 to 14 one after the other).
+    const int n_seq = a.s.n_seq;
+    const bool few = n_seq < 64;
+    int of_before = 0, of_start = 0, of_length = 0;          // lane b: of sequence b
+    if (few) {
+        of_before = a.decode_before[min(lane, n_seq)];
+        of_start = a.s.starts[min(lane, n_seq)];
+        of_length = a.s.lengths[min(lane, n_seq - 1)];
+    }
+    const int total = few ? __builtin_amdgcn_readlane(of_before, n_seq) : a.decode_before[n_seq];
     const int w = srft_block_by_die();
     const pool_shares shares(total, gridDim.x, W);
     if (total == 0 || w >= shares.groups) return;            // (uniform)
     const int end = shares.begin(w + 1);
-    int unit = shares.begin(w);
-    int seq = __builtin_amdgcn_readfirstlane(pool_sequence_of(a.decode_before, a.s.n_seq, unit));
+    int unit = shares.begin(w), seq, units_before;
+    pool_seq q;
+    if (few) {
+        seq = min((int)__popcll(__ballot(lane <= n_seq && of_before <= unit)) - 1, n_seq - 1);
+        units_before = __builtin_amdgcn_readlane(of_before, seq);
+        q = pool_seq_from(a.s, __builtin_amdgcn_readlane(of_start, seq), __builtin_amdgcn_readlane(of_start, seq + 1), __builtin_amdgcn_readlane(of_length, seq));
+    } else {
+        seq = __builtin_amdgcn_readfirstlane(pool_sequence_of(a.decode_before, n_seq, unit));
+        units_before = a.decode_before[seq];
+        q = pool_seq_of(a.s, seq);
+    }
     const int R = 1 << a.s.log_R, n_scales = D / a.g;
     unsigned char* const kt = lds + wave * P::WAVE_BYTES;    // this wavefront's keys, and then values, and scales
     unsigned char* const vt = kt;
@@ -193,29 +223,108 @@ __global__ void __launch_bounds__(64 * kPoolTeam, kPoolDecodeWavesAsked) srft_po
     const int s_key = lane & (KEYS - 1), s_first = min(KEYS == 64 ? 0 : lane / 32 * NH, NS - NH);      // a lane's scales: of this key, these columns
     const int s_skip = GM == kGroupWide ? 0 : 4 * s_first;     // bytes behind the row's first scale
     for (bool at_begin = true; unit < end; at_begin = false) {
-        while (seq + 1 < a.s.n_seq && a.decode_before[seq + 1] <= unit) ++seq;
-        const pool_seq q = pool_seq_of(a.s, seq);
+        if (!at_begin) {
+            while (seq + 1 < n_seq && a.decode_before[seq + 1] <= unit) ++seq;
+            units_before = a.decode_before[seq];
+            q = pool_seq_of(a.s, seq);
+        }
         const int tiles = pool_tiles(q.length, q.full, KEYS), page_tiles = (q.full + KEYS - 1) / KEYS, tail = q.length - q.full;
-        const int rel = unit - a.decode_before[seq], item = rel / tiles, t0 = rel - item * tiles, t1 = min(tiles, t0 + end - unit);
+        const int rel = unit - units_before, item = rel / tiles, t0 = rel - item * tiles, t1 = min(tiles, t0 + end - unit);
         const int blocks_of_rows = (q.n_new * a.group + 16 * CB - 1) / (16 * CB), head = item / blocks_of_rows, r0 = 16 * CB * (item - head * blocks_of_rows);
         if (t1 <= t0) return;                                // (only if the device arrays were written during the call)
+        const int32_t* const table = a.s.table + seq * a.s.max_pages;
+        const int last_page_tile = min(t1, page_tiles) - 1;
+        int t = t0 + wave;
+        u32x4 kc[NV], vc[NV];
+        pool_floats<NH> kf, vf;
+        // pages of the tile's blocks of 16 keys (lane i: block i % (KEYS / 16)); behind the last page, the last block again
+        const auto page_of = [&](int tile) __attribute__((always_inline)) {
+            return table[min(tile * KEYS + 16 * (lane & (KEYS / 16 - 1)), q.full - 16) >> a.s.log_R];
+        };
+        uint32_t there = 0;
+        uint64_t c0 = 0, c1 = 0, c2 = 0, c3 = 0;         // blocks' codes
+        const auto code_of = [&](int block) __attribute__((always_inline)) {
+            uint64_t r = block & 1 ? c1 : c0;
+            if constexpr (KEYS == 64) r = block & 2 ? block & 1 ? c3 : c2 : r;
+            return r;
+        };
+        const auto fetch_values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) vc[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.vb.codes_dev + (code_of(piece_block[i]) + piece_off[i])));
+        };
+        const auto fetch = [&](int tile, int pages) __attribute__((always_inline)) {
+            // Blocks' addresses in scalar registers: in bytes of codes, and of scales.  (The empty asm keeps the choice between them a
+            // choice of registers: the compiler makes branches of it otherwise.)
+            uint32_t known = 0;
+            uint64_t f0, f1, f2 = 0, f3 = 0;
+            const auto address = [&](int i, uint64_t& code, uint64_t& scale) __attribute__((always_inline)) {
+                const int page = __builtin_amdgcn_readlane(pages, i), slot = min(tile * KEYS + 16 * i, q.full - 16) & (R - 1);
+                const bool ok = pool_there(page, a.s.n_pages);
+                known |= (ok ? 1u : 0u) << i;
+                const uint64_t row = ((uint64_t)((ok ? page : 0) * (uint64_t)a.heads + head) << a.s.log_R) + slot;
+                code = row * CBY;
+                scale = row * (4 * n_scales);
+                asm("" : "+s"(code), "+s"(scale));
+            };
+            address(0, c0, f0);
+            address(1, c1, f1);
+            if constexpr (KEYS == 64) {
+                address(2, c2, f2);
+                address(3, c3, f3);
+            }
+            there = known;
+            uint64_t f = s_key & 16 ? f1 : f0;
+            if constexpr (KEYS == 64) f = s_key & 32 ? s_key & 16 ? f3 : f2 : f;
+            const uint64_t s_at = f + (s_key & 15) * (4 * n_scales) + s_skip;
+            const char *const sk = (const char*)a.kb.scales_dev + s_at, *const sv = (const char*)a.vb.scales_dev + s_at;
+            if constexpr (GM == kGroupWide) {
+#pragma unroll
+                for (int i = 0; i < NH; ++i) {           // (the offset is uniform but for the half of the wavefront)
+                    const int at = (s_first + i) * 32 / a.g;
+                    kf[i] = reinterpret_cast<const float*>(sk)[at];
+                    vf[i] = reinterpret_cast<const float*>(sv)[at];
+                }
+            } else {
+                kf = *reinterpret_cast<const pool_floats<NH>*>(sk);
+                vf = *reinterpret_cast<const pool_floats<NH>*>(sv);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) kc[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.kb.codes_dev + (code_of(piece_block[i]) + piece_off[i])));
+        };
+        constexpr bool EARLY = pool_decode_early(D, BITS, CB, GM);
+        // the first tile: its pages, then the queries, then its codes are on their way
+        int pages = 0;
+        if (EARLY && t <= last_page_tile) pages = page_of(t);
         pool_row row[CB];
         float factor[CB];
+        constexpr int NQ = (2 * G + W - 1) / W;
+        u32x4 x[CB][NQ];
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             row[c] = pool_row_of(q, head, a.group, r0 + 16 * c + l16);
             const long long q_row = (long long)row[c].token * (a.heads * a.group) + row[c].head;
             factor[c] = fmaxf(a.q_factor[q_row], 1.17549435e-38f);
-            for (int j = wave; j < 2 * G; j += W) {          // (hi and lo of run j / 2)
-                uint4 x = reinterpret_cast<const uint4*>((j % 2 ? a.q_rows_low : a.q_rows) + q_row * D)[4 * (j / 2) + quarter];
-                if constexpr (P::OFFSET && BITS == 4) {
-                    const half2v sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
-                    x.y = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x.y) * sixteenth);
-                    x.w = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x.w) * sixteenth);
-                }
-                qs[(c * G * 2 + j) * 64 + lane] = x;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {                   // (hi and lo of run j / 2)
+                const int j = min(wave + W * i, 2 * G - 1);
+                x[c][i] = reinterpret_cast<const u32x4*>((j % 2 ? a.q_rows_low : a.q_rows) + q_row * D)[4 * (j / 2) + quarter];
             }
         }
+        if (EARLY && t <= last_page_tile) {
+            fetch(t, pages);
+            pages = page_of(min(t + W, last_page_tile));
+        }
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                if constexpr (P::OFFSET && BITS == 4) {
+                    const half2v sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
+                    x[c][i][1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, (uint32_t)x[c][i][1]) * sixteenth);
+                    x[c][i][3] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, (uint32_t)x[c][i][3]) * sixteenth);
+                }
+                qs[(c * G * 2 + min(wave + W * i, 2 * G - 1)) * 64 + lane] = __builtin_bit_cast(uint4, x[c][i]);     // (past the last, the last again)
+            }
         __syncthreads();
         floatx4 start[P::OFFSET ? CB : 1][P::OFFSET ? NS : 1];               // what the score product starts from
         if constexpr (P::OFFSET) {
@@ -245,8 +354,6 @@ __global__ void __launch_bounds__(64 * kPoolTeam, kPoolDecodeWavesAsked) srft_po
         } else {
             start[0][0] = floatx4{0, 0, 0, 0};
         }
-        const int32_t* const table = a.s.table + seq * a.s.max_pages;
-
         floatx4 acc[CB][NB];
         float top[CB], den[CB];
         int e_now = kPoolNoExponent;
@@ -305,69 +412,13 @@ __global__ void __launch_bounds__(64 * kPoolTeam, kPoolDecodeWavesAsked) srft_po
                 }
         };
 
-        const int last_page_tile = min(t1, page_tiles) - 1;
-        int t = t0 + wave;
         bool first = true;
         if (t <= last_page_tile) {
-            u32x4 kc[NV], vc[NV];
-            pool_floats<NH> kf, vf;
-            // pages of the tile's blocks of 16 keys (lane i: block i % (KEYS / 16)); behind the last page, the last block again
-            const auto page_of = [&](int tile) __attribute__((always_inline)) {
-                return table[min(tile * KEYS + 16 * (lane & (KEYS / 16 - 1)), q.full - 16) >> a.s.log_R];
-            };
-            uint32_t there = 0;
-            uint64_t c0 = 0, c1 = 0, c2 = 0, c3 = 0;         // blocks' codes
-            const auto code_of = [&](int block) __attribute__((always_inline)) {
-                uint64_t r = block & 1 ? c1 : c0;
-                if constexpr (KEYS == 64) r = block & 2 ? block & 1 ? c3 : c2 : r;
-                return r;
-            };
-            const auto fetch_values = [&]() __attribute__((always_inline)) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) vc[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.vb.codes_dev + (code_of(piece_block[i]) + piece_off[i])));
-            };
-            const auto fetch = [&](int tile, int pages) __attribute__((always_inline)) {
-                // Blocks' addresses in scalar registers: in bytes of codes, and of scales.  (The empty asm keeps the choice between them a
-                // choice of registers: the compiler makes branches of it otherwise.)
-                uint32_t known = 0;
-                uint64_t f0, f1, f2 = 0, f3 = 0;
-                const auto address = [&](int i, uint64_t& code, uint64_t& scale) __attribute__((always_inline)) {
-                    const int page = __builtin_amdgcn_readlane(pages, i), slot = min(tile * KEYS + 16 * i, q.full - 16) & (R - 1);
-                    const bool ok = pool_there(page, a.s.n_pages);
-                    known |= (ok ? 1u : 0u) << i;
-                    const uint64_t row = ((uint64_t)((ok ? page : 0) * (uint64_t)a.heads + head) << a.s.log_R) + slot;
-                    code = row * CBY;
-                    scale = row * (4 * n_scales);
-                    asm("" : "+s"(code), "+s"(scale));
-                };
-                address(0, c0, f0);
-                address(1, c1, f1);
-                if constexpr (KEYS == 64) {
-                    address(2, c2, f2);
-                    address(3, c3, f3);
-                }
-                there = known;
-                uint64_t f = s_key & 16 ? f1 : f0;
-                if constexpr (KEYS == 64) f = s_key & 32 ? s_key & 16 ? f3 : f2 : f;
-                const uint64_t s_at = f + (s_key & 15) * (4 * n_scales) + s_skip;
-                const char *const sk = (const char*)a.kb.scales_dev + s_at, *const sv = (const char*)a.vb.scales_dev + s_at;
-                if constexpr (GM == kGroupWide) {
-#pragma unroll
-                    for (int i = 0; i < NH; ++i) {           // (the offset is uniform but for the half of the wavefront)
-                        const int at = (s_first + i) * 32 / a.g;
-                        kf[i] = reinterpret_cast<const float*>(sk)[at];
-                        vf[i] = reinterpret_cast<const float*>(sv)[at];
-                    }
-                } else {
-                    kf = *reinterpret_cast<const pool_floats<NH>*>(sk);
-                    vf = *reinterpret_cast<const pool_floats<NH>*>(sv);
-                }
-#pragma unroll
-                for (int i = 0; i < NV; ++i) kc[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.kb.codes_dev + (code_of(piece_block[i]) + piece_off[i])));
-            };
-            fetch(t, page_of(t));
+            if constexpr (!EARLY) {
+                fetch(t, page_of(t));
+                pages = page_of(min(t + W, last_page_tile));
+            }
             fetch_values();
-            int pages = page_of(min(t + W, last_page_tile));
             for (; t <= last_page_tile; t += W) {
                 // ---- scales and keys to LDS (of one wavefront: its accesses complete in program order)
                 const uint32_t blocks = there;
