@@ -2,9 +2,10 @@
 //
 // 2048 new tokens behind 14,336, 32 query heads on 8 key heads, d = 128, 4 bits: 607 us, 0.85 PFLOP/s of the two products.  The same loop
 // without softmax, decoding and reads of LDS takes 370 (the rate of a large library product, 1.4 PFLOP/s, at the power limit);
-// without the decoding alone 559, without the softmax alone 523: bound by the sum of its matrix and vector instructions, which
-// overlap little although two wavefronts share a SIMD.  Priorities (s_setprio) for either half of the wavefronts, decoding before the
-// products in one half and behind them in the other, and rows of LDS without bank conflicts at the writes change nothing.
+// without the decoding alone 559, without the softmax alone 523; on zeros, the same instructions with nothing toggling, 500.  So it is the
+// energy of its instructions that bounds it, matrix and vector ones alike: priorities (s_setprio) for either half of the wavefronts, decoding before
+// the products in one half and behind them in the other, a softmax spread between the matrix instructions of the values, and rows of
+// LDS without bank conflicts at the writes change nothing.
 //
 // A tile of keys is
 // decoded once for all the workgroup's rows, by all its wavefronts, into LDS (two buffers: the next tile is decoded while this one is
