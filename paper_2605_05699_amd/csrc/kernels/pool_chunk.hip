@@ -27,8 +27,8 @@ constexpr int kAhead = 2;                                    // reads of LDS ahe
 constexpr int kRoom = 2;                                     // powers of two that scales may grow before the exponent changes
 
 template <int D, int BITS>
-__global__ void __launch_bounds__(64 * kPoolChunkWaves<D>, 2) srft_pool_chunk_kernel(const pool_attention_args a) {
-    constexpr int W = kPoolChunkWaves<D>, NT = 64 * W, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * W, KB = KEYS / 32;
+__global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kernel(const pool_attention_args a) {
+    constexpr int W = kPoolChunkWaves, NT = 64 * W, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * W, KB = KEYS / 32;
     constexpr int T = D / 16, CB = D * BITS / 8;
     constexpr int KROW = 2 * D + 16, VROW = 2 * D + 32;      // bytes of a row in LDS: 16-byte reads of 32 rows, transposed reads of 8, on different banks
     constexpr int UNITS = KEYS * T;                          // of 16 channels, of K and of V each

@@ -8,10 +8,9 @@
 
 namespace {
 
-constexpr int kTeam = kPoolTeam;
 template <int D>
 __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsigned workgroup, uint4* ops, float (*tops)[32]) {
-    constexpr int BLOCKS = kPoolChunkWaves<D>, ROWS = kPoolBlock * BLOCKS, KEYS = kPoolChunkKeys<D>, G = D / 32, T = D / 16, OWN = (G + kTeam - 1) / kTeam, AHEAD = 2;
+    constexpr int BLOCKS = kPoolChunkWaves, ROWS = kPoolBlock * BLOCKS, KEYS = kPoolChunkKeys<D>, G = D / 32, T = D / 16, OWN = (G + kPoolTeam - 1) / kPoolTeam, AHEAD = 2;
     // ops: [k-step][hi, lo][lane]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int of = (int)(workgroup / (unsigned)a.merge_blocks), at = (int)workgroup - of * a.merge_blocks;
@@ -24,7 +23,7 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     char* const dst = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
     if (tiles == 0) {
         if (dst)
-            for (int i = 2 * wave + half; i < D / 8; i += 2 * kTeam) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
+            for (int i = 2 * wave + half; i < D / 8; i += 2 * kPoolTeam) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
         return;
     }
     const int* const before = a.chunk_before;
@@ -58,7 +57,7 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
 #pragma unroll
             for (int i = 0; i < OWN; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[k][i][j] = reinterpret_cast<const floatx4*>(p)[(4 * min(wave + kTeam * i, G - 1) + j) * 64 + lane];
+                for (int j = 0; j < 4; ++j) x[k][i][j] = reinterpret_cast<const floatx4*>(p)[(4 * min(wave + kPoolTeam * i, G - 1) + j) * 64 + lane];
             const float g = v + k <= w1 ? __builtin_amdgcn_exp2f(p[32 * D + lane] - t_all) : 0.0f;
             den = fmaf(p[32 * D + 64 + lane], g, den);
             f[k] = g * pool_power((int)__float_as_uint(p[32 * D + 128 + lane]) - e_all);
@@ -76,19 +75,19 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     float m = 0.0f;
 #pragma unroll
     for (int i = 0; i < OWN; ++i)
-        if (wave + kTeam * i < G)
+        if (wave + kPoolTeam * i < G)
 #pragma unroll
             for (int v = 0; v < 16; ++v) m = fmaxf(m, fabsf(sums[i][v]));
     m = other_half_max(m);
     tops[wave][lane & 31] = m;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kTeam; ++w) m = fmaxf(m, tops[w][lane & 31]);
+    for (int w = 0; w < kPoolTeam; ++w) m = fmaxf(m, tops[w][lane & 31]);
     const int e = max((int)((__float_as_uint(m) >> 23) & 0xFF) - 127, -100);
     const float up = pool_power(14 - e);
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
-        const int b = wave + kTeam * i;
+        const int b = wave + kPoolTeam * i;
         if (b < G)                                           // uniform
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -105,7 +104,7 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     }
     __syncthreads();
     const float down = (den > 0.0f ? 1.0f / den : 0.0f) * a.out_unscale, p0 = pool_power(e - 14), p1 = pool_power(e_all);
-    for (int j = wave; j < G; j += kTeam) {
+    for (int j = wave; j < G; j += kPoolTeam) {
         floatx16 acc{0};
 #pragma unroll
         for (int k = 0; k < T; ++k) {
@@ -120,9 +119,9 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
 }
 
 template <int D, int CB>
-__global__ void __launch_bounds__(64 * kTeam) srft_pool_merge_kernel(const pool_attention_args a) {
+__global__ void __launch_bounds__(64 * kPoolTeam) srft_pool_merge_kernel(const pool_attention_args a) {
     constexpr int OPS = D / 16 * 2 * 64;
-    __shared__ __align__(16) unsigned char lds[std::max(kPoolFinishBytes<D>, OPS * 16 + kTeam * 32 * 4)];
+    __shared__ __align__(16) unsigned char lds[std::max(kPoolFinishBytes<D>, OPS * 16 + kPoolTeam * 32 * 4)];
     if (blockIdx.x < (unsigned)a.decode_merges)              // uniform
         pool_decode_merge<D, CB>(a, blockIdx.x, lds);
     else

@@ -18,7 +18,7 @@ constexpr int position_channel(int e) { return BITS == 8 ? (e & 4) + ((e & 1) <<
 // units of work in front of each sequence, by one workgroup
 template <int D>
 __device__ __forceinline__ void count_units(const pool_attention_args& a) {
-    constexpr int NT = 2 * D, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * kPoolChunkWaves<D>;
+    constexpr int NT = 2 * D, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * kPoolChunkWaves;
     const pool_seqs& s = a.s;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     // the sequences' own units first, then their sums in place

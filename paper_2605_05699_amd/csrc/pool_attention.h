@@ -29,13 +29,11 @@ constexpr float kPoolLowest = -3.0e38f;                      // "no key yet": fi
 constexpr int kPoolNoExponent = -200;                        // of V: "no value yet"
 constexpr float kLazy = 8.0f;                                // how far (in powers of two) weights may grow past the maximum that they are taken from
 constexpr int kPoolDecodeRows = 32;                          // most rows of one key head that pool_decode takes, in blocks of 16
-constexpr int kPoolDecodeWaves = 4;
+constexpr int kPoolTeam = 4;                                 // wavefronts of a workgroup of pool_decode and pool_merge
 constexpr int pool_decode_keys(int d, int cb) { return d <= 128 && cb == 1 ? 64 : 32; }      // of a tile
 constexpr int kPoolBlock = 32;                               // rows of a wavefront
 template <int D> constexpr int kPoolChunkKeys = D <= 128 ? 64 : 32;
-template <int D> constexpr int kPoolChunkWaves = 8;
-constexpr int pool_chunk_keys(int d) { return d <= 128 ? 64 : 32; }
-constexpr int pool_chunk_waves(int) { return 8; }
+constexpr int kPoolChunkWaves = 8;
 
 struct pool_attention_args {
     pool_seqs s;
@@ -192,25 +190,6 @@ template <int D> struct pool_block {
         p[32 * D + lane] = top;
         p[32 * D + 64 + lane] = den;
         p[32 * D + 128 + lane] = __uint_as_float((uint32_t)e);
-    }
-    // adds what put() left at p
-    __device__ __forceinline__ void add(const float* p, int lane) {
-        const float top_p = p[32 * D + lane], den_p = p[32 * D + 64 + lane];
-        const int e_p = (int)__float_as_uint(p[32 * D + 128 + lane]);
-        const float t = fmaxf(top, top_p), f = __builtin_amdgcn_exp2f(top - t), f_p = __builtin_amdgcn_exp2f(top_p - t);
-        const int m = max(e, e_p);
-        const float g = f * pool_power(e - m), g_p = f_p * pool_power(e_p - m);
-#pragma unroll
-        for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const floatx4 x = reinterpret_cast<const floatx4*>(p)[(4 * b + i) * 64 + lane];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sums[b][4 * i + j] = fmaf(x[j], g_p, sums[b][4 * i + j] * g);
-            }
-        top = t;
-        den = fmaf(den_p, f_p, den * f);
-        e = m;
     }
 };
 

@@ -40,7 +40,7 @@ workspace layout(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new, in
     };
     const split s16 = split_of(s, n_new, group, d);
     w.decode_grid = workgroups(p, p->decode_blocks[s16.cb - 1]);
-    w.chunk_grid = workgroups(p, 8 / pool_chunk_waves(d));
+    w.chunk_grid = workgroups(p, 1);
     w.decode_before = take(4LL * (s->n_seq + 1));
     w.chunk_before = take(4LL * (s->n_seq + 1));
     w.q_rows = take(2 * rows * d);
@@ -50,7 +50,7 @@ workspace layout(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new, in
     w.tail_factor = take(4 * tail);
     w.tail_columns = take(tail * d);
     w.decode_parts = take(2LL * w.decode_grid * s16.cb * (16 * d + 3 * 64) * 4);
-    w.chunk_parts = take(s16.chunk ? 2LL * w.chunk_grid * pool_chunk_waves(d) * pool_part(d) * 4 : 0);
+    w.chunk_parts = take(s16.chunk ? 2LL * w.chunk_grid * kPoolChunkWaves * pool_part(d) * 4 : 0);
     w.bytes = at;
     return w;
 }
@@ -64,10 +64,10 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, int64_t n_new, int
     if (rc != SRFT_OK) return rc;
     if (q_heads < 1 || q_heads % pool->heads != 0 || q_heads > 64 * pool->heads || n_new * q_heads >= (1LL << 31) - 32) return SRFT_ERR_BAD_N;
     // units of work, tiles and workgroups are counted with 32 bits
-    const int d = pool->plan_k->d, group = q_heads / pool->heads, rows = kPoolBlock * pool_chunk_waves(d);
+    const int d = pool->plan_k->d, group = q_heads / pool->heads, rows = kPoolBlock * kPoolChunkWaves;
     const int64_t most = 1LL << 31, tiles = seqs->max_length / 32 + 2, heads = (int64_t)seqs->n_seq * pool->heads;
     const int64_t blocks = row_blocks(seqs, n_new, group, rows), all_blocks = n_new * group / rows + seqs->n_seq;
-    if (2 * heads * tiles >= most || all_blocks * pool->heads * tiles >= most || heads * std::max<int64_t>(blocks, 1) * pool_chunk_waves(d) >= most ||
+    if (2 * heads * tiles >= most || all_blocks * pool->heads * tiles >= most || heads * std::max<int64_t>(blocks, 1) * kPoolChunkWaves >= most ||
         heads * pool->R / kTileVecs * 2 >= most / 2)
         return SRFT_ERR_BAD_N;
     return SRFT_OK;
@@ -121,7 +121,7 @@ int srft_pool_tables(srft_pool* p) {
                     image[at + 64 * 8] = ol[src];
                 }
     for (int cb = 1; cb <= 2; ++cb) {
-        SRFT_HIP(hipOccupancyMaxActiveBlocksPerMultiprocessor(&p->decode_blocks[cb - 1], (const void*)srft_pool_decode_kernel_of(p->plan_k, cb), 64 * kPoolDecodeWaves, 0));
+        SRFT_HIP(hipOccupancyMaxActiveBlocksPerMultiprocessor(&p->decode_blocks[cb - 1], (const void*)srft_pool_decode_kernel_of(p->plan_k, cb), 64 * kPoolTeam, 0));
         p->decode_blocks[cb - 1] = std::max(1, std::min(4, p->decode_blocks[cb - 1]));
     }
     SRFT_HIP(hipMalloc((void**)&p->tables, image.size() * 2));
@@ -198,12 +198,12 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     const hipStream_t st = (hipStream_t)hip_stream;
     const int tail_tiles = 2 * seqs->n_seq * (pool->heads * pool->R / kTileVecs), heads = seqs->n_seq * pool->heads;
     rc = srft_launch(srft_pick_pool_rotate(d, pk->bits), dim3((unsigned)(1 + a.q_grid + tail_tiles)), 2 * d, st, a);
-    if (rc == SRFT_OK && sp.chunk) rc = srft_launch(srft_pick_pool_chunk(d, pk->bits), dim3((unsigned)a.chunk_grid), 64 * pool_chunk_waves(d), st, a);
-    if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb), dim3((unsigned)a.decode_grid), 64 * kPoolDecodeWaves, st, a);
-    a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * pool_chunk_waves(d)) * pool_chunk_waves(d);
+    if (rc == SRFT_OK && sp.chunk) rc = srft_launch(srft_pick_pool_chunk(d, pk->bits), dim3((unsigned)a.chunk_grid), 64 * kPoolChunkWaves, st, a);
+    if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb), dim3((unsigned)a.decode_grid), 64 * kPoolTeam, st, a);
+    a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * kPoolChunkWaves) * kPoolChunkWaves;
     a.decode_merges = sp.decode ? heads * ((a.decode_rows + a.decode_block - 1) / a.decode_block) : 0;
     const unsigned merges = (unsigned)(a.decode_merges + (sp.chunk ? heads * a.merge_blocks : 0));
-    if (rc == SRFT_OK && merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb), dim3(merges), 64 * kPoolDecodeWaves, st, a);
+    if (rc == SRFT_OK && merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb), dim3(merges), 64 * kPoolTeam, st, a);
     return rc;
 }
 

@@ -31,7 +31,6 @@ __device__ __forceinline__ float pool_quarters_sum(float s) {
 
 // ---- the end of 16 rows, by a workgroup of four wavefronts: wavefront w holds the sums of the channels 16 c .. for c = w, w + 4, ...
 // (o[i], lane l: channels 16 c + 4 (l / 16) + 0 .. 3 of row l % 16).
-constexpr int kPoolTeam = 4;
 template <int D> constexpr int kPoolOwn = (D / 16 + kPoolTeam - 1) / kPoolTeam;
 template <int D> constexpr int kPoolFinishBytes = D / 32 * 2 * 64 * 16 + kPoolTeam * 16 * 4;
 // lds: kPoolFinishBytes<D>, free before and after a barrier of the caller's.  dst: the lane's row or null.
