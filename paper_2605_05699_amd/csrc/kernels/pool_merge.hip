@@ -3,7 +3,8 @@
 // (pool_decode_merge), the others those of chunks, in one launch: apart, the first took 17 us beside the 29 of the others (d = 256).
 // Chunks: one workgroup of four wavefronts per 32 rows of a key head, each with every fourth
 // run of 32 positions of the sums and then of the outputs (one wavefront per 32 rows read every part, and the matrix, one after
-// the other: 104 us at d = 256, 28 at d = 128).  Rows that their scan has finished have nothing to do here.
+// the other: 104 us at d = 256, 28 at d = 128).  Bound by the chain of loads where parts are few (a first round for the maxima alone: 6.9 us,
+// now 5.5, for a step of 4 sequences), by the parts' bytes where they are many (23 us for 67 MB at d = 128; more of them in flight is slower).  Rows that their scan has finished have nothing to do here.
 #include "../pool_decode.h"
 
 namespace {
@@ -38,30 +39,24 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     };
     float t_all = kPoolLowest, den = 0.0f;
     int e_all = kPoolNoExponent;
-    for (int v = w0; v <= w1; v += 4) {
-        float t[4], e[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) t[k] = part(min(v + k, w1))[32 * D + lane], e[k] = part(min(v + k, w1))[32 * D + 128 + lane];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) t_all = fmaxf(t_all, t[k]), e_all = max(e_all, (int)__float_as_uint(e[k]));
-    }
     floatx16 sums[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i) sums[i] = floatx16{0};
     for (int v = w0; v <= w1; v += AHEAD) {
         floatx4 x[AHEAD][OWN][4];
-        float f[AHEAD];
+        pool_part_head h[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const float* const p = part(min(v + k, w1));
+            h[k].load(p + 32 * D, lane);
 #pragma unroll
             for (int i = 0; i < OWN; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[k][i][j] = reinterpret_cast<const floatx4*>(p)[(4 * min(wave + kPoolTeam * i, G - 1) + j) * 64 + lane];
-            const float g = v + k <= w1 ? __builtin_amdgcn_exp2f(p[32 * D + lane] - t_all) : 0.0f;
-            den = fmaf(p[32 * D + 64 + lane], g, den);
-            f[k] = g * pool_power((int)__float_as_uint(p[32 * D + 128 + lane]) - e_all);
         }
+        const float before = pool_join(t_all, den, e_all, h, v, w1);
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) sums[i] *= before;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
@@ -69,7 +64,7 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) sums[i][4 * j + m] = fmaf(x[k][i][j][m], f[k], sums[i][4 * j + m]);
+                    for (int m = 0; m < 4; ++m) sums[i][4 * j + m] = fmaf(x[k][i][j][m], h[k].factor, sums[i][4 * j + m]);
     }
     // ---- as pool_finish, the operands through LDS
     float m = 0.0f;

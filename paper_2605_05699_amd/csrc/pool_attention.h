@@ -118,6 +118,32 @@ __device__ __forceinline__ int pool_exponent(float scale) {
 }
 __device__ __forceinline__ float pool_power(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
 
+// ---- the merge: maximum, sum of weights and exponent of a part, and what its sums are to be multiplied with
+struct pool_part_head {
+    float top, den, e, factor;
+    __device__ __forceinline__ void load(const float* p, int lane) { top = p[lane], den = p[64 + lane], e = p[128 + lane]; }
+};
+// Parts v .. v + N - 1 (those behind the last, w1, are it again and count for nothing) under one maximum with what has been added so far; what its
+// sums are to be multiplied with.
+template <int N>
+__device__ __forceinline__ float pool_join(float& top, float& den, int& e, pool_part_head (&h)[N], int v, int w1) {
+    float t = top;
+    int m = e;
+#pragma unroll
+    for (int k = 0; k < N; ++k) t = fmaxf(t, h[k].top), m = max(m, (int)__float_as_uint(h[k].e));
+    const float f = __builtin_amdgcn_exp2f(top - t), before = f * pool_power(e - m);
+    den *= f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const float g = v + k <= w1 ? __builtin_amdgcn_exp2f(h[k].top - t) : 0.0f;
+        den = fmaf(h[k].den, g, den);
+        h[k].factor = g * pool_power((int)__float_as_uint(h[k].e) - m);
+    }
+    top = t;
+    e = m;
+    return before;
+}
+
 // ---- 16 codes of a row (two dwords at 4 bits, four at 8) -> two units of eight fp16 values times a scale
 template <int BITS> struct pool_codes;
 template <> struct pool_codes<4> { typedef u32x2 type; };

@@ -669,6 +669,7 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int all = (a.decode_rows + 16 * CB - 1) / (16 * CB), at = (int)(block / (unsigned)all), rb = (int)block - at * all;
     const int seq = at / a.heads, head = at - seq * a.heads;
+    const int units = a.decode_before[a.s.n_seq], units_before = a.decode_before[seq];       // (with the sequence's, in one round of loads)
     const pool_seq q = pool_seq_of(a.s, seq);
     const int rows = q.n_new * a.group, blocks_of_rows = (rows + 16 * CB - 1) / (16 * CB);
     if (rows == 0 || !pool_is_decode(q, a.group, a.decode_rows) || rb >= blocks_of_rows) return;
@@ -680,8 +681,8 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
         }
         return;
     }
-    const pool_shares shares(a.decode_before[a.s.n_seq], a.decode_grid, W);
-    const int first = a.decode_before[seq] + (head * blocks_of_rows + rb) * tiles, w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
+    const pool_shares shares(units, a.decode_grid, W);
+    const int first = units_before + (head * blocks_of_rows + rb) * tiles, w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
     if (w0 == w1) return;
     const int behind = shares.begin(w0) != first ? 1 : 0;    // the first part's workgroup began with other rows
     const auto part = [&](int w, int c) __attribute__((always_inline)) {
@@ -690,32 +691,26 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
     for (int c = 0; c < CB; ++c) {
         float t_all = kPoolLowest, den = 0.0f;
         int e_all = kPoolNoExponent;
-        for (int v = w0; v <= w1; v += AHEAD) {
-            float t[AHEAD], e[AHEAD];
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) t[k] = part(min(v + k, w1), c)[16 * D + lane], e[k] = part(min(v + k, w1), c)[16 * D + 128 + lane];
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) t_all = fmaxf(t_all, t[k]), e_all = max(e_all, (int)__float_as_uint(e[k]));
-        }
         floatx4 o[kPoolOwn<D>];
 #pragma unroll
         for (int i = 0; i < kPoolOwn<D>; ++i) o[i] = floatx4{0, 0, 0, 0};
-        for (int v = w0; v <= w1; v += AHEAD) {
+        for (int v = w0; v <= w1; v += AHEAD) {              // (one round of loads for AHEAD parts, the sums so far brought under their maximum)
             floatx4 x[AHEAD][kPoolOwn<D>];
-            float f[AHEAD];
+            pool_part_head h[AHEAD];
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 const float* const at = part(min(v + k, w1), c);
+                h[k].load(at + 16 * D, lane);
 #pragma unroll
                 for (int i = 0; i < kPoolOwn<D>; ++i) x[k][i] = reinterpret_cast<const floatx4*>(at)[min(wave + W * i, NB - 1) * 64 + lane];
-                const float g = v + k <= w1 ? __builtin_amdgcn_exp2f(at[16 * D + lane] - t_all) : 0.0f;
-                den = fmaf(at[16 * D + 64 + lane], g, den);
-                f[k] = g * pool_power((int)__float_as_uint(at[16 * D + 128 + lane]) - e_all);
             }
+            const float before = pool_join(t_all, den, e_all, h, v, w1);
+#pragma unroll
+            for (int i = 0; i < kPoolOwn<D>; ++i) o[i] *= before;
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
-                for (int i = 0; i < kPoolOwn<D>; ++i) o[i] += x[k][i] * f[k];
+                for (int i = 0; i < kPoolOwn<D>; ++i) o[i] += x[k][i] * h[k].factor;
         }
         const pool_row r = pool_row_of(q, head, a.group, (rb * CB + c) * 16 + (lane & 15));
         char* const dst = r.there ? a.out + r.token * a.out_token + r.head * a.out_head : nullptr;
