@@ -2,7 +2,7 @@
 // tokens of them): the scan over the keys, and the merge of what its workgroups leave.
 //
 // Bound by the records' bytes where there are enough of them, with the vector instructions that decode them close behind: 24 sequences up
-// to 32,768 tokens, 8 key heads of 128 channels, 4 bits: 388 MB in 110 us, 3.5 TB/s (a sum over 2 GiB reads 4.0 here; the vector ALU is busy 59 %
+// to 32,768 tokens, 8 key heads of 128 channels, 4 bits: 388 MB in 110 us, 3.5 TB/s (a sum over 2 GiB reads 4.0 here; the vector ALU is busy 60 %
 // of the time).  Codes are loaded past the L2, where nobody reads them again: 6 % slower without that.  A wavefront has
 // a tile of KEYS keys to itself, keys on the rows of the score product and 16 query rows on its columns (16x16x32; CB blocks of
 // them): a lane holds, for ITS row (lane % 16), the keys of its quarter of the wavefront (lane / 16), which is what the running maximum
