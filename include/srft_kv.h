@@ -316,8 +316,10 @@ int srft_rotary(const srft_rotary_rows* rows, int count, int64_t n_tokens, int d
  * read by the kernels, so that a step can be captured in a graph and replayed with other lengths).
  *
  * srft_pool_create   plan_k, plan_v: same d, group size, code width, transform and device.  page_tokens is 16, 32, 64, 128 or 256,
- *                    n_heads * page_tokens a multiple of 32, n_pages and n_windows >= 1 (else SRFT_ERR_BAD_N).  Allocates device tables
- *                    (12 d^2 bytes) on the plans' GPU.  The plans must outlive the pool.
+ *                    n_heads * page_tokens a multiple of 32, n_pages >= 0, n_windows >= 1 (else SRFT_ERR_BAD_N).  n_pages == 0 is a pool
+ *                    of windows alone, for sequences shorter than a page: codes_dev and scales_dev are NULL then (else SRFT_ERR_BAD_N).
+ *                    Allocates device tables (12 d^2 bytes, and a page of zeros where n_pages is 0) on the plans' GPU.  The plans
+ *                    must outlive the pool.
  */
 typedef struct srft_pool srft_pool_t;
 typedef struct srft_pool_buffers {

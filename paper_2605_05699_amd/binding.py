@@ -535,7 +535,7 @@ class PagedSeqs:
 
 class PagePool:
     """One layer's pages (srft_pool_create) over tensors of the caller's: k and v are (codes [pages, heads, R, code bytes] uint8,
-    scales [pages, heads, R, groups] float32, window [windows, heads, R, d] float16) each."""
+    scales [pages, heads, R, groups] float32, window [windows, heads, R, d] float16) each.  No pages: sequences shorter than one."""
 
     def __init__(self, plan_k: "Plan", plan_v: "Plan", k, v):
         self.handle = None
@@ -548,7 +548,7 @@ class PagePool:
                     window.shape != (windows, heads, R, d):
                 raise ValueError("codes must be [pages, heads, R, code bytes], scales [pages, heads, R, groups], window [windows, heads, R, d]")
         of = [_PoolBuffers(_dev_ptr(c, torch.uint8, "codes"), _dev_ptr(s, torch.float32, "scales"), _dev_ptr(w, torch.float16, "window"))
-              for c, s, w in (self.k, self.v)]
+              for c, s, w in (self.k, self.v)]                 # (a tensor of no pages has no address)
         handle = C.c_void_p()
         _check(lib().srft_pool_create(C.byref(handle), plan_k.handle, plan_v.handle, heads, R, pages, windows, C.byref(of[0]), C.byref(of[1])),
                "srft_pool_create")

@@ -148,12 +148,13 @@ int srft_pool_create(srft_pool_t** out, const srft_plan_t* plan_k, const srft_pl
     if (!out) return SRFT_ERR_NULL;
     *out = nullptr;
     if (!plan_k || !plan_v || !k || !v) return SRFT_ERR_NULL;
-    if (n_heads < 1 || n_heads > 1024 || !known_page(page_tokens) || n_heads * page_tokens % kTileVecs != 0 || n_pages < 1 || n_windows < 1 ||
+    if (n_heads < 1 || n_heads > 1024 || !known_page(page_tokens) || n_heads * page_tokens % kTileVecs != 0 || n_pages < 0 || n_windows < 1 ||
         n_pages >= (1LL << 31) || n_windows >= (1LL << 31))
         return SRFT_ERR_BAD_N;
     if (!srft_plans_compatible(plan_k, plan_v)) return SRFT_ERR_MISMATCH;
     for (const srft_pool_buffers* b : {k, v}) {
-        if (!b->codes_dev || !b->scales_dev || !b->window_f16_dev) return SRFT_ERR_NULL;
+        if (n_pages == 0 && (b->codes_dev || b->scales_dev)) return SRFT_ERR_BAD_N;
+        if ((n_pages > 0 && (!b->codes_dev || !b->scales_dev)) || !b->window_f16_dev) return SRFT_ERR_NULL;
         if (!srft_aligned(b->codes_dev, 16) || !srft_aligned(b->scales_dev, 16) || !srft_aligned(b->window_f16_dev, 16)) return SRFT_ERR_ALIGN;
     }
     return srft_no_throw([&] {

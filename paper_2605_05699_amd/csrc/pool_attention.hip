@@ -120,12 +120,21 @@ int srft_pool_tables(srft_pool* p) {
                     image[at] = oh[src];
                     image[at + 64 * 8] = ol[src];
                 }
+    // The scans read page 0 in the place of one that does not exist (and count it for nothing): where there is none, zeros behind the tables.
+    const size_t rows = p->n_pages > 0 ? 0 : (size_t)p->heads * p->R, code_bytes = rows * d * bits / 8, scale_bytes = rows * (d / p->plan_k->g) * 4;
+    const size_t table_bytes = image.size() * 2;
+    image.resize((table_bytes + code_bytes + scale_bytes) / 2);
     for (int cb = 1; cb <= 2; ++cb) {
         SRFT_HIP(hipOccupancyMaxActiveBlocksPerMultiprocessor(&p->decode_blocks[cb - 1], (const void*)srft_pool_decode_kernel_of(p->plan_k, cb), 64 * kPoolTeam, 0));
         p->decode_blocks[cb - 1] = std::max(1, std::min(4, p->decode_blocks[cb - 1]));
     }
     SRFT_HIP(hipMalloc((void**)&p->tables, image.size() * 2));
     SRFT_HIP(hipMemcpy(p->tables, image.data(), image.size() * 2, hipMemcpyHostToDevice));
+    if (rows > 0)
+        for (srft_pool_buffers* b : {&p->k, &p->v}) {
+            b->codes_dev = (uint8_t*)p->tables + table_bytes;
+            b->scales_dev = (float*)(b->codes_dev + code_bytes);
+        }
     return SRFT_OK;
 }
 
