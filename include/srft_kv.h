@@ -338,6 +338,8 @@ int srft_pool_destroy(srft_pool_t* pool);        /* NULL is accepted; the buffer
  * another window than windows[b][0] (no other sequence's either), else it is the same.
  * max_new and max_length bound what the device arrays hold: they size launches and workspaces.  What is beyond them is cut off;
  * a page or window number out of range names no memory: its tokens are neither read nor written, and count for nothing.
+ * Each row belongs to one sequence at most.  Where starts give rows to several, calls keep to their buffers; which pages they fill and
+ * which rows they answer is not defined then.
  * 0 <= n_seq <= 4096, 0 <= max_new, 0 <= max_length < 2^30, max_pages >= max_length / R (else SRFT_ERR_BAD_N).
  */
 typedef struct srft_paged_seqs {

@@ -13,7 +13,7 @@ namespace {
 // two kernels need no order between their parts.  The list is in no fixed order (a counter in LDS); every page is quantized by itself, so the
 // results do not depend on it.
 constexpr int kWindowUnits = 1024;                           // of 16 bytes: what a workgroup copies at a time
-__global__ void __launch_bounds__(256) srft_pool_window_kernel(const pool_append_args a, int U, int split) {
+__global__ void __launch_bounds__(256) srft_pool_window_kernel(const pool_append_args a, int U, int split, int most) {
     const pool_seqs& s = a.s;
     const int R = 1 << s.log_R;
     if (blockIdx.x == 0) {
@@ -22,25 +22,28 @@ __global__ void __launch_bounds__(256) srft_pool_window_kernel(const pool_append
         __shared__ int listed;
         int base = 0;
         if (threadIdx.x == 0) listed = 0;
-        for (int b0 = 0; b0 < s.n_seq; b0 += 256) {          // exclusive sums of the candidates per sequence
+        // Exclusive sums of the candidates per sequence.  They stop at `most`, the entries that the workspace holds: starts that overlap count
+        // new tokens more than once.
+        for (int b0 = 0; b0 < s.n_seq; b0 += 256) {
             const int b = b0 + threadIdx.x;
             int n = 0;
             if (b < s.n_seq) {
                 const pool_seq q = pool_seq_of(s, b);
-                n = max((q.length >> s.log_R) - (max(q.before, 0) >> s.log_R), 0);
+                n = min(max((q.length >> s.log_R) - (max(q.before, 0) >> s.log_R), 0), most);
             }
             int sum = n;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
                 const int other = __shfl_up(sum, d);
-                if ((int)(threadIdx.x & 63) >= d) sum += other;
+                if ((int)(threadIdx.x & 63) >= d) sum = min(sum + other, most);
             }
+            const int left = __shfl_up(sum, 1);
             if ((threadIdx.x & 63) == 63) wave_sums[threadIdx.x >> 6] = sum;
             __syncthreads();
-            int before = base;
+            int before = base + ((threadIdx.x & 63) > 0 ? left : 0);
             for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += wave_sums[w];
-            base += wave_sums[0] + wave_sums[1] + wave_sums[2] + wave_sums[3];
-            if (b < s.n_seq) prefix[b] = before + sum - n;
+            base = min(base + wave_sums[0] + wave_sums[1] + wave_sums[2] + wave_sums[3], most);
+            if (b < s.n_seq) prefix[b] = min(before, most);
             __syncthreads();
         }
         if (threadIdx.x == 0) prefix[s.n_seq] = base;
@@ -219,7 +222,7 @@ int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const
     // d = 256 took 9.7 us, now 4.1)
     const int64_t units = (int64_t)std::min<int64_t>(seqs->max_new, pool->R) * pool->heads * pool->units();
     const int split = (int)std::max<int64_t>(1, std::min<int64_t>((units + kWindowUnits - 1) / kWindowUnits, 4096 / (2 * seqs->n_seq)));
-    rc = srft_launch(srft_pool_window_kernel, dim3((unsigned)(1 + 2 * seqs->n_seq * split)), 256, st, a, pool->units(), split);
+    rc = srft_launch(srft_pool_window_kernel, dim3((unsigned)(1 + 2 * seqs->n_seq * split)), 256, st, a, pool->units(), split, (int)fills);
     if (rc != SRFT_OK) return rc;
     int threads = 0;
     const pool_append_kernel_t kernel = srft_plan_pool_append_kernel(pk, &threads);
