@@ -28,9 +28,11 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
         return;
     }
     const int* const before = a.chunk_before;
+    const int units = before[a.s.n_seq];
+    if (units == 0) return;                                  // (too many of them: see kPoolMostUnits)
     const int first = before[seq] + head * pool_chunk_units(q, a.group, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS) +
                       pool_chunk_units(q, a.group, ROWS, KEYS, rt);
-    const pool_shares shares(before[a.s.n_seq], a.chunk_grid, 1);
+    const pool_shares shares(units, a.chunk_grid, 1);
     const int w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
     if (w0 == w1) return;
     const int behind = shares.begin(w0) != first ? 1 : 0;    // the first part's workgroup began with other rows

@@ -34,17 +34,19 @@ __device__ __forceinline__ void count_units(const pool_attention_args& a) {
     __syncthreads();
     for (int which = wave; which < 2; which += NT / 64) {
         int* const at = which == 0 ? a.decode_before : a.chunk_before;
-        int sum = 0;
+        unsigned sum = 0;
         if (lane == 0) at[0] = 0;
         for (int b0 = 1; b0 <= s.n_seq; b0 += 64) {
-            int x = b0 + lane <= s.n_seq ? at[b0 + lane] : 0;
+            const int b = b0 + lane;
+            unsigned x = b <= s.n_seq ? at[b] : 0;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
-                const int other = __shfl_up(x, d);
-                if (lane >= d) x += other;
+                const unsigned other = __shfl_up(x, d);
+                if (lane >= d) x = min(x + other, kPoolMostUnits);
             }
-            if (b0 + lane <= s.n_seq) at[b0 + lane] = sum + x;
-            sum += __shfl(x, 63);
+            const unsigned before = min(sum + x, kPoolMostUnits);
+            if (b <= s.n_seq) at[b] = b == s.n_seq && before == kPoolMostUnits ? 0 : (int)before;
+            sum = min(sum + (unsigned)__shfl(x, 63), kPoolMostUnits);
         }
     }
 }

@@ -64,6 +64,9 @@ template <int D> constexpr int kPoolPart = 32 * D + 3 * 64;
 constexpr long long pool_part(int d) { return 32LL * d + 3 * 64; }
 
 // ---- units of work.  A tile is of pages' keys or of the window's, never of both.
+// Rows that belong to one sequence each come to less than kPoolMostUnits of them (the host's checks).  Starts that give the same rows to many
+// sequences can come to more: then there are none, and nothing is answered.
+constexpr unsigned kPoolMostUnits = 0x7FFFFF00;         // (sums of it and a small number are below 2^31)
 __device__ __forceinline__ int pool_tiles(int seen, int full, int keys) {
     const int pages = max(min(seen, full), 0), window = max(seen - full, 0);
     return (pages + keys - 1) / keys + (window + keys - 1) / keys;

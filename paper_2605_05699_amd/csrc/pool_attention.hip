@@ -63,9 +63,9 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, int64_t n_new, int
     const int rc = srft_pool_check(pool, seqs, n_new);
     if (rc != SRFT_OK) return rc;
     if (q_heads < 1 || q_heads % pool->heads != 0 || q_heads > 64 * pool->heads || n_new * q_heads >= (1LL << 31) - 32) return SRFT_ERR_BAD_N;
-    // units of work, tiles and workgroups are counted with 32 bits
+    // units of work (kPoolMostUnits), tiles and workgroups are counted with 32 bits
     const int d = pool->plan_k->d, group = q_heads / pool->heads, rows = kPoolBlock * kPoolChunkWaves;
-    const int64_t most = 1LL << 31, tiles = seqs->max_length / 32 + 2, heads = (int64_t)seqs->n_seq * pool->heads;
+    const int64_t most = kPoolMostUnits, tiles = seqs->max_length / 32 + 2, heads = (int64_t)seqs->n_seq * pool->heads;
     const int64_t blocks = row_blocks(seqs, n_new, group, rows), all_blocks = n_new * group / rows + seqs->n_seq;
     if (2 * heads * tiles >= most || all_blocks * pool->heads * tiles >= most || heads * std::max<int64_t>(blocks, 1) * kPoolChunkWaves >= most ||
         heads * pool->R / kTileVecs * 2 >= most / 2)

@@ -698,6 +698,7 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
         }
         return;
     }
+    if (units == 0) return;                                  // (too many of them: see kPoolMostUnits)
     const pool_shares shares(units, a.decode_grid, W);
     const int first = units_before + (head * blocks_of_rows + rb) * tiles, w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
     if (w0 == w1) return;

@@ -80,3 +80,27 @@ def test_zeros_behind_the_last_sequence_are_no_overlap(B):
             assert np.array_equal(got[0].reshape(want.shape), want.cpu().numpy()) and np.array_equal(got[1].reshape(scales.shape), scales.cpu().numpy())
             assert np.array_equal(s.window(which, b)[: n - full], s.tokens[which][b][full:])
     s.close()
+
+
+@pytest.mark.parametrize("n,new,length", [(65, 40, 300), (66, 700, 900), (4096, 32768, 1 << 20)])
+def test_attention_keeps_to_its_workspace(B, n, new, length):
+    """Every second sequence brings all rows.  The last case comes to more pairs of tiles of keys and blocks of rows than 32 bits count."""
+    d, R, heads = 64, 256, 1
+    plans = [B.Plan(d, 32, 5 + i) for i in range(2)]
+    pool = B.PagePool.empty(*plans, heads, R, 1, 1)
+    table = torch.full((n, length // R), -1, dtype=torch.int32, device="cuda")               # (no page is there: a tile costs little)
+    windows = torch.full((n, 2), -1, dtype=torch.int32, device="cuda")
+    starts = ints([new * (i % 2) for i in range(n + 1)])
+    seqs = B.PagedSeqs(table, windows, ints([length] * n), starts, max_new=new, max_length=length)
+    if n == 4096:
+        tiles = sum((length - new + (r + 1) * 256) // 64 for r in range(new // 256))
+        assert tiles * (n // 2) > 1 << 31
+    q = torch.randn(new, heads, d, device="cuda").half()
+    rows = q.numel() * 2
+    out_whole, out = guarded(rows)
+    whole, space = guarded(B.srft_pool_attention_workspace_bytes(pool, seqs, new, heads))
+    assert space.data_ptr() % 256 == 0
+    B.srft_pool_attention(pool, seqs, q, 0.1, out.view(F16).view(new, heads, d), space)
+    torch.cuda.synchronize()
+    assert untouched(whole) and untouched(out_whole)
+    pool.close()
