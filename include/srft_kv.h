@@ -372,7 +372,8 @@ int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const
  *   q_dev, out_dev   [n_new][n_q_heads][d], both of `type` (SRFT_F16 or SRFT_BF16), 16-byte aligned, strides in elements, multiples of 8.
  *   n_q_heads        a multiple of n_heads, at most 64 n_heads.
  *   softmax_scale    finite.
- *   workspace_dev    srft_pool_attention_workspace_bytes bytes, 256-byte aligned, overwritten.
+ *   workspace_dev    srft_pool_attention_workspace_bytes bytes, 256-byte aligned, overwritten.  (Whatever srft_plan_set_max_workgroups is
+ *                    called with before or after: the size does not depend on it.)
  */
 int64_t srft_pool_attention_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, int64_t n_new, int n_q_heads);
 int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, const void* q_dev, int type, int64_t n_new, int n_q_heads,

@@ -11,7 +11,12 @@ struct workspace {
     int64_t decode_before, chunk_before, q_rows, q_rows_low, q_factor, tail_rows, tail_factor, tail_columns, decode_parts, chunk_parts, bytes;
     int decode_grid, chunk_grid;
 };
-int workgroups(const srft_pool* p, int per_unit) { return p->plan_k->max_wgs > 0 ? p->plan_k->max_wgs : p->plan_k->compute_units * per_unit; }
+// Workgroups of a launch.  A cap on them (srft_plan_set_max_workgroups) may change between the call that sizes a workspace and the one that
+// uses it: it makes launches smaller, never larger, and the workspace is for launches without one.
+int workgroups(const srft_pool* p, int per_unit) {
+    const int all = p->plan_k->compute_units * per_unit;
+    return p->plan_k->max_wgs > 0 ? std::min(p->plan_k->max_wgs, all) : all;
+}
 int64_t row_blocks(const srft_paged_seqs* s, int64_t n_new, int group, int rows) {           // of one sequence and key head, at most
     return (std::min<int64_t>(s->max_new, n_new) * group + rows - 1) / rows;
 }
@@ -39,7 +44,8 @@ workspace layout(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new, in
         return here;
     };
     const split s16 = split_of(s, n_new, group, d);
-    w.decode_grid = workgroups(p, p->decode_blocks[s16.cb - 1]);
+    const int cus = p->plan_k->compute_units, per_unit = p->decode_blocks[s16.cb - 1];
+    w.decode_grid = workgroups(p, per_unit);
     w.chunk_grid = workgroups(p, 1);
     w.decode_before = take(4LL * (s->n_seq + 1));
     w.chunk_before = take(4LL * (s->n_seq + 1));
@@ -49,8 +55,8 @@ workspace layout(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new, in
     w.tail_rows = take(2 * tail * d);
     w.tail_factor = take(4 * tail);
     w.tail_columns = take(tail * d);
-    w.decode_parts = take(2LL * w.decode_grid * s16.cb * (16 * d + 3 * 64) * 4);
-    w.chunk_parts = take(s16.chunk ? 2LL * w.chunk_grid * kPoolChunkWaves * pool_part(d) * 4 : 0);
+    w.decode_parts = take(2LL * cus * per_unit * s16.cb * (16 * d + 3 * 64) * 4);
+    w.chunk_parts = take(s16.chunk ? 2LL * cus * kPoolChunkWaves * pool_part(d) * 4 : 0);
     w.bytes = at;
     return w;
 }
