@@ -383,7 +383,8 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
 /*
  * Copies inside pools: page pages[i][0] to page pages[i][1] and window windows[i][0] to windows[i][1], K and V, in each of n_pools pools of
  * one geometry (the layers of a model): what a fork or a compaction needs.  Device arrays [n][2] of int32.  No destination may be
- * another destination or a source of the same call; a pair with a number out of range is skipped.  Up to 64 pools go into one launch.
+ * another destination or a source of the same call; a pair with a number out of range is skipped.  Up to 64 pools and 2^22 pairs of pages and
+ * of windows each go into one launch.
  */
 int srft_pool_copy(const srft_pool_t* const* pools, int n_pools, const int32_t* pages_dev, int64_t n_page_pairs,
                    const int32_t* windows_dev, int64_t n_window_pairs, void* hip_stream);

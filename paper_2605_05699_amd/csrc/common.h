@@ -321,6 +321,11 @@ int srft_launch(void (*kernel)(P...), dim3 grid, int threads, hipStream_t st, co
     return srft_hip_fail(e);
 }
 
+// A grid of n workgroups whose kernel takes the number blockIdx.y * gridDim.x + blockIdx.x and has nothing to do from n on: a dimension is limited
+// to less than 2^32 threads.
+constexpr int64_t kGridRow = 1 << 20;
+inline dim3 srft_grid(int64_t n) { return n <= kGridRow ? dim3((unsigned)n) : dim3((unsigned)kGridRow, (unsigned)((n + kGridRow - 1) / kGridRow)); }
+
 // the kernels a plan launches, and their block sizes
 // (tiles: of the launch; lines: its results start at a multiple of 64 bytes)
 quantize_kernel_t srft_plan_quantize_kernel(const srft_plan* p, int out, int* threads, long long n_tiles = 0, bool lines = true);

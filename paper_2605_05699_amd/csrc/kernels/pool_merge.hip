@@ -119,10 +119,12 @@ template <int D, int CB>
 __global__ void __launch_bounds__(64 * kPoolTeam) srft_pool_merge_kernel(const pool_attention_args a) {
     constexpr int OPS = D / 16 * 2 * 64;
     __shared__ __align__(16) unsigned char lds[std::max(kPoolFinishBytes<D>, OPS * 16 + kPoolTeam * 32 * 4)];
-    if (blockIdx.x < (unsigned)a.decode_merges)              // uniform
-        pool_decode_merge<D, CB>(a, blockIdx.x, lds);
+    const unsigned workgroup = blockIdx.y * gridDim.x + blockIdx.x;          // (what follows is uniform)
+    if (workgroup >= a.merges) return;
+    if (workgroup < (unsigned)a.decode_merges)
+        pool_decode_merge<D, CB>(a, workgroup, lds);
     else
-        chunk_merge<D>(a, blockIdx.x - a.decode_merges, reinterpret_cast<uint4*>(lds), reinterpret_cast<float (*)[32]>(lds + OPS * 16));
+        chunk_merge<D>(a, workgroup - a.decode_merges, reinterpret_cast<uint4*>(lds), reinterpret_cast<float (*)[32]>(lds + OPS * 16));
 }
 
 template <int D> pool_attention_kernel_t pick(int cb) {

@@ -48,7 +48,7 @@ __device__ __forceinline__ float2 turn(double t) {
     return make_float2(c, s);
 }
 
-// V: pairs of a thread; IN, OUT: types.  One workgroup per token (blockIdx.x); LDS: rot / 2 pairs (cos, sin) times factor.
+// V: pairs of a thread; IN, OUT: types.  One workgroup per token (srft_grid); LDS: rot / 2 pairs (cos, sin) times factor.
 template <class IN, class OUT, int V>
 __device__ __forceinline__ void rows_of_token(const rotary_args& a, const srft_rotary_rows& t, long long token, const float2* cs) {
     const IN* const in = (const IN*)t.in_dev + token * t.in_token;
@@ -105,9 +105,10 @@ __device__ __forceinline__ void rows_of_token(const rotary_args& a, const srft_r
 }
 
 template <class IN, class OUT, int V>
-__global__ void __launch_bounds__(256) srft_rotary_kernel(const rotary_args a, int count) {
+__global__ void __launch_bounds__(256) srft_rotary_kernel(const rotary_args a, int count, unsigned n_tokens) {
     __shared__ float2 cs[512];
-    const long long token = blockIdx.x;
+    const long long token = blockIdx.y * gridDim.x + blockIdx.x;
+    if (token >= n_tokens) return;                           // (uniform)
     const double pos = (double)a.positions[token];
     for (int i = threadIdx.x; i < a.rot / 2; i += blockDim.x) {
         const float2 t = turn(pos * a.freq[i]);
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(256) srft_rotary_kernel(const rotary_args a, i
     for (int k = 0; k < count; ++k) rows_of_token<IN, OUT, V>(a, a.t[k], token, cs);
 }
 
-typedef void (*rotary_kernel_t)(const rotary_args, int);
+typedef void (*rotary_kernel_t)(const rotary_args, int, unsigned);
 template <class IN, class OUT> rotary_kernel_t pick(int v) {
     if (v == 8) return srft_rotary_kernel<IN, OUT, 8>;
     return v == 4 ? srft_rotary_kernel<IN, OUT, 4> : srft_rotary_kernel<IN, OUT, 1>;
@@ -189,7 +190,7 @@ extern "C" int srft_rotary(const srft_rotary_rows* rows, int count, int64_t n_to
                                        : rows[i].in_type == SRFT_F16 ? pick<_Float16>(rows[i].out_type, v)
                                                                      : pick<bf16>(rows[i].out_type, v);
         const int threads = (int)std::min(256LL, (units * a.row_units[1] + 63) / 64 * 64);
-        const int rc = srft_launch(kernel, dim3((unsigned)n_tokens), threads, (hipStream_t)hip_stream, a, n);
+        const int rc = srft_launch(kernel, srft_grid(n_tokens), threads, (hipStream_t)hip_stream, a, n, (unsigned)n_tokens);
         if (rc != SRFT_OK) return rc;
     }
     return SRFT_OK;

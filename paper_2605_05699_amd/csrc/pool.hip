@@ -95,6 +95,7 @@ __global__ void __launch_bounds__(256) srft_pool_window_kernel(const pool_append
 // ordinary loads and stores, which leave in the L2 what nobody reads next, 194.
 constexpr int kCopyPools = 64;
 constexpr int kCopyUnits = 2048;                           // of 16 bytes, a workgroup's
+constexpr int kCopyPairs = 1 << 22;                         // of pages and of windows in a launch, whose first dimension is limited to 2^32 threads
 struct pool_copy_args {
     struct { char *codes, *scales, *window; } of[kCopyPools][2];
     struct { const int32_t* pairs; int n_pairs, count, units[2]; } what[2];  // pages, windows: numbers that exist; 16-byte units of codes and scales, or of a window and 0
@@ -227,7 +228,7 @@ int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const
     int threads = 0;
     const pool_append_kernel_t kernel = srft_plan_pool_append_kernel(pk, &threads);
     if (!kernel) return SRFT_ERR_BAD_D;
-    const int64_t budget = std::max(1, (pk->max_wgs > 0 ? pk->max_wgs : pk->grid_q) / 2);
+    const int64_t budget = std::clamp((pk->max_wgs > 0 ? pk->max_wgs : pk->grid_q) / 2, 1, 1 << 20);
     return srft_launch(kernel, dim3((unsigned)(2 * std::min(fills * page_tiles, budget))), threads, st, a);
 }
 
@@ -249,19 +250,23 @@ int srft_pool_copy(const srft_pool_t* const* pools, int n_pools, const int32_t* 
     if (pairs == 0) return SRFT_OK;
     const srft_pool* p = pools[0];
     const int rows = p->heads * p->R, d = p->plan_k->d;
-    for (int i0 = 0; i0 < n_pools; i0 += kCopyPools) {
+    const auto some = [](int64_t all, int64_t from) { return (int)std::clamp<int64_t>(all - from, 0, kCopyPairs); };
+    for (int64_t at = 0; at < std::max(n_page_pairs, n_window_pairs); at += kCopyPairs) {
+        const int pages = some(n_page_pairs, at), windows = some(n_window_pairs, at);
         pool_copy_args a;
-        const int n = std::min(kCopyPools, n_pools - i0);
-        for (int i = 0; i < n; ++i)
-            for (int v = 0; v < 2; ++v) {
-                const srft_pool_buffers& b = v ? pools[i0 + i]->v : pools[i0 + i]->k;
-                a.of[i][v] = {(char*)b.codes_dev, (char*)b.scales_dev, (char*)b.window_f16_dev};
-            }
-        a.what[0] = {pages_dev, (int)n_page_pairs, p->n_pages, {rows * d * p->plan_k->bits / 128, rows * (d / p->plan_k->g) / 4}};
-        a.what[1] = {windows_dev, (int)n_window_pairs, p->n_windows, {rows * d / 8, 0}};
-        const int units = 2 * std::max(n_page_pairs ? a.what[0].units[0] + a.what[0].units[1] : 0, n_window_pairs ? a.what[1].units[0] : 0);
-        const int rc = srft_launch(srft_pool_copy_kernel, dim3((unsigned)pairs, (unsigned)n, (unsigned)((units + kCopyUnits - 1) / kCopyUnits)), 256, (hipStream_t)hip_stream, a);
-        if (rc != SRFT_OK) return rc;
+        a.what[0] = {pages_dev + 2 * at, pages, p->n_pages, {rows * d * p->plan_k->bits / 128, rows * (d / p->plan_k->g) / 4}};
+        a.what[1] = {windows_dev + 2 * at, windows, p->n_windows, {rows * d / 8, 0}};
+        const int units = 2 * std::max(pages ? a.what[0].units[0] + a.what[0].units[1] : 0, windows ? a.what[1].units[0] : 0);
+        for (int i0 = 0; i0 < n_pools; i0 += kCopyPools) {
+            const int n = std::min(kCopyPools, n_pools - i0);
+            for (int i = 0; i < n; ++i)
+                for (int v = 0; v < 2; ++v) {
+                    const srft_pool_buffers& b = v ? pools[i0 + i]->v : pools[i0 + i]->k;
+                    a.of[i][v] = {(char*)b.codes_dev, (char*)b.scales_dev, (char*)b.window_f16_dev};
+                }
+            const int rc = srft_launch(srft_pool_copy_kernel, dim3((unsigned)(pages + windows), (unsigned)n, (unsigned)((units + kCopyUnits - 1) / kCopyUnits)), 256, (hipStream_t)hip_stream, a);
+            if (rc != SRFT_OK) return rc;
+        }
     }
     return SRFT_OK;
 }

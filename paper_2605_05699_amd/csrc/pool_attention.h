@@ -58,6 +58,7 @@ struct pool_attention_args {
     int decode_grid, chunk_grid;
     int decode_rows, decode_block, decode_keys;              // rows that go to pool_decode, those of a workgroup, keys of its tiles
     int merge_blocks, decode_merges;                         // of 32 rows, of a sequence and key head; workgroups that merge what pool_decode left
+    unsigned merges;                                         // workgroups of pool_merge (srft_grid)
 };
 // Sums of a block of 32 rows that a segment leaves: [D / 8 float4][64 lanes], then per lane maximum, sum of weights and V's exponent.
 template <int D> constexpr int kPoolPart = 32 * D + 3 * 64;

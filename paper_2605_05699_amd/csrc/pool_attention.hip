@@ -74,7 +74,7 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, int64_t n_new, int
     const int64_t most = kPoolMostUnits, tiles = seqs->max_length / 32 + 2, heads = (int64_t)seqs->n_seq * pool->heads;
     const int64_t blocks = row_blocks(seqs, n_new, group, rows), all_blocks = n_new * group / rows + seqs->n_seq;
     if (2 * heads * tiles >= most || all_blocks * pool->heads * tiles >= most || heads * std::max<int64_t>(blocks, 1) * kPoolChunkWaves >= most ||
-        heads * pool->R / kTileVecs * 2 >= most / 2)
+        (heads * pool->R / kTileVecs * 2 + pool->plan_k->compute_units * 3 + 1) * 2 * d > UINT32_MAX)        // (threads of pool_rotate)
         return SRFT_ERR_BAD_N;
     return SRFT_OK;
 }
@@ -217,8 +217,8 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb), dim3((unsigned)a.decode_grid), 64 * kPoolTeam, st, a);
     a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * kPoolChunkWaves) * kPoolChunkWaves;
     a.decode_merges = sp.decode ? heads * ((a.decode_rows + a.decode_block - 1) / a.decode_block) : 0;
-    const unsigned merges = (unsigned)(a.decode_merges + (sp.chunk ? heads * a.merge_blocks : 0));
-    if (rc == SRFT_OK && merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb), dim3(merges), 64 * kPoolTeam, st, a);
+    a.merges = (unsigned)a.decode_merges + (sp.chunk ? (unsigned)heads * a.merge_blocks : 0);
+    if (rc == SRFT_OK && a.merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb), srft_grid(a.merges), 64 * kPoolTeam, st, a);
     return rc;
 }
 
