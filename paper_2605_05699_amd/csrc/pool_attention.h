@@ -15,7 +15,7 @@
 // cores bound, has one matrix instruction where that would take two: q', the dequantized w (code * scale, the scale rounded first) and
 // the weights p are fp16, half a step (2^-11) each at most.  Against 64 bits that is 3e-4 and 1.2e-3 of an output's size, the output's own
 // rounding to fp16 included.  Sums, maxima and exponents are fp32.  None of the operands can leave fp16's range: q' has a power of two per
-// row, w a running one taken from the scales, the weights are at most 2^kLazy.
+// row, w a running one taken from the scales, the weights are at most 2^(kLazy + kHigh) in pool_chunk, and times a scale 2^(kLazy + 7) in pool_decode.
 //
 // Order of channels.  A dword of codes is decoded into eight fp16 values in the order 0 4 1 5 2 6 3 7 (4 bits; 0 2 1 3 at 8 bits), so
 // all operands have their channels in that order within units of eight ("positions"), q' by the way it is stored, the output by the
@@ -28,6 +28,10 @@
 constexpr float kPoolLowest = -3.0e38f;                      // "no key yet": finite, so that differences of two are
 constexpr int kPoolNoExponent = -200;                        // of V: "no value yet"
 constexpr float kLazy = 8.0f;                                // how far (in powers of two) weights may grow past the maximum that they are taken from
+// pool_chunk rounds weights to fp16, so it takes them as large as that allows: up to 2^(kLazy + kHigh).  What is lost then are weights below
+// 2^-32 of a row's largest; under the maximum itself they were those below 2^-25, and behind one dominant key the others lost up to 2^-25 of it each (3 %
+// of the output over 2^20 keys).  From kNear on, where an exponent's own rounding could take a weight past fp16's range, they have the older room.
+constexpr float kHigh = 7.0f, kNear = 1048576.0f;
 constexpr int kPoolDecodeRows = 32;                          // most rows of one key head that pool_decode takes, in blocks of 16
 constexpr int kPoolTeam = 4;                                 // wavefronts of a workgroup of pool_decode and pool_merge
 constexpr int pool_decode_keys(int d, int cb) { return d <= 128 && cb == 1 ? 64 : 32; }      // of a tile
@@ -197,7 +201,7 @@ __device__ __forceinline__ half8 pool_transposed(const unsigned char* keys0, con
 // What a wavefront holds of 32 rows: sums[b][v] is position 32 b + 8 (v / 4) + 4 (l / 32) + v % 4 of row l % 32.
 template <int D> struct pool_block {
     floatx16 sums[D / 32];
-    float top, den;                                          // maximum (a power of two's exponent), sum of weights (of this lane's keys)
+    float top, den;                                          // what weights are taken under (an exponent, see kLazy and kHigh), sum of weights (of this lane's keys)
     int e;                                                   // sums are to be multiplied by 2^e
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -224,7 +228,7 @@ template <int D> struct pool_block {
 };
 
 // A tile's weights.  s: scores of K keys, register v of 32 of them key 8 (v / 4) + 4 (l / 32) + v % 4; c > 0 turns them into
-// exponents.  Masked scores are -infinity.  On return the weights, under b.top; the block's sums are scaled where that grew.
+// exponents.  Masked scores are -infinity.  On return the weights, 2^(exponent - b.top); the block's sums are scaled where that grew.
 template <int D, int N>
 __device__ __forceinline__ void pool_weights(pool_block<D>& b, floatx16 (&s)[N], float c, int e, bool first) {
     float m = fmaxf(s[0][0], s[0][1]);
@@ -234,10 +238,11 @@ __device__ __forceinline__ void pool_weights(pool_block<D>& b, floatx16 (&s)[N],
         for (int v = n == 0 ? 2 : 0; v < 16; ++v) m = fmaxf(m, s[n][v]);
     m = fmaxf(other_half_max(m) * c, kPoolLowest);
     // The sums are kept under an older maximum as long as no weight passes 2^kLazy: after the first tiles they are hardly ever scaled.
-    const bool grown = m > b.top + kLazy;
+    const bool near = fabsf(b.top) < kNear;
+    const bool grown = m > b.top + (near ? kLazy + kHigh : kLazy);
     const int e_new = max(b.e, e);                           // (uniform)
     if (__ballot(grown) || e_new != b.e) {
-        const float t = grown ? m : b.top, f = __builtin_amdgcn_exp2f(b.top - t);
+        const float t = grown ? m - (fabsf(m) < kNear ? kHigh : 0.0f) : b.top, f = __builtin_amdgcn_exp2f(b.top - t);
         if (!first) b.scale(f * pool_power(b.e - e_new));
         b.den *= f;
         b.top = t;
