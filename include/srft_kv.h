@@ -285,7 +285,7 @@ int srft_lambda_from_absmax(const float* amax_host, int d, float* lambda_host);
  * inverse != 0 turns by -t: with the same factor that is the gradient of the call with inverse = 0.
  *   rows        HOST array of `count` tensors (0 .. SRFT_ROTARY_MAX), each [n_tokens][n_heads][d] in in_dev and out_dev with the
  *               given strides in elements (the channels next to each other).  out_dev == in_dev with the same strides and type
- *               turns in place; overlapping otherwise is not allowed.  Every pointer is aligned to its element.
+ *               turns in place (with others: SRFT_ERR_BAD_N); overlapping otherwise is not allowed.  Every pointer is aligned to its element.
  *   layout      SRFT_ROTARY_HALF: pair i is channels i and i + rot / 2.  SRFT_ROTARY_PAIRS: channels 2 i and 2 i + 1.
  *   positions_dev  [n_tokens] int32;  freq_dev [rot / 2] fp64, radians per token (of a long context: whatever scaling the
  *               model takes, srft_rotary knows of none).  Angles are formed and reduced in 64 bits.

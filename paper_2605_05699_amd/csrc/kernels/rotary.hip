@@ -158,6 +158,10 @@ extern "C" int srft_rotary(const srft_rotary_rows* rows, int count, int64_t n_to
         if (!rows[i].in_dev || !rows[i].out_dev) return SRFT_ERR_NULL;
         if (!srft_aligned(rows[i].in_dev, type_bytes(rows[i].in_type)) || !srft_aligned(rows[i].out_dev, type_bytes(rows[i].out_type)))
             return SRFT_ERR_ALIGN;
+        // in place a thread writes where it has read, and nowhere else
+        if (rows[i].in_dev == rows[i].out_dev && (rows[i].in_type != rows[i].out_type || (n_tokens > 1 && rows[i].in_token != rows[i].out_token) ||
+                                                  (rows[i].n_heads > 1 && rows[i].in_head != rows[i].out_head)))
+            return SRFT_ERR_BAD_N;
     }
     // tensors of one pair of types and one width share a launch
     bool done[SRFT_ROTARY_MAX] = {};

@@ -116,3 +116,18 @@ def test_copies_of_more_pairs_than_one_dimension_of_a_launch_holds(B):
             old[b] = old[a]
         assert torch.equal(x, old)
     pool.close()
+
+
+def test_rotary_in_place_where_a_stride_does_not_count(B):
+    """One token, one head: what their strides are is nothing that in and out can differ in."""
+    from tests.test_gpu_rotary import check as turned_right
+    positions, freq = torch.tensor([70], dtype=torch.int32, device="cuda"), torch.rand(32, device="cuda", dtype=torch.float64)
+    for shape, a, b in (((1, 5, 64), (320, 64, 1), (8, 64, 1)), ((1, 1, 64), (64, 64, 1), (8, 128, 1))):
+        x = torch.randn(shape, device="cuda").half()
+        first = x.clone()
+        B.srft_rotary([(x.as_strided(shape, a), x.as_strided(shape, b))], positions, freq)
+        torch.cuda.synchronize()
+        turned_right(x, first, positions, freq, "half", 1.0, False)
+    with pytest.raises(B.SrftError) as e:
+        B.srft_rotary([(x, x.view(torch.bfloat16))], positions, freq)
+    assert e.value.status == -7

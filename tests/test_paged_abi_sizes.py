@@ -1,0 +1,16 @@
+"""Rotary positions at the C boundary, without a GPU: what else is refused before any HIP call."""
+import pytest
+
+from paper_2605_05699_amd import binding as B
+from tests.test_paged_abi import rotary
+
+
+@pytest.fixture(scope="module")
+def L():
+    return B.lib()
+
+
+def test_rotary_in_place_takes_one_type_and_one_layout(L):
+    here = 1 << 20
+    for other in (dict(out_type=2), dict(in_type=0, out_type=1), dict(out_token=256), dict(out_head=72), dict(in_token=0), dict(in_head=0)):
+        assert rotary(L, out_dev=here, **other) == -7, other
