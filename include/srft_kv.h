@@ -289,8 +289,9 @@ int srft_lambda_from_absmax(const float* amax_host, int d, float* lambda_host);
  *   layout      SRFT_ROTARY_HALF: pair i is channels i and i + rot / 2.  SRFT_ROTARY_PAIRS: channels 2 i and 2 i + 1.
  *   positions_dev  [n_tokens] int32;  freq_dev [rot / 2] fp64, radians per token (of a long context: whatever scaling the
  *               model takes, srft_rotary knows of none).  Angles are formed and reduced in 64 bits.
- * d even, 2 <= d <= 1024, rot even, 0 <= rot <= d, types of srft_dtype, n_tokens * n_heads < 2^31 (else SRFT_ERR_BAD_N).  n_tokens == 0 or count == 0 is
- * a successful no-op.  One kernel.
+ * d even, 2 <= d <= 1024, rot even, 0 <= rot <= d, types of srft_dtype, n_tokens * n_heads < 2^31, n_heads * d < 2^31 (else SRFT_ERR_BAD_N).
+ * n_tokens == 0 or count == 0 is a successful no-op.  One kernel for the tensors of one pair of types whose sizes, strides and addresses
+ * let threads move 16 bytes at a time; those that take smaller accesses have one of their own.
  */
 typedef enum srft_dtype { SRFT_F32 = 0, SRFT_F16 = 1, SRFT_BF16 = 2 } srft_dtype;
 typedef enum srft_rotary_layout { SRFT_ROTARY_HALF = 0, SRFT_ROTARY_PAIRS = 1 } srft_rotary_layout;

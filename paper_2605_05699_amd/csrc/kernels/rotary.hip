@@ -148,7 +148,7 @@ extern "C" int srft_rotary(const srft_rotary_rows* rows, int count, int64_t n_to
         return SRFT_ERR_BAD_N;
     if (count > 0 && !rows) return SRFT_ERR_NULL;
     for (int i = 0; i < count; ++i)
-        if (rows[i].n_heads < 1 || n_tokens * rows[i].n_heads >= (1LL << 31) || !type_known(rows[i].in_type) || !type_known(rows[i].out_type) ||
+        if (rows[i].n_heads < 1 || n_tokens * rows[i].n_heads >= (1LL << 31) || (int64_t)rows[i].n_heads * d >= (1LL << 31) || !type_known(rows[i].in_type) || !type_known(rows[i].out_type) ||
             rows[i].reserved != 0)
             return SRFT_ERR_BAD_N;
     if (count == 0 || n_tokens == 0) return SRFT_OK;

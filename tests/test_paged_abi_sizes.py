@@ -14,3 +14,8 @@ def test_rotary_in_place_takes_one_type_and_one_layout(L):
     here = 1 << 20
     for other in (dict(out_type=2), dict(in_type=0, out_type=1), dict(out_token=256), dict(out_head=72), dict(in_token=0), dict(in_head=0)):
         assert rotary(L, out_dev=here, **other) == -7, other
+
+
+def test_rotary_rows_of_a_token_are_counted_with_32_bits(L):
+    for over in (dict(n_heads=1 << 25), dict(n_heads=1 << 21, d=1024, rot=1024), dict(n_heads=(1 << 30) - 1, d=2, rot=2, tokens=3)):
+        assert rotary(L, **dict(dict(tokens=1), **over)) == -7, over
