@@ -525,6 +525,8 @@ class PagedSeqs:
         n = lengths.shape[0]
         if page_table.dim() != 2 or page_table.shape[0] != n or windows.shape != (n, 2) or starts.shape != (n + 1,):
             raise ValueError("page_table must be [n, max_pages], windows [n, 2], lengths [n], starts [n + 1]")
+        if not 0 <= max_new < 1 << 31 or not 0 <= max_length < 1 << 63:              # (ctypes would keep the low bits)
+            raise ValueError("max_new and max_length must fit int32_t and int64_t and not be negative")
         self.n_seq, self.max_new, self.max_length = n, max_new, max_length
         self.page_table, self.windows, self.lengths, self.starts = page_table, windows, lengths, starts
         self.struct = _PagedSeqs(n, max_new, max_length, page_table.shape[1], _dev_ptr(page_table, torch.int32, "page_table"),
