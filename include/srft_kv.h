@@ -359,6 +359,8 @@ typedef struct srft_paged_seqs {
  * bit), the tokens behind them are copied into the window.  The result does not depend on how the tokens are split into calls.
  *   k_f16_dev, v_f16_dev   [n_new][n_heads][d] fp16, 16-byte aligned, strides in elements, multiples of 8.
  *   workspace_dev          srft_pool_append_workspace_bytes bytes, 16-byte aligned, overwritten.
+ * The tokens must be finite.  Sizes are counted with 32 bits (else SRFT_ERR_BAD_N): with F = n_new / R + min(n_seq, n_new), the pages that a call can
+ * fill at most, and T = n_heads * R / 32, n_new * n_heads, 32 F T and F T^2 stay below 2^31.
  */
 int64_t srft_pool_append_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, int64_t n_new);
 int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const void* k_f16_dev, const void* v_f16_dev,
@@ -369,10 +371,16 @@ int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const
  * Attention of the new tokens over the cache that holds them: out = softmax(softmax_scale * q K^T) V, causal (the i-th of the n new
  * tokens of a sequence of length L sees the tokens 0 .. L - n + i), query head h reading key head h / (n_q_heads / n_heads).  K and V
  * are the read path's reconstruction before its fp16 rounding where a page is full, and the window's fp16 values behind it.  A row that
- * sees nothing is zero.
+ * sees nothing is zero.  q, and the windows' tokens, must be finite.
+ * Sums, maxima and scores' sums are fp32.  Sequences that bring up to 16 rows (new tokens times n_q_heads / n_heads), or 32 where max_new allows 17
+ * to 32, round a weight times a scale to fp16: with the output's rounding to fp16, 3e-4 of an output's size.  Those that bring more also round the
+ * transformed queries, scales, and code times scale: 1.2e-3, up to 1.5e-3 with one scale a row.
  *   q_dev, out_dev   [n_new][n_q_heads][d], both of `type` (SRFT_F16 or SRFT_BF16), 16-byte aligned, strides in elements, multiples of 8.
  *   n_q_heads        a multiple of n_heads, at most 64 n_heads.
  *   softmax_scale    finite.
+ * Sizes are counted with 32 bits (else SRFT_ERR_BAD_N): with G = n_q_heads / n_heads, tiles = max_length / 32 + 2, S = n_seq * n_heads and blocks =
+ * min(max_new, n_new) * G / 256 rounded up, 2 S tiles, (n_new * G / 256 + n_seq) * n_heads * tiles and 8 S blocks stay below 2^31 - 256,
+ * n_new * n_q_heads below 2^31 - 32 and (S * R / 16 + 3 compute units + 1) * 2 d below 2^32.
  *   workspace_dev    srft_pool_attention_workspace_bytes bytes, 256-byte aligned, overwritten.  (Whatever srft_plan_set_max_workgroups is
  *                    called with before or after: the size does not depend on it.)
  */
@@ -406,7 +414,8 @@ int srft_plan_get_signs(const srft_plan_t* plan, int8_t* out_host /* d entries, 
  * Launch shape: both kernels are persistent (a fixed grid loops over tiles of 32 vectors).
  * max_workgroups > 0 caps the grid of this plan's launches (to leave compute units to other streams, or to
  * check that results do not depend on the grid); 0 restores the default (compute units x resident workgroups
- * per unit).  Results are bit-identical for every grid size.  The library reads no environment variables.
+ * per unit).  Records and reconstructions are bit-identical for every grid size.  (srft_pool_attention takes the cap of plan_k and, with
+ * another grid, adds the sums of a row up in other parts: within the roundings named there.)  The library reads no environment variables.
  */
 int srft_plan_set_max_workgroups(srft_plan_t* plan, int max_workgroups);
 

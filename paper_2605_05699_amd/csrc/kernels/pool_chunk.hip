@@ -1,11 +1,13 @@
 // Attention over a pool for many rows a key head (a chunk of a prompt): 256 rows (tokens x query heads of the group) a workgroup.
 //
-// 2048 new tokens behind 14,336, 32 query heads on 8 key heads, d = 128, 4 bits: 607 us, 0.85 PFLOP/s of the two products.  The same loop
-// without softmax, decoding and reads of LDS takes 370 (the rate of a large library product, 1.4 PFLOP/s, at the power limit);
-// without the decoding alone 559, without the softmax alone 523; on zeros, the same instructions with nothing toggling, 500.  So it is the
-// energy of its instructions that bounds it, matrix and vector ones alike: priorities (s_setprio) for either half of the wavefronts, decoding before
-// the products in one half and behind them in the other, a softmax spread between the matrix instructions of the values, and rows of
-// LDS without bank conflicts at the writes change nothing.
+// 2048 new tokens behind 14,336, 32 query heads on 8 key heads, d = 128, 4 bits: 584 to 590 us the call in a row of calls, 38 of them the
+// transform and the merge; in the profiler, which lets no launches overlap, the scan has 612 to 678.  The two products alone, the same loop
+// without softmax, decoding and reads of LDS, took 370 (the rate of a large library product, 1.4 PFLOP/s, at the power limit).  What bounds it is that
+// matrix and vector instructions hardly overlap: of a SIMD's 1.11 M clocks the matrix unit is busy for 0.49 M and the vector ALU for 0.60 M,
+// 98 % together.  The energy of data that toggle comes on top: on zeros, the same instructions, the scan takes 500 to 513 us.
+// Tried on that without a gain: priorities (s_setprio) for either half of the wavefronts, decoding before the products in one half and
+// behind them in the other, a softmax spread between the matrix instructions of the values, and rows of LDS without bank conflicts at
+// the writes.  Each of these left the order within a wavefront to the fences (sched_barrier) around the matrix instructions.
 //
 // A tile of keys is
 // decoded once for all the workgroup's rows, by all its wavefronts, into LDS (two buffers: the next tile is decoded while this one is

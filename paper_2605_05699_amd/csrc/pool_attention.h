@@ -13,8 +13,8 @@
 // Roundings to 16 bits.  pool_decode, which memory bounds: codes go to the matrix cores as they are (exact in fp16) against q' as fp16
 // hi + lo, scales on the results in fp32; a weight times the scale of its key and group is rounded to fp16 once.  pool_chunk, which the matrix
 // cores bound, has one matrix instruction where that would take two: q', the dequantized w (code * scale, the scale rounded first) and
-// the weights p are fp16, half a step (2^-11) each at most.  Against 64 bits that is 3e-4 and 1.2e-3 of an output's size, the output's own
-// rounding to fp16 included.  Sums, maxima and exponents are fp32.  None of the operands can leave fp16's range: q' has a power of two per
+// the weights p are fp16, half a step (2^-11) each at most.  Against 64 bits that is 3e-4 and 1.2e-3 of an output's size (1.5e-3 where one scale
+// serves a whole row), the output's own rounding to fp16 included.  Sums, maxima and exponents are fp32.  None of the operands can leave fp16's range: q' has a power of two per
 // row, w a running one taken from the scales, the weights are at most 2^(kLazy + kHigh) in pool_chunk, and times a scale 2^(kLazy + 7) in pool_decode.
 //
 // Order of channels.  A dword of codes is decoded into eight fp16 values in the order 0 4 1 5 2 6 3 7 (4 bits; 0 2 1 3 at 8 bits), so

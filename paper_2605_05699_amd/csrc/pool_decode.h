@@ -1,14 +1,15 @@
 // pool_decode.h -- attention over a pool for few rows a key head (a decode step: the query heads of a group; a few speculated
 // tokens of them): the scan over the keys, and the merge of what its workgroups leave.
 //
-// Bound by the records' bytes where there are enough of them, with the vector instructions that decode them close behind: 24 sequences up
-// to 32,768 tokens, 8 key heads of 128 channels, 4 bits: 388 MB in 110 us, 3.5 TB/s (a sum over 2 GiB reads 4.0 here; the vector ALU is busy 60 %
-// of the time).  Codes are loaded past the L2, where nobody reads them again: 6 % slower without that.  A wavefront has
+// Bound by the chain of a tile in a wavefront, its loads, decoding and products one after the other: 24 sequences up to 32,768 tokens, 8 key heads
+// of 128 channels, 4 bits: 388 MB in 110 us, 3.5 TB/s, where a kernel that only reads gets 6.2 to 6.5 (62 us).  The vector ALU is busy for half of a
+// SIMD's clocks (60 % of a wavefront's life), the matrix unit for 14 %; neither they nor the bytes bind alone, and two wavefronts a SIMD, which
+// is what the registers leave, do not cover each other's waits.  Codes are loaded past the L2, where nobody reads them again: 6 % slower without that.  A wavefront has
 // a tile of KEYS keys to itself, keys on the rows of the score product and 16 query rows on its columns (16x16x32; CB blocks of
 // them): a lane holds, for ITS row (lane % 16), the keys of its quarter of the wavefront (lane / 16), which is what the running maximum
 // and sum want and what the product with the values takes as its B operand.  Scores and weights stay in registers.
 //   scores: one group of 32 channels a step, the codes (exact in fp16) against q' as fp16 hi + lo, and the group's scale on the result in
-//           fp32: no rounding but fp32's.
+//           fp32: no rounding but fp32's, of sums that start up to 1152 times the queries' sum away from the result (see OFFSET).
 //   values: the codes go through the wavefront's LDS to be read transposed; a weight times the scale of the key and group, under a running power
 //           of two, is rounded to fp16 once.
 // Loads are straight-line, one tile ahead; a tile's pages are found by 16-key blocks (a page holds at least 16 tokens), their
@@ -138,7 +139,8 @@ struct pool_decode {
     }
     // Scores take the codes as 1024 + u (4 bits, low nibbles: u = code + 8; high ones: 1024 + 16 u; 8 bits: u = code + 128), which saves half of the
     // decoding: the queries' values that meet high nibbles are divided by 16, and what the offsets come to, a number per query and column
-    // of scales, is what the product starts from.  It costs 2^-24 of 1032 / 7 of the sum: 1e-5 of a score.
+    // of scales, is what the product starts from.  It costs a few roundings of 2^-24 of sums some 400 times a code's: 2.5e-5 of a score each.  (A
+    // decode step whose scores spread over 4 natural units is 3.1e-4 of its size off 64 bits with it, 2.9e-4 without.)
     static constexpr bool OFFSET = NS <= 4;                  // (four registers a column)
     static __device__ __forceinline__ half8 eight_up(uint32_t v) {
         const uint32_t w = v >> 8;
@@ -166,10 +168,14 @@ __device__ __forceinline__ uint32_t pool_product2(float a, float f, float b, flo
 }
 
 // Wavefronts per SIMD asked of the compiler.  Two fit (LDS, and 256 registers each).  Asked for one it fills the latencies with what registers there
-// are, and mostly ends below 256: us of the scan of 24 sequences up to 32,768 tokens, 8 rows a key head, asked for one / two: d = 64 73 / 78, d = 128
-// 109 / 121, 256 at 4 bits 209 / 247, 192 at 8 bits 201 / 227.  Where it ends above (one wavefront a SIMD), asking for two costs some spilled registers and
-// is faster up to 40 of them: at 8 bits d = 96 146 / 130, 128 189 / 160, 224 342 / 284, 256 389 / 326, 24 rows of d = 128 at 4 bits 261 / 187 (but at 8 bits,
-// with 69 spilled, 258 / 299).
+// are, and mostly ends at 256 or below, so that two fit all the same; that is the faster form then (d = 128 at 4 bits, 24 sequences up to
+// 32,768 tokens, 8 rows a key head, the whole call: 118 us, asked for two 131; d = 64 82 / 88, 256 207 / 238, 192 at 8 bits and g = 32 211 / 222).
+// Where it ends above, one wavefront is left, and asking for two is faster as long as that spills no more than some 40 registers.  Formats that
+// do, asked for one / two, groups of 16, 32 and d: 8 bits, d = 96 201 / 156, 151 / 140, 151 / 141; d = 128 254 / 194, 195 / 169, 196 / 170;
+// d = 192 with one group 260 / 222; d = 224 417 / 328, 334 / 279, 321 / 276; d = 256 472 / 381, 370 / 310, 358 / 309; 4 bits, d = 224 with one group
+// 292 / 228.  With two blocks of rows (24 rows a key head): 8 bits, d = 64 in groups of 16 221 / 152, d = 96 291 / 211, 232 / 172, 232 / 174; 4 bits, d = 96
+// in groups of 16 283 / 196, with one 237 / 161, d = 128 in groups of 32 265 / 194, with one 265 / 210.  Beyond 40: d = 128 at 4 bits in groups of 16
+// (87 spilled) 334 / 415, at 8 bits (69 to 120) 363 / 565, 271 / 314, 273 / 345.  (All formats: profiles/pool_decode_registers.txt.)
 constexpr int pool_decode_waves(int d, int bits, int cb, int gm) {
     if (bits == 8) return d == 96 || (cb == 1 && (d == 128 || d >= 224 || (d == 192 && gm == kGroupWide))) || (cb == 2 && d == 64 && gm == kGroup16) ? 2 : 1;
     if (cb == 2) return (d == 128 && gm != kGroup16) || (d == 96 && gm != kGroup32) ? 2 : 1;
