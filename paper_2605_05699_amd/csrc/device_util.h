@@ -188,6 +188,8 @@ __device__ __forceinline__ srft_work srft_work_of_block(const srft_batch<N>& a) 
 // q.  A nibble one position higher (bits 4..7 of the 16-bit half) gives 1024 + 16 u instead; times 1/16 minus 72 is q again
 // (exact), which saves the shift.  Selecting the nibble, flipping its bit and setting the exponent is one v_bitop3: nine
 // vector-ALU operations per dword (ten with the flip in front).
+// (For vector instructions only: a matrix instruction has to wait two states for an operand that a vector instruction writes, and the compiler
+// does not put them behind one that it does not see.)
 __device__ __forceinline__ uint32_t and_xor(uint32_t v, uint32_t mask, uint32_t bits) {
     uint32_t r;                                  // (v & mask) ^ bits as one instruction; `bits` is kept in a vector register
     asm("v_bitop3_b32 %0, %1, %2, %3 bitop3:0x6a" : "=v"(r) : "v"(v), "s"(mask), "v"(bits));

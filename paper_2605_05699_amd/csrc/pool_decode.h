@@ -142,14 +142,18 @@ struct pool_decode {
     // of scales, is what the product starts from.  It costs a few roundings of 2^-24 of sums some 400 times a code's: 2.5e-5 of a score each.  (A
     // decode step whose scores spread over 4 natural units is 3.1e-4 of its size off 64 bits with it, 2.9e-4 without.)
     static constexpr bool OFFSET = NS <= 4;                  // (four registers a column)
+    // What goes straight into a matrix instruction, these and pool_product2's, is written for the compiler: it has to wait two states between a vector
+    // instruction and a matrix instruction that reads its result, which it does not do behind inline asm.  (As asm, the scan for two blocks of
+    // rows at d = 32, 4 bits and groups of 16 had a weight written one state before its product, and gave wrong rows.)
+    static __device__ __forceinline__ uint32_t up(uint32_t v, uint32_t mask, uint32_t bits) { return __builtin_amdgcn_bitop3_b32(v, mask, bits, 0x6a); }       // (v & mask) ^ bits
     static __device__ __forceinline__ half8 eight_up(uint32_t v) {
         const uint32_t w = v >> 8;
-        return __builtin_bit_cast(half8, make_uint4(and_xor(v, 0x000F000Fu, 0x64086408u), and_xor(v, 0x00F000F0u, 0x64806480u),
-                                                    and_xor(w, 0x000F000Fu, 0x64086408u), and_xor(w, 0x00F000F0u, 0x64806480u)));
+        return __builtin_bit_cast(half8, make_uint4(up(v, 0x000F000Fu, 0x64086408u), up(v, 0x00F000F0u, 0x64806480u),
+                                                    up(w, 0x000F000Fu, 0x64086408u), up(w, 0x00F000F0u, 0x64806480u)));
     }
     static __device__ __forceinline__ half8 eight_up(uint2 c) {
-        return __builtin_bit_cast(half8, make_uint4(and_xor(c.x, 0x00FF00FFu, 0x64806480u), and_xor(c.x >> 8, 0x00FF00FFu, 0x64806480u),
-                                                    and_xor(c.y, 0x00FF00FFu, 0x64806480u), and_xor(c.y >> 8, 0x00FF00FFu, 0x64806480u)));
+        return __builtin_bit_cast(half8, make_uint4(up(c.x, 0x00FF00FFu, 0x64806480u), up(c.x >> 8, 0x00FF00FFu, 0x64806480u),
+                                                    up(c.y, 0x00FF00FFu, 0x64806480u), up(c.y >> 8, 0x00FF00FFu, 0x64806480u)));
     }
     static constexpr bool high(int e) { return BITS == 4 && e / 2 % 2; }
     static constexpr float offset(int e) { return BITS == 8 ? 1152.0f : high(e) ? 72.0f * 16.0f : 1032.0f; }      // of 1024 + u, in element e's units
@@ -161,10 +165,8 @@ template <int N> using pool_floats = float __attribute__((ext_vector_type(N), al
 
 // weight times scale, rounded once to fp16: two of them
 __device__ __forceinline__ uint32_t pool_product2(float a, float f, float b, float g) {
-    uint32_t r;
-    asm("v_fma_mixlo_f16 %0, %1, %2, 0" : "=v"(r) : "v"(a), "v"(f));
-    asm("v_fma_mixhi_f16 %0, %1, %2, 0" : "+v"(r) : "v"(b), "v"(g));
-    return r;
+    const half2v r = {(_Float16)__builtin_fmaf(a, f, 0.0f), (_Float16)__builtin_fmaf(b, g, 0.0f)};       // v_fma_mixlo_f16, v_fma_mixhi_f16
+    return __builtin_bit_cast(uint32_t, r);
 }
 
 // Wavefronts per SIMD asked of the compiler.  Two fit (LDS, and 256 registers each).  Asked for one it fills the latencies with what registers there
