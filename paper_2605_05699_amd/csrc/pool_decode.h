@@ -170,14 +170,14 @@ __device__ __forceinline__ uint32_t pool_product2(float a, float f, float b, flo
 }
 
 // Wavefronts per SIMD asked of the compiler.  Two fit (LDS, and 256 registers each).  Asked for one it fills the latencies with what registers there
-// are, and mostly ends at 256 or below, so that two fit all the same; that is the faster form then (d = 128 at 4 bits, 24 sequences up to
-// 32,768 tokens, 8 rows a key head, the whole call: 118 us, asked for two 131; d = 64 82 / 88, 256 207 / 238, 192 at 8 bits and g = 32 211 / 222).
-// Where it ends above, one wavefront is left, and asking for two is faster as long as that spills no more than some 40 registers.  Formats that
-// do, asked for one / two, groups of 16, 32 and d: 8 bits, d = 96 201 / 156, 151 / 140, 151 / 141; d = 128 254 / 194, 195 / 169, 196 / 170;
-// d = 192 with one group 260 / 222; d = 224 417 / 328, 334 / 279, 321 / 276; d = 256 472 / 381, 370 / 310, 358 / 309; 4 bits, d = 224 with one group
-// 292 / 228.  With two blocks of rows (24 rows a key head): 8 bits, d = 64 in groups of 16 221 / 152, d = 96 291 / 211, 232 / 172, 232 / 174; 4 bits, d = 96
-// in groups of 16 283 / 196, with one 237 / 161, d = 128 in groups of 32 265 / 194, with one 265 / 210.  Beyond 40: d = 128 at 4 bits in groups of 16
-// (87 spilled) 334 / 415, at 8 bits (69 to 120) 363 / 565, 271 / 314, 273 / 345.  (All formats: profiles/pool_decode_registers.txt.)
+// are, and mostly ends at 256 or below, so that two fit all the same; that is the faster form then (24 sequences up to 32,768 tokens, 8 rows a key
+// head, 4 bits, the whole call, asked for one / two, us: d = 64 82 / 88, 128 122 / 127, 256 212 / 238; 192 at 8 bits 212 / 222).  Where it ends
+// above, one wavefront is left, and asking for two is faster as long as that spills no more than some 40 registers.  Formats that do, groups of
+// 16, 32 and d: 8 bits, d = 96 199 / 155, 149 / 135, 149 / 136; d = 128 247 / 192, 192 / 168, 193 / 167; d = 192 with one group 259 / 218;
+// d = 224 419 / 328, 333 / 277, 321 / 276; d = 256 469 / 379, 371 / 310, 359 / 308; 4 bits, d = 224 with one group 294 / 228.  With two blocks
+// of rows (24 rows a key head): 8 bits, d = 64 in groups of 16 213 / 148, d = 96 287 / 211, 231 / 174, 232 / 175; 4 bits, d = 96 in groups of 16
+// 282 / 195, with one 238 / 161, d = 128 in groups of 32 263 / 192, with one 266 / 208.  Beyond 40: d = 128 at 4 bits in groups of 16 (87 spilled)
+// 331 / 406, at 8 bits (75 to 120) 361 / 567, 274 / 347, 270 / 336.  (All formats: profiles/pool_decode_registers.txt.)
 constexpr int pool_decode_waves(int d, int bits, int cb, int gm) {
     if (bits == 8) return d == 96 || (cb == 1 && (d == 128 || d >= 224 || (d == 192 && gm == kGroupWide))) || (cb == 2 && d == 64 && gm == kGroup16) ? 2 : 1;
     if (cb == 2) return (d == 128 && gm != kGroup16) || (d == 96 && gm != kGroup32) ? 2 : 1;
