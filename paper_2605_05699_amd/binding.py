@@ -472,12 +472,13 @@ class _RotaryRows(C.Structure):
 
 
 def _rows(t: torch.Tensor, name: str) -> tuple[int, int, int]:
-    """Address and strides of a tensor [tokens, heads, d] whose channels lie next to each other."""
+    """Address and strides of a tensor [tokens, heads, d] whose channels lie next to each other.  (Strides that lead nowhere are given as 0: of one token,
+    of one head, of nothing.)"""
     if not t.is_cuda:
         raise ValueError(f"{name} must live in device memory")
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1 and t.numel() > 0):
         raise ValueError(f"{name} must be [tokens, heads, d] with its channels next to each other")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return (t.data_ptr(), *(t.stride(i) if t.shape[i] > 1 and t.numel() > 0 else 0 for i in (0, 1)))
 
 
 def srft_rotary(items, positions: torch.Tensor, freq: torch.Tensor, layout: str = "half", factor: float = 1.0, inverse: bool = False,

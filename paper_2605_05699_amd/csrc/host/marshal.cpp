@@ -219,10 +219,12 @@ const at::Tensor* rows_of(PyObject* o) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
     return t.defined() && t.is_cuda() && t.layout() == at::kStrided && t.unsafeGetTensorImpl()->has_storage() && t.dim() == 3 &&
-                   (t.size(2) <= 1 || t.stride(2) == 1)
+                   (t.size(2) <= 1 || t.stride(2) == 1 || t.numel() == 0)
                ? &t
                : nullptr;
 }
+// the stride of its tokens (0) or heads (1); 0 where it leads nowhere
+int64_t step_of(const at::Tensor& t, int i) { return t.size(i) > 1 && t.numel() > 0 ? t.stride(i) : 0; }
 int type_of(const at::Tensor& t) {                           // srft_dtype, or -1
     return t.scalar_type() == at::kFloat ? SRFT_F32 : t.scalar_type() == at::kHalf ? SRFT_F16 : t.scalar_type() == at::kBFloat16 ? SRFT_BF16 : -1;
 }
@@ -247,8 +249,8 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (!x || !y || !x->sizes().equals(y->sizes()) || x->size(0) != tokens || type_of(*x) < 0 || type_of(*y) < 0) return false;
             if (i == 0) d = x->size(2);
             if (x->size(2) != d || d > INT32_MAX || x->size(1) > INT32_MAX) return false;
-            rows[i].in_dev = x->data_ptr(), rows[i].in_token = x->stride(0), rows[i].in_head = x->stride(1);
-            rows[i].out_dev = y->data_ptr(), rows[i].out_token = y->stride(0), rows[i].out_head = y->stride(1);
+            rows[i].in_dev = x->data_ptr(), rows[i].in_token = step_of(*x, 0), rows[i].in_head = step_of(*x, 1);
+            rows[i].out_dev = y->data_ptr(), rows[i].out_token = step_of(*y, 0), rows[i].out_head = step_of(*y, 1);
             rows[i].n_heads = (int32_t)x->size(1), rows[i].in_type = type_of(*x), rows[i].out_type = type_of(*y);
         }
         const long layout = PyLong_AsLong(a[3]);
@@ -276,7 +278,7 @@ PyObject* pool_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t tokens = k->size(0), need = g.pool_append_bytes(pool, seqs, tokens);
         if (need < 0 || bytes_of(*w) < need) return false;
         void *const kp = k->data_ptr(), *const vp = v->data_ptr(), *const wp = w->data_ptr(), *const st = current_stream();
-        const int64_t kt = k->stride(0), kh = k->stride(1), vt = v->stride(0), vh = v->stride(1);
+        const int64_t kt = step_of(*k, 0), kh = step_of(*k, 1), vt = step_of(*v, 0), vh = step_of(*v, 1);
         *rc = without_gil([&] { return g.pool_append(pool, seqs, kp, vp, tokens, kt, kh, vt, vh, wp, st); });
         return true;
     });
@@ -294,7 +296,7 @@ PyObject* pool_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t tokens = q->size(0), need = g.pool_attention_bytes(pool, seqs, tokens, (int)q->size(1));
         if (need < 0 || bytes_of(*w) < need) return false;
         void *const qp = q->data_ptr(), *const op = o->data_ptr(), *const wp = w->data_ptr(), *const st = current_stream();
-        const int64_t qt = q->stride(0), qh = q->stride(1), ot = o->stride(0), oh = o->stride(1);
+        const int64_t qt = step_of(*q, 0), qh = step_of(*q, 1), ot = step_of(*o, 0), oh = step_of(*o, 1);
         const int heads = (int)q->size(1), type = type_of(*q);
         const float scale = (float)PyFloat_AS_DOUBLE(a[4]);
         *rc = without_gil([&] { return g.pool_attention(pool, seqs, qp, type, tokens, heads, qt, qh, scale, op, ot, oh, wp, st); });
