@@ -9,7 +9,8 @@
 // them): a lane holds, for ITS row (lane % 16), the keys of its quarter of the wavefront (lane / 16), which is what the running maximum
 // and sum want and what the product with the values takes as its B operand.  Scores and weights stay in registers.
 //   scores: one group of 32 channels a step, the codes (exact in fp16) against q' as fp16 hi + lo, and the group's scale on the result in
-//           fp32: no rounding but fp32's, of sums that start up to 1152 times the queries' sum away from the result (see OFFSET).
+//           fp32: no rounding but fp32's.  (The codes themselves, not the 1024 + code that half of the decoding gives: what the offsets add up to
+//           is a thousand times the queries' sum, in whose last bits a group is lost whose large queries meet small codes.)
 //   values: the codes go through the wavefront's LDS to be read transposed; a weight times the scale of the key and group, under a running power
 //           of two, is rounded to fp16 once.
 // Loads are straight-line, one tile ahead; a tile's pages are found by 16-key blocks (a page holds at least 16 tokens), their
@@ -137,33 +138,16 @@ struct pool_decode {
         const uint2 x = decode4_bytes(c.x), y = decode4_bytes(c.y);
         return __builtin_bit_cast(half8, make_uint4(x.x, x.y, y.x, y.y));
     }
-    // Scores take the codes as 1024 + u (4 bits, low nibbles: u = code + 8; high ones: 1024 + 16 u; 8 bits: u = code + 128), which saves half of the
-    // decoding: the queries' values that meet high nibbles are divided by 16, and what the offsets come to, a number per query and column
-    // of scales, is what the product starts from.  It costs a few roundings of 2^-24 of sums some 400 times a code's: 2.5e-5 of a score each.  (A
-    // decode step whose scores spread over 4 natural units is 3.1e-4 of its size off 64 bits with it, 2.9e-4 without.)
-    static constexpr bool OFFSET = NS <= 4;                  // (four registers a column)
-    // What goes straight into a matrix instruction, these and pool_product2's, is written for the compiler: it has to wait two states between a vector
-    // instruction and a matrix instruction that reads its result, which it does not do behind inline asm.  (As asm, the scan for two blocks of
-    // rows at d = 32, 4 bits and groups of 16 had a weight written one state before its product, and gave wrong rows.)
-    static __device__ __forceinline__ uint32_t up(uint32_t v, uint32_t mask, uint32_t bits) { return __builtin_amdgcn_bitop3_b32(v, mask, bits, 0x6a); }       // (v & mask) ^ bits
-    static __device__ __forceinline__ half8 eight_up(uint32_t v) {
-        const uint32_t w = v >> 8;
-        return __builtin_bit_cast(half8, make_uint4(up(v, 0x000F000Fu, 0x64086408u), up(v, 0x00F000F0u, 0x64806480u),
-                                                    up(w, 0x000F000Fu, 0x64086408u), up(w, 0x00F000F0u, 0x64806480u)));
-    }
-    static __device__ __forceinline__ half8 eight_up(uint2 c) {
-        return __builtin_bit_cast(half8, make_uint4(up(c.x, 0x00FF00FFu, 0x64806480u), up(c.x >> 8, 0x00FF00FFu, 0x64806480u),
-                                                    up(c.y, 0x00FF00FFu, 0x64806480u), up(c.y >> 8, 0x00FF00FFu, 0x64806480u)));
-    }
-    static constexpr bool high(int e) { return BITS == 4 && e / 2 % 2; }
-    static constexpr float offset(int e) { return BITS == 8 ? 1152.0f : high(e) ? 72.0f * 16.0f : 1032.0f; }      // of 1024 + u, in element e's units
     // which of a quarter's eight keys of a step is element e of an operand of decoded codes
     static constexpr int key_of(int e) { return BITS == 4 ? e / 2 + 4 * (e % 2) : (e & 4) + ((e & 1) << 1) + ((e & 2) >> 1); }
 };
 
 template <int N> using pool_floats = float __attribute__((ext_vector_type(N), aligned(4)));     // (native vectors: arrays of classes end up in memory)
 
-// weight times scale, rounded once to fp16: two of them
+// weight times scale, rounded once to fp16: two of them.  They go straight into a matrix instruction and are therefore written for the compiler: it
+// has to wait two states between a vector instruction and a matrix instruction that reads its result, which it does not do behind inline
+// asm.  (As asm, the scan for two blocks of rows at d = 32, 4 bits and groups of 16 had a weight written one state before its product, and gave
+// wrong rows.)
 __device__ __forceinline__ uint32_t pool_product2(float a, float f, float b, float g) {
     const half2v r = {(_Float16)__builtin_fmaf(a, f, 0.0f), (_Float16)__builtin_fmaf(b, g, 0.0f)};       // v_fma_mixlo_f16, v_fma_mixhi_f16
     return __builtin_bit_cast(uint32_t, r);
@@ -171,23 +155,21 @@ __device__ __forceinline__ uint32_t pool_product2(float a, float f, float b, flo
 
 // Wavefronts per SIMD asked of the compiler.  Two fit (LDS, and 256 registers each).  Asked for one it fills the latencies with what registers there
 // are, and mostly ends at 256 or below, so that two fit all the same; that is the faster form then (24 sequences up to 32,768 tokens, 8 rows a key
-// head, 4 bits, the whole call, asked for one / two, us: d = 64 82 / 88, 128 122 / 127, 256 212 / 238; 192 at 8 bits 212 / 222).  Where it ends
+// head, 4 bits, the whole call, asked for one / two, us: d = 64 84 / 89, 128 123 / 132, 256 212 / 237; 192 at 8 bits 215 / 221).  Where it ends
 // above, one wavefront is left, and asking for two is faster as long as that spills no more than some 40 registers.  Formats that do, groups of
-// 16, 32 and d: 8 bits, d = 96 199 / 155, 149 / 135, 149 / 136; d = 128 247 / 192, 192 / 168, 193 / 167; d = 192 with one group 259 / 218;
-// d = 224 419 / 328, 333 / 277, 321 / 276; d = 256 469 / 379, 371 / 310, 359 / 308; 4 bits, d = 224 with one group 294 / 228.  With two blocks
-// of rows (24 rows a key head): 8 bits, d = 64 in groups of 16 213 / 148, d = 96 287 / 211, 231 / 174, 232 / 175; 4 bits, d = 96 in groups of 16
-// 282 / 195, with one 238 / 161, d = 128 in groups of 32 263 / 192, with one 266 / 208.  Beyond 40: d = 128 at 4 bits in groups of 16 (87 spilled)
-// 331 / 406, at 8 bits (75 to 120) 361 / 567, 274 / 347, 270 / 336.  (All formats: profiles/pool_decode_registers.txt.)
+// 16, 32 and d: 8 bits, d = 96 in groups of 16 199 / 156; d = 128 248 / 193, 183 / 161, 180 / 159; d = 192 with one group 260 / 225;
+// d = 224 418 / 328, 335 / 278, 320 / 276; d = 256 472 / 380, 371 / 311, 359 / 309; 4 bits, d = 224 with one group 293 / 227.  With two blocks
+// of rows (24 rows a key head): 8 bits, d = 96 in groups of 16 289 / 211, d = 128 in groups of 32 280 / 211, with one 279 / 212; 4 bits, the same three
+// 282 / 196, 274 / 187, 275 / 187.  Beyond 40: d = 128 in groups of 16, two blocks, at 4 bits (87 spilled) 332 / 414, at 8 (120) 361 / 566.
+// (All formats: profiles/pool_decode_registers.txt.)
 constexpr int pool_decode_waves(int d, int bits, int cb, int gm) {
-    if (bits == 8) return d == 96 || (cb == 1 && (d == 128 || d >= 224 || (d == 192 && gm == kGroupWide))) || (cb == 2 && d == 64 && gm == kGroup16) ? 2 : 1;
-    if (cb == 2) return (d == 128 && gm != kGroup16) || (d == 96 && gm != kGroup32) ? 2 : 1;
-    return d == 224 && gm == kGroupWide ? 2 : 1;
+    if (cb == 2) return d == (gm == kGroup16 ? 96 : 128) ? 2 : 1;
+    if (bits == 4) return d == 224 && gm == kGroupWide ? 2 : 1;
+    return d == 128 || d >= 224 || (d == 96 && gm == kGroup16) || (d == 192 && gm == kGroupWide) ? 2 : 1;
 }
-// Whether a segment's first tile is asked for before its queries are in LDS: 115 us -> 109 at d = 128, 142 -> 135 at 160; where the registers are full
-// (256: 209 -> 291) it is not.
-constexpr bool pool_decode_early(int d, int bits, int cb, int gm) {
-    return pool_decode_waves(d, bits, cb, gm) == 1 && d <= 160 && !(d == 128 && gm == kGroup16);
-}
+// Whether a segment's first tile is asked for before its queries are in LDS (4 bits, groups of 32, with / without: d = 64 84 / 85, 96 104 / 107,
+// 160 147 / 148).  Not where the registers are full: at d = 128 one wavefront is left with it (149 / 123), nor above 160 (256: 209 -> 291 when it was tried).
+constexpr bool pool_decode_early(int d, int bits, int cb, int gm) { return pool_decode_waves(d, bits, cb, gm) == 1 && d <= 160 && d != 128; }
 template <int D, int BITS, int CB, int GM>
 __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB, GM)) srft_pool_decode_kernel(const pool_attention_args a) {
     using P = pool_decode<D, BITS, CB, GM>;
@@ -342,42 +324,9 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
         for (int c = 0; c < CB; ++c)
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
-                if constexpr (P::OFFSET && BITS == 4) {
-                    const half2v sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
-                    x[c][i][1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, (uint32_t)x[c][i][1]) * sixteenth);
-                    x[c][i][3] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, (uint32_t)x[c][i][3]) * sixteenth);
-                }
                 qs[(c * G * 2 + min(wave + W * i, 2 * G - 1)) * 64 + lane] = __builtin_bit_cast(uint4, x[c][i]);     // (past the last, the last again)
             }
         __syncthreads();
-        floatx4 start[P::OFFSET ? CB : 1][P::OFFSET ? NS : 1];               // what the score product starts from
-        if constexpr (P::OFFSET) {
-#pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        const half8 x = __builtin_bit_cast(half8, qs[((c * G + j) * 2 + part) * 64 + lane]);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sum = fmaf((float)x[e], -P::offset(e), sum);
-                    }
-                    if constexpr (FINE) {                    // (quarters 0 and 1 are one group, 2 and 3 the other)
-                        const uint2 x = swap16(__float_as_uint(sum), __float_as_uint(sum));
-                        const float pair = __uint_as_float(x.x) + __uint_as_float(x.y);
-                        const uint2 y = swap32(__float_as_uint(pair), __float_as_uint(pair));
-                        const float f0 = __uint_as_float(y.x), f1 = __uint_as_float(y.y);
-                        start[c][2 * j] = floatx4{f0, f0, f0, f0};
-                        start[c][2 * j + 1 < NS ? 2 * j + 1 : 0] = floatx4{f1, f1, f1, f1};
-                    } else {
-                        sum = pool_quarters_sum(sum);
-                        start[c][j] = floatx4{sum, sum, sum, sum};
-                    }
-                }
-        } else {
-            start[0][0] = floatx4{0, 0, 0, 0};
-        }
         floatx4 acc[CB][NB];
         float top[CB], den[CB];
         int e_now = kPoolNoExponent;
@@ -475,7 +424,7 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
 #pragma unroll
                         for (int b = 0; b < BK; ++b) {
                             const unit_t codes = *reinterpret_cast<const unit_t*>(k_src + 4 * b * P::ROW + 4 * BITS * j);
-                            half8 k = P::OFFSET ? P::eight_up(codes) : P::eight(codes);
+                            half8 k = P::eight(codes);
                             if constexpr (FINE) {            // (the other group's half of the step: zeros)
                                 const uint4 z = make_uint4(0, 0, 0, 0);
                                 k = quarter >> 1 == half ? k : __builtin_bit_cast(half8, z);
@@ -484,7 +433,7 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
                             const float fv[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
                             for (int c = 0; c < CB; ++c) {
-                                floatx4 s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, __builtin_bit_cast(half8, qs[((c * G + j) * 2 + 0) * 64 + lane]), start[P::OFFSET ? c : 0][P::OFFSET ? column : 0], 0, 0, 0);
+                                floatx4 s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, __builtin_bit_cast(half8, qs[((c * G + j) * 2 + 0) * 64 + lane]), floatx4{0, 0, 0, 0}, 0, 0, 0);
                                 s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, __builtin_bit_cast(half8, qs[((c * G + j) * 2 + 1) * 64 + lane]), s, 0, 0, 0);
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) p[c][b][i] = column == 0 ? s[i] * fv[i] : fmaf(s[i], fv[i], p[c][b][i]);
@@ -578,14 +527,12 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
                         floatx4 s{0, 0, 0, 0};
 #pragma unroll
                         for (int j = 0; j < G; ++j) {
-                            half8 k = __builtin_bit_cast(half8, kr[j]);
-                            if constexpr (P::OFFSET && BITS == 4)            // (rows are below 2^15: as fp16 they cannot be multiplied by 16)
-                                k = k * half8{0.0625f, 0.0625f, 1.0f, 1.0f, 0.0625f, 0.0625f, 1.0f, 1.0f};
+                            const half8 k = __builtin_bit_cast(half8, kr[j]);
                             s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, __builtin_bit_cast(half8, qs[((c * G + j) * 2 + 0) * 64 + lane]), s, 0, 0, 0);
                             s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, __builtin_bit_cast(half8, qs[((c * G + j) * 2 + 1) * 64 + lane]), s, 0, 0, 0);
                         }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) p[c][b][i] = s[i] * (P::OFFSET && BITS == 4 ? 16.0f * fk[i] : fk[i]);
+                        for (int i = 0; i < 4; ++i) p[c][b][i] = s[i] * fk[i];
                     }
                 } else {                                     // (masked: keys behind the last)
 #pragma unroll

@@ -61,3 +61,28 @@ def test_many_small_weights_behind_a_dominant_one(B, d, bits, behind, rows):
     error = np.linalg.norm(got - want, axis=-1) / np.linalg.norm(want, axis=-1)
     assert error.max() <= tolerance, (float(error.max()), tolerance)
     s.close()
+
+
+@pytest.mark.parametrize("d,g,bits", [(128, 32, 4), (128, 32, 8), (64, 16, 4), (64, 32, 8), (32, 32, 4), (96, 96, 4), (256, 32, 4)])
+@pytest.mark.parametrize("new,group", [([1, 1], 8), ([3, 4], 8), ([60, 1], 2)])
+def test_channels_whose_codes_are_small_beside_large_queries(B, d, g, bits, new, group):
+    """Half of each group's channels have a lambda 2^12 times the others': these have small codes, mostly 0, and a transformed query 2^12 times as large.
+    What they add to a score is small, and what their sizes cost has to be too.  Some keys are a hundred times the others, so that an error that all
+    of a row's products share is none that cancels.  (As everywhere: three roundings of 2^-11 of each product, 32-bit sums.)"""
+    from tests.test_gpu_paged import check, queries
+    s = Serving(B, d, g, bits, 32, 2, n=2, max_length=400, seed=d + g, lam_spread=0.3)
+    s.pool.close()
+    for lam in s.lam:
+        lam[1::2] *= np.float32(2.0 ** -12)
+    s.plans = [B.Plan(d, g, d + g + i, s.lam[i], bits) for i in range(2)]
+    s.pool = B.PagePool(*s.plans, s.pool.k, s.pool.v)
+    for more, gain in (([200, 37], 0.01), ([20, 19], 1.0), ([60, 40], 0.01)):
+        s.append(more, gain)
+    s.append(new, 0.01)
+    q = queries(s, sum(new), group, F16)
+    scores = [np.abs(q[0, :group].double().cpu().numpy() @ s.inverse(0) @ s.values(0, 0)[:, 0].T).max(), 1e-30]
+    scale = float(np.float32(3.0 / max(scores)))
+    out = s.run(q, new, scale)
+    torch.cuda.synchronize()
+    check(s, q, new, scale, out, group)
+    s.close()
