@@ -2,8 +2,8 @@
 // tokens of them): the scan over the keys, and the merge of what its workgroups leave.
 //
 // Bound by the chain of a tile in a wavefront, its loads, decoding and products one after the other: 24 sequences up to 32,768 tokens, 8 key heads
-// of 128 channels, 4 bits: 388 MB in 110 us, 3.5 TB/s, where a kernel that only reads gets 6.2 to 6.5 (62 us).  The vector ALU is busy for half of a
-// SIMD's clocks (60 % of a wavefront's life), the matrix unit for 14 %; neither they nor the bytes bind alone, and two wavefronts a SIMD, which
+// of 128 channels, 4 bits: 388 MB in 112 us, 3.5 TB/s, where a kernel that only reads gets 6.2 to 6.5 (62 us).  The vector ALU is busy for 54 % of a
+// SIMD's clocks (66 % of a wavefront's life), the matrix unit for 14 %; neither they nor the bytes bind alone, and two wavefronts a SIMD, which
 // is what the registers leave, do not cover each other's waits.  Codes are loaded past the L2, where nobody reads them again: 6 % slower without that.  A wavefront has
 // a tile of KEYS keys to itself, keys on the rows of the score product and 16 query rows on its columns (16x16x32; CB blocks of
 // them): a lane holds, for ITS row (lane % 16), the keys of its quarter of the wavefront (lane / 16), which is what the running maximum

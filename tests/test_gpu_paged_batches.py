@@ -91,8 +91,8 @@ def test_long_sequences(B, new, group, d, bits, R):
 @pytest.mark.parametrize("d,g,bits,group", [(128, 32, 4, 8), (128, 32, 8, 16), (64, 16, 4, 8), (256, 32, 8, 4), (128, 32, 4, 24)])
 def test_scores_of_a_decode_step_are_exact_but_for_32_bits(B, d, g, bits, group):
     """Scores of four natural units' spread over 4000 tokens in pages.  What the scan rounds to fp16 is a weight times a scale, and the
-    output: 2^-11 of each at most, 2.0e-4 of the size in the root mean square (a uniform error over one binade's mantissas), together 2.9e-4.  The offsets that
-    scores start from cost some 1e-4 more at that spread (sums 400 times a code's, in 2^-24), together 3.1e-4.  Queries rounded to fp16,
+    output: 2^-11 of each at most, 2.0e-4 of the size in the root mean square (a uniform error over one binade's mantissas), together 2.9e-4.  32-bit
+    sums of scores add less than 1e-4 at that spread, together 3.1e-4.  Queries rounded to fp16,
     without what that leaves, would make it 6e-4, which the definition with that mistake shows."""
     tolerance = 4.5e-4
     s = Serving(B, d, g, bits, 16, 2, n=2, max_length=4000, seed=d + bits, lam_spread=0.2)
