@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import weakref
 
 import numpy as np
 import torch
@@ -541,7 +542,7 @@ class PagePool:
     scales [pages, heads, R, groups] float32, window [windows, heads, R, d] float16) each.  No pages: sequences shorter than one."""
 
     def __init__(self, plan_k: "Plan", plan_v: "Plan", k, v):
-        self.handle = None
+        self.handle, self.tables = None, []
         self.plans, self.k, self.v = (plan_k, plan_v), tuple(k), tuple(v)
         pages, heads, R, _ = self.k[0].shape
         windows, d = self.k[2].shape[0], plan_k.d
@@ -567,6 +568,8 @@ class PagePool:
 
     def close(self) -> None:
         if self.handle:
+            for table in filter(None, (ref() for ref in self.tables)):
+                table.handles[:] = [None if p is self else h for p, h in zip(table.pools, table.handles)]
             _check(lib().srft_pool_destroy(self.handle), "srft_pool_destroy")
             self.handle = None
 
@@ -578,12 +581,14 @@ class PagePool:
 
 
 class PoolTable:
-    """The pools of the layers of a model, for calls over all of them.  The pools are kept alive."""
+    """The pools of the layers of a model, for calls over all of them.  The pools are kept alive; with one of them closed, calls are refused."""
 
     def __init__(self, pools):
         self.pools = list(pools)
         self.handles = (C.c_void_p * len(self.pools))(*[int(p.handle) for p in self.pools])
         self.address = C.addressof(self.handles)
+        for p in self.pools:
+            p.tables = [ref for ref in p.tables if ref() is not None] + [weakref.ref(self)]
 
 
 def _sized(bytes_: int, where: str) -> int:
