@@ -378,9 +378,9 @@ int srft_pool_append(const srft_pool_t* pool, const srft_paged_seqs* seqs, const
  *   q_dev, out_dev   [n_new][n_q_heads][d], both of `type` (SRFT_F16 or SRFT_BF16), 16-byte aligned, strides in elements, multiples of 8.
  *   n_q_heads        a multiple of n_heads, at most 64 n_heads.
  *   softmax_scale    finite.
- * Sizes are counted with 32 bits (else SRFT_ERR_BAD_N): with G = n_q_heads / n_heads, tiles = max_length / 32 + 2, S = n_seq * n_heads and blocks =
- * min(max_new, n_new) * G / 256 rounded up, 2 S tiles, (n_new * G / 256 + n_seq) * n_heads * tiles and 8 S blocks stay below 2^31 - 256,
- * n_new * n_q_heads below 2^31 - 32 and (S * R / 16 + 3 compute units + 1) * 2 d below 2^32.
+ * Sizes are counted with 32 bits (else SRFT_ERR_BAD_N): with G = n_q_heads / n_heads, tiles = max_length / 32 + 2 and S = n_seq * n_heads,
+ * 2 S tiles and (n_new * G / 256 + n_seq) * n_heads * max(tiles, 8) stay below 2^31 - 256, n_new * n_q_heads below 2^31 - 32 and
+ * (S * R / 16 + 3 compute units + 1) * 2 d below 2^32.
  *   workspace_dev    srft_pool_attention_workspace_bytes bytes, 256-byte aligned, overwritten.  (Whatever srft_plan_set_max_workgroups is
  *                    called with before or after: the size does not depend on it.)
  */

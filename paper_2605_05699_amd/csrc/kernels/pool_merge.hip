@@ -1,7 +1,8 @@
 // Attention over a pool, the end: the sums of rows whose keys went to several workgroups are added in the order of the keys and
 // finished; rows of sequences without a tile are zero.  The first a.decode_merges workgroups take the rows of the scan for few rows
 // (pool_decode_merge), the others those of chunks, in one launch: apart, the first took 17 us beside the 29 of the others (d = 256).
-// Chunks: one workgroup of four wavefronts per 32 rows of a key head, each with every fourth
+// Chunks: one workgroup of four wavefronts per 32 rows of a key head, of the blocks of 256 rows that there are (by the longest sequence for each, 255 decode steps beside a
+// prompt of 4096 tokens, 64 query heads, were a million workgroups, nearly all of them empty: 1376 us, now 36), each with every fourth
 // run of 32 positions of the sums and then of the outputs (one wavefront per 32 rows read every part, and the matrix, one after
 // the other: 104 us at d = 256, 28 at d = 128).  Bound by the chain of loads where parts are few (a first round for the maxima alone: 6.9 us,
 // now 5.5, for a step of 4 sequences), by the parts' bytes where they are many (23 us for 67 MB at d = 128; more of them in flight is slower).  Rows that their scan has finished have nothing to do here.
@@ -14,11 +15,12 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     constexpr int BLOCKS = kPoolChunkWaves, ROWS = kPoolBlock * BLOCKS, KEYS = kPoolChunkKeys<D>, G = D / 32, T = D / 16, OWN = (G + kPoolTeam - 1) / kPoolTeam, AHEAD = 2;
     // ops: [k-step][hi, lo][lane]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int of = (int)(workgroup / (unsigned)a.merge_blocks), at = (int)workgroup - of * a.merge_blocks;
-    const int seq = of / a.heads, head = of - seq * a.heads, rt = at / BLOCKS, block = at - rt * BLOCKS;
+    const int of = (int)(workgroup / BLOCKS), block = (int)workgroup - of * BLOCKS, at = of / a.heads, head = of - at * a.heads;
+    if (at >= a.blocks_before[a.s.n_seq]) return;
+    const int seq = a.s.n_seq == 1 ? 0 : __builtin_amdgcn_readfirstlane(pool_sequence_of(a.blocks_before, a.s.n_seq, at)), rt = at - a.blocks_before[seq];
     const pool_seq q = pool_seq_of(a.s, seq);
     const int r0 = rt * ROWS + block * kPoolBlock;
-    if (q.n_new == 0 || pool_is_decode(q, a.group, a.decode_rows) || r0 >= q.n_new * a.group) return;
+    if (r0 >= q.n_new * a.group) return;
     const int tiles = pool_tiles(pool_seen(q, a.group, ROWS, rt), q.full, KEYS);
     const pool_row row = pool_row_of(q, head, a.group, r0 + (lane & 31));
     char* const dst = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;

@@ -27,13 +27,14 @@ __device__ __forceinline__ void count_units(const pool_attention_args& a) {
         const bool decode = pool_is_decode(q, a.group, a.decode_rows);
         const int chunk = decode || q.n_new == 0 ? 0 : a.heads * pool_chunk_units(q, a.group, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS);
         if (lane == 0) {
+            if (a.blocks_before) a.blocks_before[b + 1] = decode ? 0 : (q.n_new * a.group + ROWS - 1) / ROWS;
             a.decode_before[b + 1] = decode ? a.heads * ((q.n_new * a.group + a.decode_block - 1) / a.decode_block) * pool_tiles(q.length, q.full, a.decode_keys) : 0;
             a.chunk_before[b + 1] = chunk;
         }
     }
     __syncthreads();
-    for (int which = wave; which < 2; which += NT / 64) {
-        int* const at = which == 0 ? a.decode_before : a.chunk_before;
+    for (int which = wave; which < (a.blocks_before ? 3 : 2); which += NT / 64) {
+        int* const at = which == 0 ? a.decode_before : which == 1 ? a.chunk_before : a.blocks_before;
         unsigned sum = 0;
         if (lane == 0) at[0] = 0;
         for (int b0 = 1; b0 <= s.n_seq; b0 += 64) {

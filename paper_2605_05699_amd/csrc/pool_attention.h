@@ -53,6 +53,7 @@ struct pool_attention_args {
     int q_tiles, q_grid;                                     // passes of query rows in pool_rotate, workgroups that take them
     // workspace
     int *decode_before, *chunk_before;                       // [n_seq + 1]: units of work in front of a sequence
+    int* blocks_before;                                      // [n_seq + 1]: blocks of 256 rows of pool_chunk's in front of a sequence (null where there are none)
     unsigned short *q_rows, *q_rows_low;                     // [n_new][n_q_heads][D] fp16: q', and what its rounding leaves
     float* q_factor;                                         // [n_new][n_q_heads]: exponent * what q_rows are to be multiplied with
     unsigned short* tail_rows;                               // [K, V][n_seq][heads][R][D] fp16
@@ -61,8 +62,8 @@ struct pool_attention_args {
     float *decode_parts, *chunk_parts;                       // sums of segments (pool_part)
     int decode_grid, chunk_grid;
     int decode_rows, decode_block, decode_keys;              // rows that go to pool_decode, those of a workgroup, keys of its tiles
-    int merge_blocks, decode_merges;                         // of 32 rows, of a sequence and key head; workgroups that merge what pool_decode left
-    unsigned merges;                                         // workgroups of pool_merge (srft_grid)
+    int decode_merges;                                       // workgroups of pool_merge that merge what pool_decode left
+    unsigned merges;                                         // all of them (srft_grid)
 };
 // Sums of a block of 32 rows that a segment leaves: [D / 8 float4][64 lanes], then per lane maximum, sum of weights and V's exponent.
 template <int D> constexpr int kPoolPart = 32 * D + 3 * 64;

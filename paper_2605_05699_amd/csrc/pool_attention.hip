@@ -8,7 +8,7 @@ namespace {
 
 // Where each part of the workspace begins, and the grids that parts of it are counted by.
 struct workspace {
-    int64_t decode_before, chunk_before, q_rows, q_rows_low, q_factor, tail_rows, tail_factor, tail_columns, decode_parts, chunk_parts, bytes;
+    int64_t decode_before, chunk_before, blocks_before, q_rows, q_rows_low, q_factor, tail_rows, tail_factor, tail_columns, decode_parts, chunk_parts, bytes;
     int decode_grid, chunk_grid;
 };
 // Workgroups of a launch.  A cap on them (srft_plan_set_max_workgroups) may change between the call that sizes a workspace and the one that
@@ -17,8 +17,11 @@ int workgroups(const srft_pool* p, int per_unit) {
     const int all = p->plan_k->compute_units * per_unit;
     return p->plan_k->max_wgs > 0 ? std::min(p->plan_k->max_wgs, all) : all;
 }
-int64_t row_blocks(const srft_paged_seqs* s, int64_t n_new, int group, int rows) {           // of one sequence and key head, at most
-    return (std::min<int64_t>(s->max_new, n_new) * group + rows - 1) / rows;
+constexpr int kChunkRows = kPoolBlock * kPoolChunkWaves;
+// blocks of kChunkRows rows of all sequences, at most, where those with fewer than `least` rows count for none
+int64_t row_blocks(const srft_paged_seqs* s, int64_t n_new, int group, int least) {
+    const int64_t rows = n_new * group;
+    return rows / kChunkRows + std::min<int64_t>(s->n_seq, rows / least);
 }
 // Sequences that bring few rows a key head go to pool_decode, cb blocks of 16 of them a workgroup, the others to pool_chunk.  Two blocks where
 // a sequence may bring 17 to 32 rows and none brings more, up to d = 128 (beyond it two blocks' sums do not fit the registers: there a
@@ -49,6 +52,7 @@ workspace layout(const srft_pool* p, const srft_paged_seqs* s, int64_t n_new, in
     w.chunk_grid = workgroups(p, 1);
     w.decode_before = take(4LL * (s->n_seq + 1));
     w.chunk_before = take(4LL * (s->n_seq + 1));
+    w.blocks_before = take(4LL * (s->n_seq + 1));
     w.q_rows = take(2 * rows * d);
     w.q_rows_low = take(2 * rows * d);
     w.q_factor = take(4 * rows);
@@ -70,10 +74,10 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, int64_t n_new, int
     if (rc != SRFT_OK) return rc;
     if (q_heads < 1 || q_heads % pool->heads != 0 || q_heads > 64 * pool->heads || n_new * q_heads >= (1LL << 31) - 32) return SRFT_ERR_BAD_N;
     // units of work (kPoolMostUnits), tiles and workgroups are counted with 32 bits
-    const int d = pool->plan_k->d, group = q_heads / pool->heads, rows = kPoolBlock * kPoolChunkWaves;
+    const int d = pool->plan_k->d, group = q_heads / pool->heads;
     const int64_t most = kPoolMostUnits, tiles = seqs->max_length / 32 + 2, heads = (int64_t)seqs->n_seq * pool->heads;
-    const int64_t blocks = row_blocks(seqs, n_new, group, rows), all_blocks = n_new * group / rows + seqs->n_seq;
-    if (2 * heads * tiles >= most || all_blocks * pool->heads * tiles >= most || heads * std::max<int64_t>(blocks, 1) * kPoolChunkWaves >= most ||
+    const int64_t blocks = n_new * group / kChunkRows + seqs->n_seq;
+    if (2 * heads * tiles >= most || blocks * pool->heads * std::max<int64_t>(tiles, kPoolChunkWaves) >= most ||
         (heads * pool->R / kTileVecs * 2 + pool->plan_k->compute_units * 3 + 1) * 2 * d > UINT32_MAX)        // (threads of pool_rotate)
         return SRFT_ERR_BAD_N;
     return SRFT_OK;
@@ -166,6 +170,7 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     const srft_plan *pk = pool->plan_k, *pv = pool->plan_v;
     const int d = pk->d, group = n_q_heads / pool->heads;
     const workspace w = layout(pool, seqs, n_new, n_q_heads);
+    const split sp = split_of(seqs, n_new, group, d);
     char* const base = (char*)workspace_dev;
     pool_attention_args a;
     a.s = pool_seqs_of(pool, seqs, n_new);
@@ -196,6 +201,7 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     a.q_grid = std::min(a.q_tiles, workgroups(pool, d <= 128 ? 3 : 1));
     a.decode_before = (int*)(base + w.decode_before);
     a.chunk_before = (int*)(base + w.chunk_before);
+    a.blocks_before = sp.chunk ? (int*)(base + w.blocks_before) : nullptr;
     a.q_rows = (unsigned short*)(base + w.q_rows);
     a.q_factor = (float*)(base + w.q_factor);
     a.tail_rows = (unsigned short*)(base + w.tail_rows);
@@ -203,7 +209,6 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     a.tail_columns = (unsigned short*)(base + w.tail_columns);
     a.decode_parts = (float*)(base + w.decode_parts);
     a.chunk_parts = (float*)(base + w.chunk_parts);
-    const split sp = split_of(seqs, n_new, group, d);
     a.q_rows_low = sp.decode ? (unsigned short*)(base + w.q_rows_low) : nullptr;     // (chunks do not read them)
     a.decode_grid = w.decode_grid;
     a.decode_rows = sp.decode ? sp.rows : 0;                 // (0: the one sequence there is goes to pool_chunk, however few tokens it brings)
@@ -215,9 +220,8 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
     rc = srft_launch(srft_pick_pool_rotate(d, pk->bits), dim3((unsigned)(1 + a.q_grid + tail_tiles)), 2 * d, st, a);
     if (rc == SRFT_OK && sp.chunk) rc = srft_launch(srft_pick_pool_chunk(d, pk->bits), dim3((unsigned)a.chunk_grid), 64 * kPoolChunkWaves, st, a);
     if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb), dim3((unsigned)a.decode_grid), 64 * kPoolTeam, st, a);
-    a.merge_blocks = (int)row_blocks(seqs, n_new, group, kPoolBlock * kPoolChunkWaves) * kPoolChunkWaves;
     a.decode_merges = sp.decode ? heads * ((a.decode_rows + a.decode_block - 1) / a.decode_block) : 0;
-    a.merges = (unsigned)a.decode_merges + (sp.chunk ? (unsigned)heads * a.merge_blocks : 0);
+    a.merges = (unsigned)a.decode_merges + (sp.chunk ? (unsigned)(row_blocks(seqs, n_new, group, a.decode_rows + 1) * pool->heads * kPoolChunkWaves) : 0);
     if (rc == SRFT_OK && a.merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb), srft_grid(a.merges), 64 * kPoolTeam, st, a);
     return rc;
 }

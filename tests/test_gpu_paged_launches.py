@@ -131,3 +131,31 @@ def test_rotary_in_place_where_a_stride_does_not_count(B):
     with pytest.raises(B.SrftError) as e:
         B.srft_rotary([(x, x.view(torch.bfloat16))], positions, freq)
     assert e.value.status == -7
+
+
+def test_the_merge_has_workgroups_for_rows_that_there_are(B):
+    """A prompt of 32,768 tokens among 4095 sequences of one, 512 query heads on 8: were every sequence as long, the merge's workgroups
+    would be more than 32 bits count, and the call refused."""
+    plan = B.Plan(64, 32, 3)
+    pool = B.PagePool.empty(plan, plan, 8, 16, 1, 1)
+    n, long_ = 4096, 32768
+    t = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device="cuda")      # noqa: E731
+    seqs = B.PagedSeqs(t(n, long_ // 16), t(n, 2), t(n), t(n + 1), max_new=long_, max_length=long_)
+    assert B.srft_pool_attention_workspace_bytes(pool, seqs, long_ + n - 1, 512) > 0
+    pool.close()
+
+
+@pytest.mark.parametrize("new", [[300, 1, 0, 17, 16, 257, 2, 256, 0, 1], [0, 0, 600, 0, 1, 5, 40, 8, 9, 0], [1] * 9 + [513]])
+@pytest.mark.parametrize("cap", [0, 2, 11])
+def test_rows_of_chunks_among_rows_of_few(B, new, cap):
+    """Blocks of rows that several workgroups share, of sequences between others that have none."""
+    s = Serving(B, 64, 32, 8, 32, 2, n=len(new), max_length=1200, seed=sum(new))
+    s.append([200, 0, 31, 500, 7, 0, 64, 33, 1, 450])
+    s.append(new)
+    q = queries(s, sum(new), 2, F16)
+    for p in s.plans:
+        B.srft_plan_set_max_workgroups(p.handle, cap)
+    out = s.run(q, new, 0.125)
+    torch.cuda.synchronize()
+    check(s, q, new, 0.125, out, 2)
+    s.close()
