@@ -308,6 +308,45 @@ int srft_rotary(const srft_rotary_rows* rows, int count, int64_t n_tokens, int d
                 const int32_t* positions_dev, const double* freq_dev, double factor, int inverse, void* hip_stream);
 
 /*
+ * RMS norms of rows of heads and their rotary positions, in one pass over several tensors of the same tokens (queries and keys).  A row
+ * x of d channels becomes srft_rotary's turn of n, with
+ *     n_i = x_i r w_i,   r = 1 / sqrt(mean_j x_j^2 + eps)          (all d channels; those from rot on are not turned).
+ * The values are fp32 up to the output, which is rounded once.  A row's mean of squares must stay inside fp32.
+ *   rows          HOST array of `count` tensors (0 .. SRFT_ROTARY_MAX): x as in srft_rotary, in place too (out_dev == in_dev with the same
+ *                 strides and type); weight_dev [d] of weight_type (a srft_dtype), aligned to its element, or NULL: all 1.
+ *   eps           from 1.17549435e-38 to 3.4e38 (else SRFT_ERR_BAD_N).
+ * All else, sizes, refusals and launches, as in srft_rotary.
+ *
+ * srft_norm_rotary_backward: from dy, the gradient of the call's outputs, and its inputs,
+ *     dx, the gradient of x, and dweight [d] fp32, that of the weights, summed over tokens and heads; both are written, not added to.
+ *   dx has x's type.  dx_dev may be x_dev or dy_dev, with the same strides and type; overlapping otherwise is not allowed.  dweight_dev NULL: not
+ *   asked for; two tensors have two of them (else SRFT_ERR_BAD_N).  n_tokens == 0 writes zeros there.
+ *   workspace_dev  srft_norm_rotary_backward_workspace_bytes bytes, 16-byte aligned, overwritten (NULL where no dweight is asked for).
+ * Sums are fp32, in an order that depends on sizes and alignment alone.
+ */
+typedef struct srft_norm_rows {
+    srft_rotary_rows x;
+    const void* weight_dev;
+    int32_t weight_type;
+    int32_t reserved;                                        /* 0 */
+} srft_norm_rows;
+int srft_norm_rotary(const srft_norm_rows* rows, int count, int64_t n_tokens, int d, int rot, int layout, const int32_t* positions_dev,
+                     const double* freq_dev, double factor, double eps, void* hip_stream);
+typedef struct srft_norm_grad_rows {
+    const void *dy_dev, *x_dev;
+    void* dx_dev;
+    const void* weight_dev;
+    float* dweight_dev;
+    int64_t dy_token, dy_head, x_token, x_head, dx_token, dx_head;       /* strides in elements */
+    int32_t n_heads;
+    int32_t dy_type, x_type, weight_type;                    /* srft_dtype */
+} srft_norm_grad_rows;
+int64_t srft_norm_rotary_backward_workspace_bytes(int count, int d);
+int srft_norm_rotary_backward(const srft_norm_grad_rows* rows, int count, int64_t n_tokens, int d, int rot, int layout,
+                              const int32_t* positions_dev, const double* freq_dev, double factor, double eps, void* workspace_dev,
+                              void* hip_stream);
+
+/*
  * Paged cache of one layer: a pool of pages for K and one for V, shared by sequences of any length.     (Sec. 7.2, with the pages of
  * a sequence in any order.)  A page holds R = page_tokens tokens of n_heads key heads as the plans' record; the tokens behind a
  * sequence's last full page are exact fp16 in a window of R tokens, as in srft_cache, and become a page when the window is full:

@@ -37,6 +37,7 @@ EXPORTS = [
     "srft_attend_workspace_bytes", "srft_kv_attend", "srft_decode_attention_workspace_bytes", "srft_kv_decode_attention",
     "srft_rotary", "srft_pool_create", "srft_pool_destroy", "srft_pool_append_workspace_bytes", "srft_pool_append",
     "srft_pool_attention_workspace_bytes", "srft_pool_attention", "srft_pool_copy",
+    "srft_norm_rotary", "srft_norm_rotary_backward_workspace_bytes", "srft_norm_rotary_backward",
 ]
 
 
@@ -105,6 +106,9 @@ def lib() -> C.CDLL:
     L.srft_kv_quantize_batched.argtypes = [vp, vp, vp, vp, vp, ci, vp]
     L.srft_kv_dequantize_batched.argtypes = [vp, vp, vp, vp, vp, ci, vp]
     L.srft_rotary.argtypes = [vp, ci, i64, ci, ci, ci, vp, vp, C.c_double, ci, vp]
+    L.srft_norm_rotary.argtypes = [vp, ci, i64, ci, ci, ci, vp, vp, C.c_double, C.c_double, vp]
+    L.srft_norm_rotary_backward_workspace_bytes.argtypes = [ci, ci]
+    L.srft_norm_rotary_backward.argtypes = [vp, ci, i64, ci, ci, ci, vp, vp, C.c_double, C.c_double, vp, vp]
     L.srft_pool_create.argtypes = [C.POINTER(vp), vp, vp, ci, ci, i64, i64, vp, vp]
     L.srft_pool_destroy.argtypes = [vp]
     L.srft_pool_append_workspace_bytes.argtypes = [vp, vp, i64]
@@ -127,6 +131,7 @@ def lib() -> C.CDLL:
     L.srft_decode_attention_workspace_bytes.restype = i64
     L.srft_pool_append_workspace_bytes.restype = i64
     L.srft_pool_attention_workspace_bytes.restype = i64
+    L.srft_norm_rotary_backward_workspace_bytes.restype = i64
     L.srft_cache_tokens.restype = i64
     L.srft_cache_quantized_tokens.restype = i64
     if _marshal is not None:
@@ -507,6 +512,85 @@ def srft_rotary(items, positions: torch.Tensor, freq: torch.Tensor, layout: str 
         r.n_heads, r.in_type, r.out_type = x.shape[1], DTYPES[x.dtype], DTYPES[y.dtype]
     _check(lib().srft_rotary(rows, len(items), n, d, 2 * freq.shape[0], ROTARY_LAYOUTS[layout], _dev_ptr(positions, torch.int32, "positions"),
                              _dev_ptr(freq, torch.float64, "freq"), factor, bool(inverse), _stream_handle(stream)), "srft_rotary")
+
+
+class _NormRows(C.Structure):
+    _fields_ = [("x", _RotaryRows), ("weight_dev", C.c_void_p), ("weight_type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class _NormGradRows(C.Structure):
+    _fields_ = [("dy_dev", C.c_void_p), ("x_dev", C.c_void_p), ("dx_dev", C.c_void_p), ("weight_dev", C.c_void_p), ("dweight_dev", C.c_void_p),
+                ("dy_token", C.c_int64), ("dy_head", C.c_int64), ("x_token", C.c_int64), ("x_head", C.c_int64), ("dx_token", C.c_int64),
+                ("dx_head", C.c_int64), ("n_heads", C.c_int32), ("dy_type", C.c_int32), ("x_type", C.c_int32), ("weight_type", C.c_int32)]
+
+
+def _norm_rows(items, positions: torch.Tensor, freq: torch.Tensor, tensors: int) -> tuple[int, int]:
+    """(tokens, channels) of a call's items, the first `tensors` of each of one shape."""
+    n, _, d = items[0][0].shape
+    if positions.shape != (n,) or freq.dim() != 1:
+        raise ValueError("positions must be [tokens], freq one-dimensional")
+    for item in items:
+        if any(t.shape != item[0].shape for t in item[:tensors]) or item[0].shape[0] != n or item[0].shape[2] != d:
+            raise ValueError("all tensors of a call must have the same tokens and channels, those of an item one shape")
+        if any(t.dtype not in DTYPES for t in item[:tensors]):
+            raise ValueError("norms take float32, float16 and bfloat16")
+    return n, d
+
+
+def _norm_weight(weight, d: int) -> tuple[int, int]:
+    """Address and type of an item's weights."""
+    if weight is None:
+        return 0, 0
+    if weight.dtype not in DTYPES or weight.shape != (d,):
+        raise ValueError("weights must be [d], float32, float16 or bfloat16, or None")
+    return _dev_ptr(weight, weight.dtype, "weight"), DTYPES[weight.dtype]
+
+
+def srft_norm_rotary(items, positions: torch.Tensor, freq: torch.Tensor, eps: float, layout: str = "half", factor: float = 1.0, stream=None) -> None:
+    """RMS norms of (x, weight, out) triples and their rotary positions: x and out [tokens, heads, d] of the same tokens, weight [d] or
+    None; x / sqrt(mean(x^2) + eps) * weight, then srft_rotary's turn.  out may be x."""
+    items = list(items)
+    if not items:
+        return
+    items = [(x, out, weight) for x, weight, out in items]
+    n, d = _norm_rows(items, positions, freq, 2)
+    rows = (_NormRows * len(items))()
+    for r, (x, y, weight) in zip(rows, items):
+        r.x.in_dev, r.x.in_token, r.x.in_head = _rows(x, "x")
+        r.x.out_dev, r.x.out_token, r.x.out_head = _rows(y, "out")
+        r.x.n_heads, r.x.in_type, r.x.out_type = x.shape[1], DTYPES[x.dtype], DTYPES[y.dtype]
+        r.weight_dev, r.weight_type = _norm_weight(weight, d)
+    _check(lib().srft_norm_rotary(rows, len(items), n, d, 2 * freq.shape[0], ROTARY_LAYOUTS[layout], _dev_ptr(positions, torch.int32, "positions"),
+                                  _dev_ptr(freq, torch.float64, "freq"), factor, eps, _stream_handle(stream)), "srft_norm_rotary")
+
+
+def srft_norm_rotary_backward_workspace_bytes(count: int, d: int) -> int:
+    return _sized(lib().srft_norm_rotary_backward_workspace_bytes(count, d), "srft_norm_rotary_backward_workspace_bytes")
+
+
+def srft_norm_rotary_backward(items, positions: torch.Tensor, freq: torch.Tensor, eps: float, workspace, layout: str = "half", factor: float = 1.0,
+                              stream=None) -> None:
+    """Gradients of srft_norm_rotary from (dy, x, weight, dx, dweight) items: dy and x [tokens, heads, d], weight [d] or None; dx, of x's type
+    and shape, and dweight [d] float32 (or None) are written.  dx may be x or dy.  workspace may be None where no dweight is asked for."""
+    items = list(items)
+    if not items:
+        return
+    items = [(dy, x, dx, weight, dweight) for dy, x, weight, dx, dweight in items]
+    n, d = _norm_rows(items, positions, freq, 3)
+    rows = (_NormGradRows * len(items))()
+    for r, (dy, x, dx, weight, dweight) in zip(rows, items):
+        if dx.dtype != x.dtype or (dweight is not None and dweight.shape != (d,)):
+            raise ValueError("dx must have x's type, dweight must be [d]")
+        r.dy_dev, r.dy_token, r.dy_head = _rows(dy, "dy")
+        r.x_dev, r.x_token, r.x_head = _rows(x, "x")
+        r.dx_dev, r.dx_token, r.dx_head = _rows(dx, "dx")
+        r.n_heads, r.dy_type, r.x_type = x.shape[1], DTYPES[dy.dtype], DTYPES[x.dtype]
+        r.weight_dev, r.weight_type = _norm_weight(weight, d)
+        r.dweight_dev = None if dweight is None else _dev_ptr(dweight, torch.float32, "dweight")
+    space = None if workspace is None else _pool_workspace(workspace, srft_norm_rotary_backward_workspace_bytes(len(items), d))
+    _check(lib().srft_norm_rotary_backward(rows, len(items), n, d, 2 * freq.shape[0], ROTARY_LAYOUTS[layout],
+                                           _dev_ptr(positions, torch.int32, "positions"), _dev_ptr(freq, torch.float64, "freq"), factor, eps, space,
+                                           _stream_handle(stream)), "srft_norm_rotary_backward")
 
 
 # ---------------------------------------------------------------------------- paged cache

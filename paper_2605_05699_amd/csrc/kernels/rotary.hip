@@ -7,13 +7,10 @@
 // head (of 40 heads at d = 128 that leaves 1.6 sine-cosine pairs a thread).  A thread moves V pairs, or V of the channels behind
 // them twice: two 16-byte loads and stores of 16-bit values.
 // 168 MB in 33.7 us, 5.0 TB/s (8192 tokens, 40 heads of 128 channels; a copy of this card gets 5.5).
-#include <algorithm>
-
-#include "../common.h"
+#include "../rotary_rows.h"
 
 namespace {
 
-typedef __bf16 bf16;
 struct rotary_args {
     srft_rotary_rows t[SRFT_ROTARY_MAX];
     int row_units[2];                       // of a row: those with pairs, all
@@ -22,31 +19,6 @@ struct rotary_args {
     const int32_t* positions;
     const double* freq;
 };
-
-template <class T, int V> struct alignas(sizeof(T) * V <= 16 ? sizeof(T) * V : 16) wide { T v[V]; };
-
-template <class T, int V>
-__device__ __forceinline__ void load(float (&x)[V], const T* p) {
-    const wide<T, V> w = *reinterpret_cast<const wide<T, V>*>(p);
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = (float)w.v[i];
-}
-template <class T, int V>
-__device__ __forceinline__ void store(const float (&x)[V], T* p) {
-    wide<T, V> w;
-#pragma unroll
-    for (int i = 0; i < V; ++i) w.v[i] = (T)x[i];
-    *reinterpret_cast<wide<T, V>*>(p) = w;
-}
-// cos and sin of t, a position times radians per token
-__device__ __forceinline__ float2 turn(double t) {
-    const double n = rint(t * 0.15915494309189533577);
-    double r = fma(n, -6.283185307179586232, t);                 // 2 pi as a sum of two numbers
-    r = fma(n, -2.4492935982947063545e-16, r);
-    float s, c;
-    sincosf((float)r, &s, &c);
-    return make_float2(c, s);
-}
 
 // V: pairs of a thread; IN, OUT: types.  One workgroup per token (srft_grid); LDS: rot / 2 pairs (cos, sin) times factor.
 template <class IN, class OUT, int V>
@@ -126,17 +98,8 @@ template <class IN, class OUT> rotary_kernel_t pick(int v) {
 template <class IN> rotary_kernel_t pick(int out, int v) {
     return out == SRFT_F32 ? pick<IN, float>(v) : out == SRFT_F16 ? pick<IN, _Float16>(v) : pick<IN, bf16>(v);
 }
-int type_bytes(int t) { return t == SRFT_F32 ? 4 : 2; }
-bool type_known(int t) { return t == SRFT_F32 || t == SRFT_F16 || t == SRFT_BF16; }
-
-// Whether threads can move V channels at once of this tensor: whole vectors from and to addresses of a vector's alignment.
 bool fits(const srft_rotary_rows& r, int rot, int d, int v) {
-    if (rot / 2 % v != 0 || (d - rot) % (2 * v) != 0) return false;
-    const auto ok = [&](const void* p, int64_t token, int64_t head, int type) {
-        const int64_t bytes = std::min(16, v * type_bytes(type));
-        return srft_aligned(p, bytes) && token * type_bytes(type) % bytes == 0 && head * type_bytes(type) % bytes == 0;
-    };
-    return ok(r.in_dev, r.in_token, r.in_head, r.in_type) && ok(r.out_dev, r.out_token, r.out_head, r.out_type);
+    return fits_row(rot, d, v) && fits(r.in_dev, r.in_token, r.in_head, r.in_type, v) && fits(r.out_dev, r.out_token, r.out_head, r.out_type, v);
 }
 
 }  // namespace
