@@ -429,6 +429,41 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
                         void* workspace_dev, void* hip_stream);
 
 /*
+ * Sliding attention: srft_pool_attention where a token sees, of the tokens up to itself, the last `recent` ones (itself among them) and the
+ * sequence's first `sinks` ones.  Pages that no row of the call sees are not read, nor are the entries of the page table that name them.
+ *   recent, sinks   recent >= 1, sinks >= 0 (else SRFT_ERR_BAD_N).  With recent + sinks >= max_length it is srft_pool_attention.
+ *   workspace_dev   srft_pool_attention_sliding_workspace_bytes bytes, 256-byte aligned, overwritten.
+ */
+int64_t srft_pool_attention_sliding_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, int64_t n_new, int n_q_heads);
+int srft_pool_attention_sliding(const srft_pool_t* pool, const srft_paged_seqs* seqs, const void* q_dev, int type, int64_t n_new, int n_q_heads,
+                                int64_t q_token, int64_t q_head, float softmax_scale, int64_t recent, int64_t sinks, void* out_dev,
+                                int64_t out_token, int64_t out_head, void* workspace_dev, void* hip_stream);
+
+/*
+ * Attention of sequences that begin with the same pages (samples of one prompt, conversations behind one long instruction: forks whose full
+ * pages are not copied).  The outputs are srft_pool_attention's, within the roundings named there; the pages in common are read once for all
+ * rows of a group.
+ * Group g is the sequences groups[g] .. groups[g + 1] - 1, whose first tokens[g] tokens lie in the same pages; of these, whole pages count
+ * that all of the group's sequences with new tokens hold without them, and the entries of its first such sequence name them (those of the
+ * others are not read).  Sequences outside of all groups are as in srft_pool_attention.  Groups are ascending: a bound below the one
+ * in front of it, or past n_seq, is taken as that.
+ *   prefixes        0 <= n_groups <= n_seq (else SRFT_ERR_BAD_N); without groups the pointers may be NULL.
+ *   workspace_dev   srft_pool_attention_shared_workspace_bytes bytes, 256-byte aligned, overwritten.
+ * With 2 n_new in the place of n_new and n_seq + n_groups in that of n_seq the sizes named at srft_pool_attention stay below the same bounds.
+ */
+typedef struct srft_shared_prefixes {
+    int32_t n_groups;
+    int32_t reserved;                                        /* 0 */
+    const int32_t* groups_dev;                               /* [n_groups + 1] */
+    const int32_t* tokens_dev;                               /* [n_groups] */
+} srft_shared_prefixes;
+int64_t srft_pool_attention_shared_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, const srft_shared_prefixes* prefixes,
+                                                   int64_t n_new, int n_q_heads);
+int srft_pool_attention_shared(const srft_pool_t* pool, const srft_paged_seqs* seqs, const srft_shared_prefixes* prefixes, const void* q_dev, int type,
+                               int64_t n_new, int n_q_heads, int64_t q_token, int64_t q_head, float softmax_scale, void* out_dev,
+                               int64_t out_token, int64_t out_head, void* workspace_dev, void* hip_stream);
+
+/*
  * Copies inside pools: page pages[i][0] to page pages[i][1] and window windows[i][0] to windows[i][1], K and V, in each of n_pools pools of
  * one geometry (the layers of a model): what a fork or a compaction needs.  Device arrays [n][2] of int32.  No destination may be
  * another destination or a source of the same call; a pair with a number out of range is skipped.  Up to 64 pools and 2^22 pairs of pages and

@@ -38,6 +38,8 @@ EXPORTS = [
     "srft_rotary", "srft_pool_create", "srft_pool_destroy", "srft_pool_append_workspace_bytes", "srft_pool_append",
     "srft_pool_attention_workspace_bytes", "srft_pool_attention", "srft_pool_copy",
     "srft_norm_rotary", "srft_norm_rotary_backward_workspace_bytes", "srft_norm_rotary_backward",
+    "srft_pool_attention_sliding_workspace_bytes", "srft_pool_attention_sliding",
+    "srft_pool_attention_shared_workspace_bytes", "srft_pool_attention_shared",
 ]
 
 
@@ -115,6 +117,10 @@ def lib() -> C.CDLL:
     L.srft_pool_append.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp]
     L.srft_pool_attention_workspace_bytes.argtypes = [vp, vp, i64, ci]
     L.srft_pool_attention.argtypes = [vp, vp, vp, ci, i64, ci, i64, i64, C.c_float, vp, i64, i64, vp, vp]
+    L.srft_pool_attention_sliding_workspace_bytes.argtypes = [vp, vp, i64, ci]
+    L.srft_pool_attention_sliding.argtypes = [vp, vp, vp, ci, i64, ci, i64, i64, C.c_float, i64, i64, vp, i64, i64, vp, vp]
+    L.srft_pool_attention_shared_workspace_bytes.argtypes = [vp, vp, vp, i64, ci]
+    L.srft_pool_attention_shared.argtypes = [vp, vp, vp, vp, ci, i64, ci, i64, i64, C.c_float, vp, i64, i64, vp, vp]
     L.srft_pool_copy.argtypes = [vp, ci, vp, i64, vp, i64, vp]
     for name in ("srft_plan_d", "srft_plan_group_size", "srft_plan_groups", "srft_plan_code_bytes"):
         getattr(L, name).argtypes = [vp]
@@ -131,6 +137,8 @@ def lib() -> C.CDLL:
     L.srft_decode_attention_workspace_bytes.restype = i64
     L.srft_pool_append_workspace_bytes.restype = i64
     L.srft_pool_attention_workspace_bytes.restype = i64
+    L.srft_pool_attention_sliding_workspace_bytes.restype = i64
+    L.srft_pool_attention_shared_workspace_bytes.restype = i64
     L.srft_norm_rotary_backward_workspace_bytes.restype = i64
     L.srft_cache_tokens.restype = i64
     L.srft_cache_quantized_tokens.restype = i64
@@ -621,6 +629,22 @@ class PagedSeqs:
         self.address = C.addressof(self.struct)
 
 
+class _SharedPrefixes(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("reserved", C.c_int32), ("groups_dev", C.c_void_p), ("tokens_dev", C.c_void_p)]
+
+
+class SharedPrefixes:
+    """Sequences with pages in common (srft_shared_prefixes): int32 device tensors groups [n + 1], bounds of the groups among a step's
+    sequences, and tokens [n], the tokens whose pages those of a group share.  The tensors are kept alive."""
+
+    def __init__(self, groups, tokens):
+        if tokens.dim() != 1 or groups.shape != (tokens.shape[0] + 1,):
+            raise ValueError("groups must be [n + 1], tokens [n]")
+        self.groups, self.tokens, self.n_groups = groups, tokens, tokens.shape[0]
+        self.struct = _SharedPrefixes(self.n_groups, 0, _dev_ptr(groups, torch.int32, "groups"), _dev_ptr(tokens, torch.int32, "tokens"))
+        self.address = C.addressof(self.struct)
+
+
 class PagePool:
     """One layer's pages (srft_pool_create) over tensors of the caller's: k and v are (codes [pages, heads, R, code bytes] uint8,
     scales [pages, heads, R, groups] float32, window [windows, heads, R, d] float16) each.  No pages: sequences shorter than one."""
@@ -717,13 +741,50 @@ def srft_pool_attention(pool: PagePool, seqs: PagedSeqs, q: torch.Tensor, softma
         status = _fast_pool_attention(pool.handle, seqs.address, pool.d, q, softmax_scale, out, workspace)
         if status is not None:
             return _check(status, "srft_pool_attention") if status else None
-    n, heads, d = q.shape
-    if q.dtype not in (torch.float16, torch.bfloat16) or out.dtype != q.dtype or out.shape != q.shape or d != pool.d:
-        raise ValueError("q and out must be [n_new, q heads, d], both float16 or both bfloat16")
+    n, heads, _ = _attention_shape(pool, q, out)
     (q_at, q_token, q_head), (o_at, o_token, o_head) = _rows(q, "q"), _rows(out, "out")
     space = _pool_workspace(workspace, srft_pool_attention_workspace_bytes(pool, seqs, n, heads))
     _check(lib().srft_pool_attention(pool.handle, seqs.address, q_at, DTYPES[q.dtype], n, heads, q_token, q_head, softmax_scale, o_at, o_token,
                                      o_head, space, _stream_handle(stream)), "srft_pool_attention")
+
+
+def _attention_shape(pool: PagePool, q: torch.Tensor, out: torch.Tensor) -> tuple[int, int, int]:
+    n, heads, d = q.shape
+    if q.dtype not in (torch.float16, torch.bfloat16) or out.dtype != q.dtype or out.shape != q.shape or d != pool.d:
+        raise ValueError("q and out must be [n_new, q heads, d], both float16 or both bfloat16")
+    return n, heads, d
+
+
+def srft_pool_attention_sliding_workspace_bytes(pool: PagePool, seqs: PagedSeqs, n_new: int, n_q_heads: int) -> int:
+    return _sized(lib().srft_pool_attention_sliding_workspace_bytes(pool.handle, seqs.address, n_new, n_q_heads),
+                  "srft_pool_attention_sliding_workspace_bytes")
+
+
+def srft_pool_attention_sliding(pool: PagePool, seqs: PagedSeqs, q: torch.Tensor, softmax_scale: float, recent: int, sinks: int, out: torch.Tensor,
+                                workspace: torch.Tensor, stream=None) -> None:
+    """out <- causal attention of q [n_new, q heads, d] over each row's last `recent` tokens and its sequence's first `sinks`."""
+    n, heads, _ = _attention_shape(pool, q, out)
+    if not -1 << 63 <= recent < 1 << 63 or not -1 << 63 <= sinks < 1 << 63:          # (ctypes would keep the low bits)
+        raise ValueError("recent and sinks must fit int64_t")
+    (q_at, q_token, q_head), (o_at, o_token, o_head) = _rows(q, "q"), _rows(out, "out")
+    space = _pool_workspace(workspace, srft_pool_attention_sliding_workspace_bytes(pool, seqs, n, heads))
+    _check(lib().srft_pool_attention_sliding(pool.handle, seqs.address, q_at, DTYPES[q.dtype], n, heads, q_token, q_head, softmax_scale, recent, sinks,
+                                             o_at, o_token, o_head, space, _stream_handle(stream)), "srft_pool_attention_sliding")
+
+
+def srft_pool_attention_shared_workspace_bytes(pool: PagePool, seqs: PagedSeqs, prefixes: SharedPrefixes, n_new: int, n_q_heads: int) -> int:
+    return _sized(lib().srft_pool_attention_shared_workspace_bytes(pool.handle, seqs.address, prefixes.address, n_new, n_q_heads),
+                  "srft_pool_attention_shared_workspace_bytes")
+
+
+def srft_pool_attention_shared(pool: PagePool, seqs: PagedSeqs, prefixes: SharedPrefixes, q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
+                               workspace: torch.Tensor, stream=None) -> None:
+    """out <- srft_pool_attention's, where groups of sequences begin with the same pages: these are read once for all rows of a group."""
+    n, heads, _ = _attention_shape(pool, q, out)
+    (q_at, q_token, q_head), (o_at, o_token, o_head) = _rows(q, "q"), _rows(out, "out")
+    space = _pool_workspace(workspace, srft_pool_attention_shared_workspace_bytes(pool, seqs, prefixes, n, heads))
+    _check(lib().srft_pool_attention_shared(pool.handle, seqs.address, prefixes.address, q_at, DTYPES[q.dtype], n, heads, q_token, q_head, softmax_scale,
+                                            o_at, o_token, o_head, space, _stream_handle(stream)), "srft_pool_attention_shared")
 
 
 def srft_pool_copy(table: PoolTable, pages: torch.Tensor, windows: torch.Tensor, stream=None) -> None:

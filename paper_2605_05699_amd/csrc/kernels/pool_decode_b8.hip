@@ -2,7 +2,7 @@
 #include "../pool_decode.h"
 
 namespace {
-template <int D> pool_attention_kernel_t pick(int cb, int gm) { return pool_pick_decode<D, 8>(cb, gm); }
+template <int D> pool_attention_kernel_t pick(int cb, int gm) { return pool_pick_decode<D, 8, kPoolCausal>(cb, gm); }
 pool_attention_kernel_t dispatch(int d, int cb, int gm) { SRFT_DISPATCH_D(d, pick, cb, gm) }
 }  // namespace
 

@@ -10,18 +10,21 @@
 
 namespace {
 
-template <int D>
+template <int D, int FORM>
 __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsigned workgroup, uint4* ops, float (*tops)[32]) {
     constexpr int BLOCKS = kPoolChunkWaves, ROWS = kPoolBlock * BLOCKS, KEYS = kPoolChunkKeys<D>, G = D / 32, T = D / 16, OWN = (G + kPoolTeam - 1) / kPoolTeam, AHEAD = 2;
     // ops: [k-step][hi, lo][lane]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int of = (int)(workgroup / BLOCKS), block = (int)workgroup - of * BLOCKS, at = of / a.heads, head = of - at * a.heads;
-    if (at >= a.blocks_before[a.s.n_seq]) return;
-    const int seq = a.s.n_seq == 1 ? 0 : __builtin_amdgcn_readfirstlane(pool_sequence_of(a.blocks_before, a.s.n_seq, at)), rt = at - a.blocks_before[seq];
-    const pool_seq q = pool_seq_of(a.s, seq);
+    const int of = (int)(workgroup / BLOCKS), block = (int)workgroup - of * BLOCKS, head = of - of / a.heads * a.heads;
+    const bool groups = FORM == kPoolShared && a.merge_groups;
+    const int n_seq = groups ? a.s.n_seq + a.n_groups : a.s.n_seq, at = of / a.heads + (groups ? a.blocks_before[a.s.n_seq] : 0);
+    if (at >= a.blocks_before[n_seq]) return;
+    const int seq = n_seq == 1 ? 0 : __builtin_amdgcn_readfirstlane(pool_sequence_of(a.blocks_before, n_seq, at)), rt = at - a.blocks_before[seq];
+    const pool_view view = pool_view_of<FORM>(a, seq);
+    const pool_seq& q = view.q;
     const int r0 = rt * ROWS + block * kPoolBlock;
     if (r0 >= q.n_new * a.group) return;
-    const int tiles = pool_tiles(pool_seen(q, a.group, ROWS, rt), q.full, KEYS);
+    const int tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, rt);
     const pool_row row = pool_row_of(q, head, a.group, r0 + (lane & 31));
     char* const dst = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
     if (tiles == 0) {
@@ -30,13 +33,13 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
         return;
     }
     const int* const before = a.chunk_before;
-    const int units = before[a.s.n_seq];
+    const int units = before[pool_count<FORM>(a)];
     if (units == 0) return;                                  // (too many of them: see kPoolMostUnits)
-    const int first = before[seq] + head * pool_chunk_units(q, a.group, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS) +
-                      pool_chunk_units(q, a.group, ROWS, KEYS, rt);
+    const int first = before[seq] + head * pool_chunk_units<FORM>(a, q, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS) +
+                      pool_chunk_units<FORM>(a, q, ROWS, KEYS, rt);
     const pool_shares shares(units, a.chunk_grid, 1);
     const int w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
-    if (w0 == w1) return;
+    if (w0 == w1 && (!view.joint || groups)) return;
     const int behind = shares.begin(w0) != first ? 1 : 0;    // the first part's workgroup began with other rows
     const auto part = [&](int w) __attribute__((always_inline)) {
         return a.chunk_parts + ((2LL * w + (w == w0 ? behind : 0)) * BLOCKS + block) * kPoolPart<D>;
@@ -46,7 +49,24 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     floatx16 sums[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i) sums[i] = floatx16{0};
-    for (int v = w0; v <= w1; v += AHEAD) {
+    const long long r_at = (long long)row.token * (a.heads * a.group) + row.head;
+    if (FORM == kPoolShared && view.joint && !groups) {
+        // the rows' sums over the tokens in common, and over their own where one workgroup has had all of these
+        for (int k = 1; k >= (w0 == w1 ? 0 : 1); --k) {
+            const floatx4 x = reinterpret_cast<const floatx4*>(a.joint_heads[k])[r_at];
+            pool_part_head h[1] = {{x[0], x[1], x[2], 0.0f}};
+            const float before = pool_join(t_all, den, e_all, h, 0, 0);
+#pragma unroll
+            for (int i = 0; i < OWN; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const floatx4 y = pool_block<D>::get4(a.joint_rows[k] + r_at * D, 4 * min(wave + kPoolTeam * i, G - 1) + j, half, a.bits);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) sums[i][4 * j + m] = fmaf(y[m], h[0].factor, sums[i][4 * j + m] * before);
+                }
+        }
+    }
+    for (int v = w0; v <= w1 && (FORM != kPoolShared || w0 != w1); v += AHEAD) {
         floatx4 x[AHEAD][OWN][4];
         pool_part_head h[AHEAD];
 #pragma unroll
@@ -69,6 +89,18 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int m = 0; m < 4; ++m) sums[i][4 * j + m] = fmaf(x[k][i][j][m], h[k].factor, sums[i][4 * j + m]);
+    }
+    if (FORM == kPoolShared && groups) {                     // (uniform)
+        if (!row.there) return;
+#pragma unroll
+        for (int i = 0; i < OWN; ++i)
+            if (wave + kPoolTeam * i < G)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    pool_block<D>::put4(a.joint_rows[1] + r_at * D, 4 * (wave + kPoolTeam * i) + j, half,
+                                        floatx4{sums[i][4 * j], sums[i][4 * j + 1], sums[i][4 * j + 2], sums[i][4 * j + 3]}, a.bits);
+        if (wave == 0 && half == 0) reinterpret_cast<floatx4*>(a.joint_heads[1])[r_at] = floatx4{t_all, den, __uint_as_float((uint32_t)e_all), 0.0f};
+        return;
     }
     // ---- as pool_finish, the operands through LDS
     float m = 0.0f;
@@ -117,25 +149,29 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     }
 }
 
-template <int D, int CB>
+template <int D, int CB, int FORM>
 __global__ void __launch_bounds__(64 * kPoolTeam) srft_pool_merge_kernel(const pool_attention_args a) {
     constexpr int OPS = D / 16 * 2 * 64;
     __shared__ __align__(16) unsigned char lds[std::max(kPoolFinishBytes<D>, OPS * 16 + kPoolTeam * 32 * 4)];
     const unsigned workgroup = blockIdx.y * gridDim.x + blockIdx.x;          // (what follows is uniform)
     if (workgroup >= a.merges) return;
     if (workgroup < (unsigned)a.decode_merges)
-        pool_decode_merge<D, CB>(a, workgroup, lds);
+        pool_decode_merge<D, CB, FORM>(a, workgroup, lds);
     else
-        chunk_merge<D>(a, workgroup - a.decode_merges, reinterpret_cast<uint4*>(lds), reinterpret_cast<float (*)[32]>(lds + OPS * 16));
+        chunk_merge<D, FORM>(a, workgroup - a.decode_merges, reinterpret_cast<uint4*>(lds), reinterpret_cast<float (*)[32]>(lds + OPS * 16));
 }
 
-template <int D> pool_attention_kernel_t pick(int cb) {
-    if constexpr (D <= 128)
-        if (cb == 2) return srft_pool_merge_kernel<D, 2>;
-    return srft_pool_merge_kernel<D, 1>;
+template <int D, int CB> pool_attention_kernel_t form_of(int form) {
+    return form == kPoolShared ? srft_pool_merge_kernel<D, CB, kPoolShared>
+           : form == kPoolSliding ? srft_pool_merge_kernel<D, CB, kPoolSliding> : srft_pool_merge_kernel<D, CB, kPoolCausal>;
 }
-pool_attention_kernel_t dispatch(int d, int cb) { SRFT_DISPATCH_D(d, pick, cb) }
+template <int D> pool_attention_kernel_t pick(int cb, int form) {
+    if constexpr (D <= 128)
+        if (cb == 2) return form_of<D, 2>(form);
+    return form_of<D, 1>(form);
+}
+pool_attention_kernel_t dispatch(int d, int cb, int form) { SRFT_DISPATCH_D(d, pick, cb, form) }
 
 }  // namespace
 
-pool_attention_kernel_t srft_pick_pool_merge(int d, int cb) { return dispatch(d, cb); }
+pool_attention_kernel_t srft_pick_pool_merge(int d, int cb, int form) { return dispatch(d, cb, form); }

@@ -15,20 +15,78 @@ namespace {
 template <int BITS>
 constexpr int position_channel(int e) { return BITS == 8 ? (e & 4) + ((e & 1) << 1) + ((e & 2) >> 1) : e / 2 + 4 * (e % 2); }
 
-// units of work in front of each sequence, by one workgroup
-template <int D>
-__device__ __forceinline__ void count_units(const pool_attention_args& a) {
-    constexpr int NT = 2 * D, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * kPoolChunkWaves;
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x = min(x, __shfl_xor(x, d));
+    return x;
+}
+// The items of the shared form, by one workgroup.  A group has in common what the caller says, as far as all its sequences with new tokens have it
+// without these, in whole pages; with one such sequence there is nothing to share.  Groups are taken as ascending, whatever the caller's array
+// holds, so that a sequence is in one at most.
+template <int NT>
+__device__ __forceinline__ void make_items(const pool_attention_args& a) {
     const pool_seqs& s = a.s;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    // the sequences' own units first, then their sums in place
-    for (int b = wave; b < s.n_seq; b += NT / 64) {
+    if (wave == 0) {
+        int before = 0;
+        for (int g0 = 0; g0 <= a.n_groups; g0 += 64) {
+            int x = min(max(a.groups[min(g0 + lane, a.n_groups)], before), s.n_seq);
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int other = __shfl_up(x, d);
+                if (lane >= d) x = max(x, other);
+            }
+            if (g0 + lane <= a.n_groups) a.bounds[g0 + lane] = x;
+            before = __shfl(x, 63);
+        }
+    }
+    for (int b = threadIdx.x; b < s.n_seq; b += NT) {
         const pool_seq q = pool_seq_of(s, b);
+        a.items[b] = {q.start, q.n_new, q.length, q.before, q.full, b, 0, -1};
+    }
+    __syncthreads();
+    for (int g = wave; g < a.n_groups; g += NT / 64) {
+        const int b0 = a.bounds[g], b1 = a.bounds[g + 1];
+        int least = kPoolMaxLength, first = s.n_seq, end = 0, count = 0;
+        for (int b = b0 + lane; b < b1; b += 64) {
+            const pool_seq q = pool_seq_of(s, b);
+            if (q.n_new == 0) continue;
+            least = min(least, q.before);
+            first = min(first, b);
+            end = max(end, q.start + q.n_new);
+            ++count;
+        }
+        least = wave_min(least);
+        first = wave_min(first);
+        end = -wave_min(-end);
+        count = pool_wave_sum(count);
+        const int common = count > 1 ? min(max(a.shared[g], 0), max(least, 0)) >> s.log_R << s.log_R : 0;            // (uniform)
+        const int start = common > 0 ? pool_seq_of(s, first).start : 0;
+        if (lane == 0) a.items[s.n_seq + g] = {start, common > 0 ? max(end - start, 0) : 0, common, common, common, common > 0 ? first : 0, 0, -1};
+        if (common > 0)
+            for (int b = b0 + lane; b < b1; b += 64) {
+                const pool_seq q = pool_seq_of(s, b);
+                if (q.n_new > 0) a.items[b] = {q.start, q.n_new, q.length - common, q.before - common, q.full - common, b, common >> s.log_R, g};
+            }
+    }
+    __syncthreads();
+}
+
+// units of work in front of each sequence (or item), by one workgroup
+template <int D, int FORM>
+__device__ __forceinline__ void count_units(const pool_attention_args& a) {
+    constexpr int NT = 2 * D, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * kPoolChunkWaves;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if constexpr (FORM == kPoolShared) make_items<NT>(a);
+    const int n_seq = pool_count<FORM>(a);
+    // the sequences' own units first, then their sums in place
+    for (int b = wave; b < n_seq; b += NT / 64) {
+        const pool_seq q = pool_view_of<FORM>(a, b).q;
         const bool decode = pool_is_decode(q, a.group, a.decode_rows);
-        const int chunk = decode || q.n_new == 0 ? 0 : a.heads * pool_chunk_units(q, a.group, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS);
+        const int chunk = decode || q.n_new == 0 ? 0 : a.heads * pool_chunk_units<FORM>(a, q, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS);
         if (lane == 0) {
             if (a.blocks_before) a.blocks_before[b + 1] = decode ? 0 : (q.n_new * a.group + ROWS - 1) / ROWS;
-            a.decode_before[b + 1] = decode ? a.heads * ((q.n_new * a.group + a.decode_block - 1) / a.decode_block) * pool_tiles(q.length, q.full, a.decode_keys) : 0;
+            a.decode_before[b + 1] = decode ? a.heads * ((q.n_new * a.group + a.decode_block - 1) / a.decode_block) * pool_decode_tiles<FORM>(a, q, a.decode_keys) : 0;
             a.chunk_before[b + 1] = chunk;
         }
     }
@@ -37,22 +95,22 @@ __device__ __forceinline__ void count_units(const pool_attention_args& a) {
         int* const at = which == 0 ? a.decode_before : which == 1 ? a.chunk_before : a.blocks_before;
         unsigned sum = 0;
         if (lane == 0) at[0] = 0;
-        for (int b0 = 1; b0 <= s.n_seq; b0 += 64) {
+        for (int b0 = 1; b0 <= n_seq; b0 += 64) {
             const int b = b0 + lane;
-            unsigned x = b <= s.n_seq ? at[b] : 0;
+            unsigned x = b <= n_seq ? at[b] : 0;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
                 const unsigned other = __shfl_up(x, d);
                 if (lane >= d) x = min(x + other, kPoolMostUnits);
             }
             const unsigned before = min(sum + x, kPoolMostUnits);
-            if (b <= s.n_seq) at[b] = b == s.n_seq && before == kPoolMostUnits ? 0 : (int)before;
+            if (b <= n_seq) at[b] = b == n_seq && before == kPoolMostUnits ? 0 : (int)before;
             sum = min(sum + (unsigned)__shfl(x, 63), kPoolMostUnits);
         }
     }
 }
 
-template <int D, int BITS>
+template <int D, int BITS, int FORM>
 __global__ void __launch_bounds__(2 * D) srft_pool_rotate_kernel(const pool_attention_args a) {
     constexpr int G = D / 32, T = D / 16, U = D / 8, ROW = U + 1, NT = 2 * D, ROWS = kTileVecs;
     __shared__ uint4 rows_lds[ROWS * ROW];
@@ -60,7 +118,7 @@ __global__ void __launch_bounds__(2 * D) srft_pool_rotate_kernel(const pool_atte
     __shared__ int shifts[ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
     if (blockIdx.x == 0) {
-        count_units<D>(a);
+        count_units<D, FORM>(a);
         return;
     }
     const bool queries = (int)blockIdx.x <= a.q_grid;
@@ -177,9 +235,13 @@ __global__ void __launch_bounds__(2 * D) srft_pool_rotate_kernel(const pool_atte
     }
 }
 
-template <int D> pool_attention_kernel_t pick(int bits) { return bits == 8 ? srft_pool_rotate_kernel<D, 8> : srft_pool_rotate_kernel<D, 4>; }
-pool_attention_kernel_t dispatch(int d, int bits) { SRFT_DISPATCH_D(d, pick, bits) }
+template <int D, int BITS> pool_attention_kernel_t form_of(int form) {
+    return form == kPoolShared ? srft_pool_rotate_kernel<D, BITS, kPoolShared>
+           : form == kPoolSliding ? srft_pool_rotate_kernel<D, BITS, kPoolSliding> : srft_pool_rotate_kernel<D, BITS, kPoolCausal>;
+}
+template <int D> pool_attention_kernel_t pick(int bits, int form) { return bits == 8 ? form_of<D, 8>(form) : form_of<D, 4>(form); }
+pool_attention_kernel_t dispatch(int d, int bits, int form) { SRFT_DISPATCH_D(d, pick, bits, form) }
 
 }  // namespace
 
-pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits) { return dispatch(d, bits); }
+pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits, int form) { return dispatch(d, bits, form); }

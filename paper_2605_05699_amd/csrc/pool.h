@@ -11,7 +11,7 @@ struct srft_pool {
     srft_pool_buffers k = {}, v = {};
     int heads = 0, R = 0, log_R = 0;
     int n_pages = 0, n_windows = 0;
-    int decode_blocks[2] = {1, 1};          // workgroups of pool_decode that a compute unit holds, for one and two blocks of rows
+    int decode_blocks[3][2] = {};           // workgroups of pool_decode that a compute unit holds: by form, for one and two blocks of rows
     uint4* tables = nullptr;                // device: the matrices of the queries and of the outputs (pool_attention.hip)
     float q_unscale = 1.0f, out_unscale = 1.0f;     // 2^-e of their scaling
     int units() const { return plan_k->d / 8; }             // 16-byte units of an fp16 row

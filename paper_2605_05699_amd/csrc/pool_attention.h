@@ -17,6 +17,12 @@
 // serves a whole row), the output's own rounding to fp16 included.  Sums, maxima and exponents are fp32.  None of the operands can leave fp16's range: q' has a power of two per
 // row, w a running one taken from the scales, the weights are at most 2^(kLazy + kHigh) in pool_chunk, and times a scale 2^(kLazy + 7) in pool_decode.
 //
+// Forms.  Causal: srft_pool_attention.  Sliding: rows see the last `recent` tokens and the first `sinks` ones; of a block's tiles those between its
+// sinks and its first row's recent tokens are left out (pool_gap), what is left is numbered through.  Shared: sequences that have pages in
+// common are taken apart into items: what a sequence has of its own, which is a sequence whose first page lies further along its table, and,
+// for each group, the tokens in common with the rows of all of its sequences, which all see all of them.  Both leave unfinished sums, and the
+// merge joins them (pool_item, joint_rows).
+//
 // Order of channels.  A dword of codes is decoded into eight fp16 values in the order 0 4 1 5 2 6 3 7 (4 bits; 0 2 1 3 at 8 bits), so
 // all operands have their channels in that order within units of eight ("positions"), q' by the way it is stored, the output by the
 // order of the columns of its matrix.
@@ -38,6 +44,15 @@ constexpr int pool_decode_keys(int d, int cb) { return d <= 128 && cb == 1 ? 64 
 constexpr int kPoolBlock = 32;                               // rows of a wavefront
 template <int D> constexpr int kPoolChunkKeys = D <= 128 ? 64 : 32;
 constexpr int kPoolChunkWaves = 8;
+
+enum { kPoolCausal = 0, kPoolSliding = 1, kPoolShared = 2, kPoolForms = 3 };
+// What the kernels of the shared form take for a sequence: first the sequences' own tokens, items 0 .. n_seq - 1, then the groups' in common.
+struct pool_item {
+    int start, n_new, length, before, full;                  // as pool_seq, without the tokens in front of first_page
+    int seq, first_page;                                     // whose page table and windows; the first page of the item in it
+    int group;                                               // the group that a sequence shares pages with, or -1
+};
+static_assert(sizeof(pool_item) == 32, "two loads");
 
 struct pool_attention_args {
     pool_seqs s;
@@ -64,6 +79,14 @@ struct pool_attention_args {
     int decode_rows, decode_block, decode_keys;              // rows that go to pool_decode, those of a workgroup, keys of its tiles
     int decode_merges;                                       // workgroups of pool_merge that merge what pool_decode left
     unsigned merges;                                         // all of them (srft_grid)
+    int recent, sinks;                                       // sliding
+    const int *groups, *shared;                              // shared: the caller's
+    int n_groups, bits;
+    int merge_groups;                                        // the merge is of the tokens in common, into joint_rows[1]
+    int* bounds;                                             // [n_groups + 1]: groups, ascending and within n_seq (workspace)
+    pool_item* items;                                        // [n_seq + n_groups] (workspace)
+    float *joint_rows[2], *joint_heads[2];                   // [n_new][n_q_heads][D] and [4]: sums by channel and maximum, sum of weights, exponent of own
+                                                             // tokens that one workgroup has had whole, and of those in common (workspace)
 };
 // Sums of a block of 32 rows that a segment leaves: [D / 8 float4][64 lanes], then per lane maximum, sum of weights and V's exponent.
 template <int D> constexpr int kPoolPart = 32 * D + 3 * 64;
@@ -82,6 +105,74 @@ __device__ __forceinline__ bool pool_is_decode(const pool_seq& q, int group, int
 __device__ __forceinline__ int pool_seen(const pool_seq& q, int group, int rows, int rt) {
     return q.before + (min((rt + 1) * rows, q.n_new * group) - 1) / group + 1;
 }
+// Tiles that a block of rows leaves out: `skip` of them from tile `begin` on.  (Sliding; none in the other forms.)
+template <int FORM> struct pool_gap {
+    int begin = 0, skip = 0;
+    __device__ __forceinline__ int tile(int t) const {       // which tile of the sequence is the block's t-th
+        if constexpr (FORM == kPoolSliding) return t < begin ? t : t + skip;
+        return t;
+    }
+    __device__ __forceinline__ int in_pages(int page_tiles) const {          // how many of them are of pages
+        if constexpr (FORM == kPoolSliding) return max(min(begin + skip, page_tiles) - min(begin, page_tiles), 0);
+        return 0;
+    }
+    int low = 0, sinks = 0;
+    // Whether no row of the block sees one of the 16 keys from `key` on: they are as if their page did not exist (what is in it need not be numbers).
+    __device__ __forceinline__ bool hides(int key) const {
+        if constexpr (FORM == kPoolSliding) return key + 16 <= low && key >= sinks;
+        return false;
+    }
+};
+// first: the block's first row's token (or an earlier one); seen: the tokens that its last row sees
+template <int FORM>
+__device__ __forceinline__ pool_gap<FORM> pool_gap_of(const pool_attention_args& a, const pool_seq& q, int first, int seen, int keys) {
+    pool_gap<FORM> g;
+    if constexpr (FORM == kPoolSliding) {
+        g.low = max(first - a.recent + 1, 0);
+        g.sinks = a.sinks;
+        g.begin = pool_tiles(min(a.sinks, seen), q.full, keys);
+        g.skip = max((g.low < q.full ? g.low / keys : (q.full + keys - 1) / keys + (g.low - q.full) / keys) - g.begin, 0);
+    }
+    return g;
+}
+// tokens that the rows of block rt of pool_chunk see at most, and the tiles that it leaves out
+template <int FORM>
+__device__ __forceinline__ int pool_chunk_seen(const pool_attention_args& a, const pool_seq& q, int rows, int rt) {
+    const int seen = pool_seen(q, a.group, rows, rt);
+    return FORM == kPoolShared ? min(seen, q.length) : seen;
+}
+template <int FORM>
+__device__ __forceinline__ pool_gap<FORM> pool_chunk_gap(const pool_attention_args& a, const pool_seq& q, int rows, int keys, int rt) {
+    return pool_gap_of<FORM>(a, q, q.before + rt * rows / a.group, pool_chunk_seen<FORM>(a, q, rows, rt), keys);
+}
+template <int FORM>
+__device__ __forceinline__ int pool_chunk_tiles(const pool_attention_args& a, const pool_seq& q, int rows, int keys, int rt) {
+    return pool_tiles(pool_chunk_seen<FORM>(a, q, rows, rt), q.full, keys) - pool_chunk_gap<FORM>(a, q, rows, keys, rt).skip;
+}
+// the same of pool_decode, whose blocks of a sequence have all the same tiles
+template <int FORM>
+__device__ __forceinline__ pool_gap<FORM> pool_decode_gap(const pool_attention_args& a, const pool_seq& q, int keys) {
+    return pool_gap_of<FORM>(a, q, q.before, q.length, keys);
+}
+template <int FORM>
+__device__ __forceinline__ int pool_decode_tiles(const pool_attention_args& a, const pool_seq& q, int keys) {
+    return pool_tiles(q.length, q.full, keys) - pool_decode_gap<FORM>(a, q, keys).skip;
+}
+// A sequence, or item, of a call.
+struct pool_view {
+    pool_seq q;
+    int seq, first_page;
+    bool joint;                                              // its sums are joined with others: they are left unfinished
+};
+template <int FORM> __device__ __forceinline__ int pool_count(const pool_attention_args& a) { return FORM == kPoolShared ? a.s.n_seq + a.n_groups : a.s.n_seq; }
+template <int FORM>
+__device__ __forceinline__ pool_view pool_view_of(const pool_attention_args& a, int i) {
+    if constexpr (FORM == kPoolShared) {
+        const pool_item t = a.items[i];
+        return {{t.start, t.n_new, t.length, t.before, t.full}, t.seq, t.first_page, i >= a.s.n_seq || t.group >= 0};
+    }
+    return {pool_seq_of(a.s, i), i, 0, false};
+}
 // sum over the lanes of a wavefront, in all of them
 __device__ __forceinline__ int pool_wave_sum(int x) {
 #pragma unroll
@@ -89,9 +180,10 @@ __device__ __forceinline__ int pool_wave_sum(int x) {
     return x;
 }
 // tiles of the blocks of rows 0 .. n - 1 of one key head (by the whole wavefront)
-__device__ __forceinline__ int pool_chunk_units(const pool_seq& q, int group, int rows, int keys, int n) {
+template <int FORM>
+__device__ __forceinline__ int pool_chunk_units(const pool_attention_args& a, const pool_seq& q, int rows, int keys, int n) {
     int sum = 0;
-    for (int rt = threadIdx.x & 63; rt < n; rt += 64) sum += pool_tiles(pool_seen(q, group, rows, rt), q.full, keys);
+    for (int rt = threadIdx.x & 63; rt < n; rt += 64) sum += pool_chunk_tiles<FORM>(a, q, rows, keys, rt);
     return pool_wave_sum(sum);
 }
 // The workgroups that take part, and where the share of workgroup w begins: the first `more` have a unit more than the others.
@@ -215,6 +307,25 @@ template <int D> struct pool_block {
 #pragma unroll
         for (int b = 0; b < D / 32; ++b) sums[b] *= f;
     }
+    // Four positions of the lane's row, 4 (l / 32) on in unit u of eight, to and from the row's channels (see "Order of channels").
+    static __device__ __forceinline__ void put4(float* row, int u, int half, floatx4 x, int bits) {
+        typedef float pair __attribute__((ext_vector_type(2)));
+        if (bits == 8) {
+            *reinterpret_cast<floatx4*>(row + 8 * u + 4 * half) = floatx4{x[0], x[2], x[1], x[3]};
+        } else {
+            *reinterpret_cast<pair*>(row + 8 * u + 2 * half) = pair{x[0], x[2]};
+            *reinterpret_cast<pair*>(row + 8 * u + 2 * half + 4) = pair{x[1], x[3]};
+        }
+    }
+    static __device__ __forceinline__ floatx4 get4(const float* row, int u, int half, int bits) {
+        typedef float pair __attribute__((ext_vector_type(2)));
+        if (bits == 8) {
+            const floatx4 x = *reinterpret_cast<const floatx4*>(row + 8 * u + 4 * half);
+            return floatx4{x[0], x[2], x[1], x[3]};
+        }
+        const pair x = *reinterpret_cast<const pair*>(row + 8 * u + 2 * half), y = *reinterpret_cast<const pair*>(row + 8 * u + 2 * half + 4);
+        return floatx4{x[0], y[0], x[1], y[1]};
+    }
     // p: kPoolPart<D> floats in memory or LDS
     __device__ __forceinline__ void put(float* p, int lane) const {
 #pragma unroll
@@ -333,10 +444,17 @@ __device__ __forceinline__ pool_row pool_row_of(const pool_seq& q, int key_head,
 }
 
 typedef void (*pool_attention_kernel_t)(const pool_attention_args);
-pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits);
+// (one translation unit for each form of the scans)
+pool_attention_kernel_t srft_pick_pool_rotate(int d, int bits, int form);
 pool_attention_kernel_t srft_pick_pool_decode_b4(int d, int cb, int gm);
 pool_attention_kernel_t srft_pick_pool_decode_b8(int d, int cb, int gm);
+pool_attention_kernel_t srft_pick_pool_decode_sliding_b4(int d, int cb, int gm);
+pool_attention_kernel_t srft_pick_pool_decode_sliding_b8(int d, int cb, int gm);
+pool_attention_kernel_t srft_pick_pool_decode_shared_b4(int d, int cb, int gm);
+pool_attention_kernel_t srft_pick_pool_decode_shared_b8(int d, int cb, int gm);
 pool_attention_kernel_t srft_pick_pool_chunk(int d, int bits);
-pool_attention_kernel_t srft_pick_pool_merge(int d, int cb);
+pool_attention_kernel_t srft_pick_pool_chunk_sliding(int d, int bits);
+pool_attention_kernel_t srft_pick_pool_chunk_shared(int d, int bits);
+pool_attention_kernel_t srft_pick_pool_merge(int d, int cb, int form);
 
 #endif  // SRFT_POOL_ATTENTION_H

@@ -170,7 +170,7 @@ constexpr int pool_decode_waves(int d, int bits, int cb, int gm) {
 // Whether a segment's first tile is asked for before its queries are in LDS (4 bits, groups of 32, with / without: d = 64 84 / 85, 96 104 / 107,
 // 160 147 / 148).  Not where the registers are full: at d = 128 one wavefront is left with it (149 / 123), nor above 160 (256: 209 -> 291 when it was tried).
 constexpr bool pool_decode_early(int d, int bits, int cb, int gm) { return pool_decode_waves(d, bits, cb, gm) == 1 && d <= 160 && d != 128; }
-template <int D, int BITS, int CB, int GM>
+template <int D, int BITS, int CB, int GM, int FORM>
 __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB, GM)) srft_pool_decode_kernel(const pool_attention_args a) {
     using P = pool_decode<D, BITS, CB, GM>;
     constexpr bool FINE = P::FINE;
@@ -181,8 +181,8 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quarter = lane >> 4;
     // The first segment's sequence: where the sequences fit the lanes, all that it takes comes with one round of loads (a step of 4
     // sequences up to 1000 tokens: 12.6 us with this and with the first tile's loads before the queries are in LDS, 13.5 to 14 one after the other).
-    const int n_seq = a.s.n_seq;
-    const bool few = n_seq < 64;
+    const int n_seq = pool_count<FORM>(a);
+    const bool few = FORM != kPoolShared && n_seq < 64;
     int of_before = 0, of_start = 0, of_length = 0;          // lane b: of sequence b
     if (few) {
         of_before = a.decode_before[min(lane, n_seq)];
@@ -195,15 +195,17 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
     if (total == 0 || w >= shares.groups) return;            // (uniform)
     const int end = shares.begin(w + 1);
     int unit = shares.begin(w), seq, units_before;
-    pool_seq q;
+    pool_view view{};
+    pool_seq& q = view.q;
     if (few) {
         seq = min((int)__popcll(__ballot(lane <= n_seq && of_before <= unit)) - 1, n_seq - 1);
         units_before = __builtin_amdgcn_readlane(of_before, seq);
-        q = pool_seq_from(a.s, __builtin_amdgcn_readlane(of_start, seq), __builtin_amdgcn_readlane(of_start, seq + 1), __builtin_amdgcn_readlane(of_length, seq));
+        view = {pool_seq_from(a.s, __builtin_amdgcn_readlane(of_start, seq), __builtin_amdgcn_readlane(of_start, seq + 1), __builtin_amdgcn_readlane(of_length, seq)),
+                seq, 0, false};
     } else {
         seq = __builtin_amdgcn_readfirstlane(pool_sequence_of(a.decode_before, n_seq, unit));
         units_before = a.decode_before[seq];
-        q = pool_seq_of(a.s, seq);
+        view = pool_view_of<FORM>(a, seq);
     }
     const int R = 1 << a.s.log_R, n_scales = D / a.g;
     unsigned char* const kt = lds + wave * P::WAVE_BYTES;    // this wavefront's keys, and then values, and scales
@@ -232,20 +234,22 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
         if (!at_begin) {
             while (seq + 1 < n_seq && a.decode_before[seq + 1] <= unit) ++seq;
             units_before = a.decode_before[seq];
-            q = pool_seq_of(a.s, seq);
+            view = pool_view_of<FORM>(a, seq);
         }
-        const int tiles = pool_tiles(q.length, q.full, KEYS), page_tiles = (q.full + KEYS - 1) / KEYS, tail = q.length - q.full;
+        const pool_gap<FORM> gap = pool_decode_gap<FORM>(a, q, KEYS);
+        const int all_page_tiles = (q.full + KEYS - 1) / KEYS, page_tiles = all_page_tiles - gap.in_pages(all_page_tiles), tail = q.length - q.full;
+        const int tiles = pool_tiles(q.length, q.full, KEYS) - gap.skip;
         const int rel = unit - units_before, item = rel / tiles, t0 = rel - item * tiles, t1 = min(tiles, t0 + end - unit);
         const int blocks_of_rows = (q.n_new * a.group + 16 * CB - 1) / (16 * CB), head = item / blocks_of_rows, r0 = 16 * CB * (item - head * blocks_of_rows);
         if (t1 <= t0) return;                                // (only if the device arrays were written during the call)
-        const int32_t* const table = a.s.table + seq * a.s.max_pages;
+        const int32_t* const table = a.s.table + view.seq * a.s.max_pages + view.first_page;
         const int last_page_tile = min(t1, page_tiles) - 1;
         int t = t0 + wave;
         u32x4 kc[NV], vc[NV];
         pool_floats<NH> kf, vf;
         // pages of the tile's blocks of 16 keys (lane i: block i % (KEYS / 16)); behind the last page, the last block again
         const auto page_of = [&](int tile) __attribute__((always_inline)) {
-            return table[min(tile * KEYS + 16 * (lane & (KEYS / 16 - 1)), q.full - 16) >> a.s.log_R];
+            return table[min(gap.tile(tile) * KEYS + 16 * (lane & (KEYS / 16 - 1)), q.full - 16) >> a.s.log_R];
         };
         uint32_t there = 0;
         uint64_t c0 = 0, c1 = 0, c2 = 0, c3 = 0;         // blocks' codes
@@ -264,8 +268,8 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
             uint32_t known = 0;
             uint64_t f0, f1, f2 = 0, f3 = 0;
             const auto address = [&](int i, uint64_t& code, uint64_t& scale) __attribute__((always_inline)) {
-                const int page = __builtin_amdgcn_readlane(pages, i), slot = min(tile * KEYS + 16 * i, q.full - 16) & (R - 1);
-                const bool ok = pool_there(page, a.s.n_pages);
+                const int page = __builtin_amdgcn_readlane(pages, i), slot = min(gap.tile(tile) * KEYS + 16 * i, q.full - 16) & (R - 1);
+                const bool ok = pool_there(page, a.s.n_pages) && !gap.hides(gap.tile(tile) * KEYS + 16 * i);
                 known |= (ok ? 1u : 0u) << i;
                 const uint64_t row = ((uint64_t)((ok ? page : 0) * (uint64_t)a.heads + head) << a.s.log_R) + slot;
                 code = row * CBY;
@@ -346,7 +350,16 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
 #pragma unroll
             for (int c = 0; c < CB; ++c) {
                 const int last = min(row[c].last, last_key) - first_key;
-                if (__ballot(last < KEYS - 1) || blocks != (1u << (KEYS / 16)) - 1) {
+                const int from = row[c].last - a.recent + 1 - first_key, sinks = a.sinks - first_key;        // (sliding: the row's first recent token, the sinks' end)
+                if (FORM == kPoolSliding && __ballot(from > 0)) {
+#pragma unroll
+                    for (int b = 0; b < BK; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = key_of(b, i);
+                            p[c][b][i] = key <= last && (key >= from || key < sinks) && (blocks >> (key >> 4) & 1) ? p[c][b][i] : -__builtin_inff();
+                        }
+                } else if (__ballot(last < KEYS - 1) || blocks != (1u << (KEYS / 16)) - 1) {
 #pragma unroll
                     for (int b = 0; b < BK; ++b)
 #pragma unroll
@@ -451,7 +464,7 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
                 fetch_values();
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_sched_barrier(0);           // (the values' operands are formed as they are used, not all ahead)
-                weights([&](int b, int i) { return KQ * quarter + 4 * b + i; }, t * KEYS, q.full - 1, blocks, e, first);
+                weights([&](int b, int i) { return KQ * quarter + 4 * b + i; }, gap.tile(t) * KEYS, q.full - 1, blocks, e, first);
                 first = false;
                 // ---- values: channels on the rows; step s takes keys 8 s .. 8 s + 7 of every quarter, in the order of decoded codes
 #pragma unroll
@@ -503,9 +516,9 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
         // of the tile here; those behind the last token are passed over.  Loads are unconditional (behind the last token, of it
         // again: its weights there are zero), so that a block's are on their way together.
         for (; t < t1; t += W) {
-            if (!pool_there(a.s.windows[2 * seq + 1], a.s.n_windows)) break;             // (uniform)
-            const int key0 = (t - page_tiles) * KEYS, held = tail - key0;                // slot of the tile's first token; tokens from there on
-            const long long of_k = (long long)(seq * a.heads + head) << a.s.log_R, of_v = of_k + ((long long)a.s.n_seq * a.heads << a.s.log_R);
+            if (!pool_there(a.s.windows[2 * view.seq + 1], a.s.n_windows)) break;             // (uniform)
+            const int key0 = (gap.tile(t) - all_page_tiles) * KEYS, held = tail - key0;                // slot of the tile's first token; tokens from there on
+            const long long of_k = (long long)(view.seq * a.heads + head) << a.s.log_R, of_v = of_k + ((long long)a.s.n_seq * a.heads << a.s.log_R);
             float fv[BK][4], most = 0.0f;
 #pragma unroll
             for (int b = 0; b < BK; ++b) {
@@ -558,7 +571,7 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
                     for (int x = 0; x < 8; ++x) pw[c][x] = (_Float16)(p[c][2 * s + x / 4][x % 4] * (fv[2 * s + x / 4][x % 4] * up));
                 // four tokens each of two blocks, next to each other in [channel][R]; past the last token, those that hold it
                 const int slot0 = min(key0 + 32 * s + 4 * quarter, (tail - 1) & ~3), slot1 = min(key0 + 32 * s + 16 + 4 * quarter, (tail - 1) & ~3);
-                const unsigned short* const at = a.tail_columns + (((long long)seq * a.heads + head) * D + l16 << a.s.log_R);
+                const unsigned short* const at = a.tail_columns + (((long long)view.seq * a.heads + head) * D + l16 << a.s.log_R);
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
                     const uint2 x = *reinterpret_cast<const uint2*>(at + (16 * n << a.s.log_R) + slot0), y = *reinterpret_cast<const uint2*>(at + (16 * n << a.s.log_R) + slot1);
@@ -612,7 +625,16 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
                     }
             }
             __syncthreads();
-            if (whole) {
+            if (FORM == kPoolShared && whole && view.joint) {            // to be joined with others: by rows
+                if (row[c].there) {
+                    const int which = seq >= a.s.n_seq;
+                    const long long at = (long long)row[c].token * (a.heads * a.group) + row[c].head;
+#pragma unroll
+                    for (int i = 0; i < kPoolOwn<D>; ++i)
+                        if (wave + W * i < NB) *reinterpret_cast<floatx4*>(a.joint_rows[which] + at * D + 16 * (wave + W * i) + 4 * quarter) = mine[i];
+                    if (wave == 0 && quarter == 0) reinterpret_cast<floatx4*>(a.joint_heads[which])[at] = floatx4{t_all, d_all, __uint_as_float((uint32_t)e_all), 0.0f};
+                }
+            } else if (whole) {
                 char* const dst = row[c].there ? a.out + row[c].token * a.out_token + row[c].head * a.out_head : nullptr;
                 pool_finish16<D, false>(mine, d_all, e_all, lds, a.out_table16, a.out_unscale, dst, a.bf16, wave, lane);
             } else {
@@ -635,17 +657,19 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
 // The parts of a key head's rows that went to several workgroups, in the order of the keys; rows of sequences without a tile are zero.  One
 // workgroup of four wavefronts per sequence and key head, each with a quarter of the channels, all parts of them on their way at once
 // (up to AHEAD).
-template <int D, int CB>
+template <int D, int CB, int FORM>
 __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, unsigned block, unsigned char* lds) {
     constexpr int NB = D / 16, W = kPoolTeam, AHEAD = 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int all = (a.decode_rows + 16 * CB - 1) / (16 * CB), at = (int)(block / (unsigned)all), rb = (int)block - at * all;
-    const int seq = at / a.heads, head = at - seq * a.heads;
-    const int units = a.decode_before[a.s.n_seq], units_before = a.decode_before[seq];       // (with the sequence's, in one round of loads)
-    const pool_seq q = pool_seq_of(a.s, seq);
+    const bool groups = FORM == kPoolShared && a.merge_groups;
+    const int seq = at / a.heads + (groups ? a.s.n_seq : 0), head = at - at / a.heads * a.heads;
+    const int units = a.decode_before[pool_count<FORM>(a)], units_before = a.decode_before[seq];     // (with the sequence's, in one round of loads)
+    const pool_view view = pool_view_of<FORM>(a, seq);
+    const pool_seq& q = view.q;
     const int rows = q.n_new * a.group, blocks_of_rows = (rows + 16 * CB - 1) / (16 * CB);
     if (rows == 0 || !pool_is_decode(q, a.group, a.decode_rows) || rb >= blocks_of_rows) return;
-    const int tiles = pool_tiles(q.length, q.full, a.decode_keys);
+    const int tiles = pool_decode_tiles<FORM>(a, q, a.decode_keys);
     if (tiles == 0) {
         for (int i = threadIdx.x + rb * 16 * CB * (D / 8); i < min(rows, (rb + 1) * 16 * CB) * (D / 8); i += 64 * W) {
             const pool_row r = pool_row_of(q, head, a.group, i / (D / 8));
@@ -656,7 +680,7 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
     if (units == 0) return;                                  // (too many of them: see kPoolMostUnits)
     const pool_shares shares(units, a.decode_grid, W);
     const int first = units_before + (head * blocks_of_rows + rb) * tiles, w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
-    if (w0 == w1) return;
+    if (w0 == w1 && (!view.joint || groups)) return;
     const int behind = shares.begin(w0) != first ? 1 : 0;    // the first part's workgroup began with other rows
     const auto part = [&](int w, int c) __attribute__((always_inline)) {
         return a.decode_parts + ((2LL * w + (w == w0 ? behind : 0)) * CB + c) * kPoolPart16<D>;
@@ -667,7 +691,27 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
         floatx4 o[kPoolOwn<D>];
 #pragma unroll
         for (int i = 0; i < kPoolOwn<D>; ++i) o[i] = floatx4{0, 0, 0, 0};
-        for (int v = w0; v <= w1; v += AHEAD) {              // (one round of loads for AHEAD parts, the sums so far brought under their maximum)
+        const pool_row r = pool_row_of(q, head, a.group, (rb * CB + c) * 16 + (lane & 15));
+        const long long r_at = (long long)r.token * (a.heads * a.group) + r.head;
+        if (FORM == kPoolShared && view.joint && !groups) {
+            // the rows' sums over the tokens in common, and over their own where one workgroup has had all of these
+            floatx4 x[2][kPoolOwn<D>], head4[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int which = k == 0 || w0 != w1 ? 1 : 0;
+                head4[k] = reinterpret_cast<const floatx4*>(a.joint_heads[which])[r_at];
+#pragma unroll
+                for (int i = 0; i < kPoolOwn<D>; ++i)
+                    x[k][i] = *reinterpret_cast<const floatx4*>(a.joint_rows[which] + r_at * D + 16 * min(wave + W * i, NB - 1) + 4 * (lane >> 4));
+            }
+            pool_part_head h[2] = {{head4[0][0], head4[0][1], head4[0][2], 0.0f}, {head4[1][0], head4[1][1], head4[1][2], 0.0f}};
+            pool_join(t_all, den, e_all, h, 0, w0 == w1 ? 1 : 0);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < kPoolOwn<D>; ++i) o[i] += x[k][i] * h[k].factor;
+        }
+        for (int v = w0; v <= w1 && (FORM != kPoolShared || w0 != w1); v += AHEAD) {              // (one round of loads for AHEAD parts, the sums so far brought under their maximum)
             floatx4 x[AHEAD][kPoolOwn<D>];
             pool_part_head h[AHEAD];
 #pragma unroll
@@ -685,23 +729,31 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
 #pragma unroll
                 for (int i = 0; i < kPoolOwn<D>; ++i) o[i] += x[k][i] * h[k].factor;
         }
-        const pool_row r = pool_row_of(q, head, a.group, (rb * CB + c) * 16 + (lane & 15));
+        if (FORM == kPoolShared && groups) {                 // (uniform)
+            if (r.there) {
+#pragma unroll
+                for (int i = 0; i < kPoolOwn<D>; ++i)
+                    if (wave + W * i < NB) *reinterpret_cast<floatx4*>(a.joint_rows[1] + r_at * D + 16 * (wave + W * i) + 4 * (lane >> 4)) = o[i];
+                if (wave == 0 && lane < 16) reinterpret_cast<floatx4*>(a.joint_heads[1])[r_at] = floatx4{t_all, den, __uint_as_float((uint32_t)e_all), 0.0f};
+            }
+            continue;
+        }
         char* const dst = r.there ? a.out + r.token * a.out_token + r.head * a.out_head : nullptr;
         if (c > 0) __syncthreads();
         pool_finish16<D, true>(o, den, e_all, lds, a.out_table16, a.out_unscale, dst, a.bf16, wave, lane);
     }
 }
 
-template <int D, int BITS, int CB>
+template <int D, int BITS, int CB, int FORM>
 pool_attention_kernel_t pool_pick_decode_groups(int gm) {
-    return gm == kGroup16 ? srft_pool_decode_kernel<D, BITS, CB, kGroup16>
-           : gm == kGroupWide ? srft_pool_decode_kernel<D, BITS, CB, kGroupWide> : srft_pool_decode_kernel<D, BITS, CB, kGroup32>;
+    return gm == kGroup16 ? srft_pool_decode_kernel<D, BITS, CB, kGroup16, FORM>
+           : gm == kGroupWide ? srft_pool_decode_kernel<D, BITS, CB, kGroupWide, FORM> : srft_pool_decode_kernel<D, BITS, CB, kGroup32, FORM>;
 }
-template <int D, int BITS>
+template <int D, int BITS, int FORM>
 pool_attention_kernel_t pool_pick_decode(int cb, int gm) {
     if constexpr (D <= 128)
-        if (cb == 2) return pool_pick_decode_groups<D, BITS, 2>(gm);
-    return pool_pick_decode_groups<D, BITS, 1>(gm);
+        if (cb == 2) return pool_pick_decode_groups<D, BITS, 2, FORM>(gm);
+    return pool_pick_decode_groups<D, BITS, 1, FORM>(gm);
 }
 
 #endif  // SRFT_POOL_DECODE_H

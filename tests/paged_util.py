@@ -99,10 +99,10 @@ class Serving:
     def Q(self):
         return O.hadamard_matrix(self.d) if self.transform == "hadamard" else O.srft_matrix(self.d)
 
-    def attention(self, q, new, scale, group, step, there=None):
+    def attention(self, q, new, scale, group, step, there=None, hidden=None):
         """(out, bound) for q [n_new, heads * group, d] (fp64 values): the definition, and how far a kernel may be from it that rounds
         q', code scales, dequantized codes and weights to fp16 and the result with half a step of `step`.  there[b]: mask of the tokens
-        that exist."""
+        that exist.  hidden(rows' tokens, tokens): what rows do not see although it is theirs."""
         out, err = np.zeros(q.shape), np.zeros(q.shape)
         rk, rv, u, at = self.inverse(0), self.inverse(1), 2.0 ** -11, 0
         for b, t in enumerate(new):
@@ -112,6 +112,8 @@ class Serving:
                 rows = q[at: at + t, h * group: (h + 1) * group].reshape(-1, self.d)
                 limit = np.repeat(np.arange(n - t, n), group)
                 see = np.arange(n)[None] <= limit[:, None]
+                if hidden is not None:
+                    see &= ~hidden(limit[:, None], np.arange(n)[None])
                 if there is not None:
                     see &= there[b][None, :n]
                 k, v = np.where(np.isfinite(wk[:, h]), wk[:, h], 0.0), np.where(np.isfinite(wv[:, h]), wv[:, h], 0.0)
