@@ -15,11 +15,9 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     constexpr int BLOCKS = kPoolChunkWaves, ROWS = kPoolBlock * BLOCKS, KEYS = kPoolChunkKeys<D>, G = D / 32, T = D / 16, OWN = (G + kPoolTeam - 1) / kPoolTeam, AHEAD = 2;
     // ops: [k-step][hi, lo][lane]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int of = (int)(workgroup / BLOCKS), block = (int)workgroup - of * BLOCKS, head = of - of / a.heads * a.heads;
-    const bool groups = FORM == kPoolShared && a.merge_groups;
-    const int n_seq = groups ? a.s.n_seq + a.n_groups : a.s.n_seq, at = of / a.heads + (groups ? a.blocks_before[a.s.n_seq] : 0);
-    if (at >= a.blocks_before[n_seq]) return;
-    const int seq = n_seq == 1 ? 0 : __builtin_amdgcn_readfirstlane(pool_sequence_of(a.blocks_before, n_seq, at)), rt = at - a.blocks_before[seq];
+    const int of = (int)(workgroup / BLOCKS), block = (int)workgroup - of * BLOCKS, at = of / a.heads, head = of - at * a.heads;
+    if (at >= a.blocks_before[a.s.n_seq]) return;
+    const int seq = a.s.n_seq == 1 ? 0 : __builtin_amdgcn_readfirstlane(pool_sequence_of(a.blocks_before, a.s.n_seq, at)), rt = at - a.blocks_before[seq];
     const pool_view view = pool_view_of<FORM>(a, seq);
     const pool_seq& q = view.q;
     const int r0 = rt * ROWS + block * kPoolBlock;
@@ -37,10 +35,11 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     if (units == 0) return;                                  // (too many of them: see kPoolMostUnits)
     const int first = before[seq] + head * pool_chunk_units<FORM>(a, q, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS) +
                       pool_chunk_units<FORM>(a, q, ROWS, KEYS, rt);
-    const pool_shares shares(units, a.chunk_grid, 1);
-    const int w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
-    if (w0 == w1 && (!view.joint || groups)) return;
-    const int behind = shares.begin(w0) != first ? 1 : 0;    // the first part's workgroup began with other rows
+    const pool_shares shares(units, a.chunk_grid, kPoolChunkLeast<FORM>);
+    const int w0 = shares.owner(first + kPoolChunkStart<FORM>), w1 = shares.owner(first + pool_chunk_cost<FORM>(tiles) - 1);
+    const bool joint = FORM == kPoolShared && view.group >= 0;
+    if (w0 == w1 && !joint) return;
+    const int behind = shares.begin(w0) < first ? 1 : 0;    // the first part's workgroup began with other rows
     const auto part = [&](int w) __attribute__((always_inline)) {
         return a.chunk_parts + ((2LL * w + (w == w0 ? behind : 0)) * BLOCKS + block) * kPoolPart<D>;
     };
@@ -49,34 +48,17 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     floatx16 sums[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i) sums[i] = floatx16{0};
-    const long long r_at = (long long)row.token * (a.heads * a.group) + row.head;
-    if (FORM == kPoolShared && view.joint && !groups) {
-        // the rows' sums over the tokens in common, and over their own where one workgroup has had all of these
-        for (int k = 1; k >= (w0 == w1 ? 0 : 1); --k) {
-            const floatx4 x = reinterpret_cast<const floatx4*>(a.joint_heads[k])[r_at];
-            pool_part_head h[1] = {{x[0], x[1], x[2], 0.0f}};
-            const float before = pool_join(t_all, den, e_all, h, 0, 0);
-#pragma unroll
-            for (int i = 0; i < OWN; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const floatx4 y = pool_block<D>::get4(a.joint_rows[k] + r_at * D, 4 * min(wave + kPoolTeam * i, G - 1) + j, half, a.bits);
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) sums[i][4 * j + m] = fmaf(y[m], h[0].factor, sums[i][4 * j + m] * before);
-                }
-        }
-    }
-    for (int v = w0; v <= w1 && (FORM != kPoolShared || w0 != w1); v += AHEAD) {
+    // parts v .. v + AHEAD - 1, up to w1, whose heads and sums (four of them: number n of the lane's) `heads` and `four` give
+    const auto join = [&](int v, int w1, auto heads, auto four) __attribute__((always_inline)) {
         floatx4 x[AHEAD][OWN][4];
         pool_part_head h[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const float* const p = part(min(v + k, w1));
-            h[k].load(p + 32 * D, lane);
+            heads(min(v + k, w1), h[k]);
 #pragma unroll
             for (int i = 0; i < OWN; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[k][i][j] = reinterpret_cast<const floatx4*>(p)[(4 * min(wave + kPoolTeam * i, G - 1) + j) * 64 + lane];
+                for (int j = 0; j < 4; ++j) x[k][i][j] = four(min(v + k, w1), 4 * min(wave + kPoolTeam * i, G - 1) + j);
         }
         const float before = pool_join(t_all, den, e_all, h, v, w1);
 #pragma unroll
@@ -89,19 +71,54 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int m = 0; m < 4; ++m) sums[i][4 * j + m] = fmaf(x[k][i][j][m], h[k].factor, sums[i][4 * j + m]);
-    }
-    if (FORM == kPoolShared && groups) {                     // (uniform)
-        if (!row.there) return;
+    };
+    if (joint) {
+        const long long r_at = (long long)row.token * (a.heads * a.group) + row.head;
+        // rows whose tokens (own: 0, in common: 1) one workgroup has had all of; the others as they are
+        const auto whole = [&](int which, bool in) __attribute__((always_inline)) {
+            const floatx4 x = reinterpret_cast<const floatx4*>(a.joint_heads[which])[r_at];
+            pool_part_head h[1] = {{x[0], x[1], x[2], 0.0f}};
+            if (!in) h[0] = {kPoolLowest, 0.0f, __uint_as_float((uint32_t)kPoolNoExponent), 0.0f};
+            const float before = pool_join(t_all, den, e_all, h, 0, 0);
 #pragma unroll
-        for (int i = 0; i < OWN; ++i)
-            if (wave + kPoolTeam * i < G)
+            for (int i = 0; i < OWN; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    pool_block<D>::put4(a.joint_rows[1] + r_at * D, 4 * (wave + kPoolTeam * i) + j, half,
-                                        floatx4{sums[i][4 * j], sums[i][4 * j + 1], sums[i][4 * j + 2], sums[i][4 * j + 3]}, a.bits);
-        if (wave == 0 && half == 0) reinterpret_cast<floatx4*>(a.joint_heads[1])[r_at] = floatx4{t_all, den, __uint_as_float((uint32_t)e_all), 0.0f};
-        return;
+                for (int j = 0; j < 4; ++j) {
+                    const floatx4 y = pool_block<D>::get4(a.joint_rows[which] + r_at * D, 4 * min(wave + kPoolTeam * i, G - 1) + j, half, a.bits);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) sums[i][4 * j + m] = fmaf(in ? y[m] : 0.0f, h[0].factor, sums[i][4 * j + m] * before);
+                }
+        };
+        const pool_common p(a, view.group, head, KEYS);
+        const int before_rows = (q.start - p.p.start) * a.group, n_rows = q.n_new * a.group, from = before_rows + r0, to = before_rows + min(r0 + 31, n_rows - 1);
+        const int mine = min(from + (lane & 31), to);
+        if (p.there && from >= 0 && to < p.p.n_new * a.group)       // (starts that are not ascending: anything)
+            for (int b = from / p.rows; b <= to / p.rows; ++b) {
+                const int v0 = p.first(b), v1 = p.last(b);
+                const bool in = mine / p.rows == b;
+                const int r = in ? mine - b * p.rows : 0;
+                if (v0 == v1) {
+                    whole(1, in);
+                    continue;
+                }
+                for (int v = v0; v <= v1; v += AHEAD)
+                    join(v, v1,
+                         [&](int w, pool_part_head& h) __attribute__((always_inline)) {
+                             const float* const x = p.template heads<D>(p.template part<D>(a, b, w, w == v0, r), r);
+                             h = {x[0], x[64], x[128], 0.0f};
+                             if (!in) h = {kPoolLowest, 0.0f, __uint_as_float((uint32_t)kPoolNoExponent), 0.0f};
+                         },
+                         [&](int w, int n) __attribute__((always_inline)) {
+                             const floatx4 x = p.positions(p.template part<D>(a, b, w, w == v0, r), r, n, half, a.bits);
+                             return in ? x : floatx4{0, 0, 0, 0};
+                         });
+            }
+        if (w0 == w1) whole(0, true);
     }
+    if (!joint || w0 != w1)
+        for (int v = w0; v <= w1; v += AHEAD)
+            join(v, w1, [&](int w, pool_part_head& h) __attribute__((always_inline)) { h.load(part(w) + 32 * D, lane); },
+                 [&](int w, int n) __attribute__((always_inline)) { return reinterpret_cast<const floatx4*>(part(w))[n * 64 + lane]; });
     // ---- as pool_finish, the operands through LDS
     float m = 0.0f;
 #pragma unroll

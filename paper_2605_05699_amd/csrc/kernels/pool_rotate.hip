@@ -82,11 +82,11 @@ __device__ __forceinline__ void count_units(const pool_attention_args& a) {
     // the sequences' own units first, then their sums in place
     for (int b = wave; b < n_seq; b += NT / 64) {
         const pool_seq q = pool_view_of<FORM>(a, b).q;
-        const bool decode = pool_is_decode(q, a.group, a.decode_rows);
+        const bool decode = pool_is_decode<FORM>(a, q, b);
         const int chunk = decode || q.n_new == 0 ? 0 : a.heads * pool_chunk_units<FORM>(a, q, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS);
         if (lane == 0) {
             if (a.blocks_before) a.blocks_before[b + 1] = decode ? 0 : (q.n_new * a.group + ROWS - 1) / ROWS;
-            a.decode_before[b + 1] = decode ? a.heads * ((q.n_new * a.group + a.decode_block - 1) / a.decode_block) * pool_decode_tiles<FORM>(a, q, a.decode_keys) : 0;
+            a.decode_before[b + 1] = decode ? a.heads * ((q.n_new * a.group + a.decode_block - 1) / a.decode_block) * pool_decode_cost<FORM>(pool_decode_tiles<FORM>(a, q, a.decode_keys)) : 0;
             a.chunk_before[b + 1] = chunk;
         }
     }

@@ -82,11 +82,11 @@ struct pool_attention_args {
     int recent, sinks;                                       // sliding
     const int *groups, *shared;                              // shared: the caller's
     int n_groups, bits;
-    int merge_groups;                                        // the merge is of the tokens in common, into joint_rows[1]
+    int common_rows;                                         // a group's rows up to which its tokens in common go to pool_decode
     int* bounds;                                             // [n_groups + 1]: groups, ascending and within n_seq (workspace)
     pool_item* items;                                        // [n_seq + n_groups] (workspace)
-    float *joint_rows[2], *joint_heads[2];                   // [n_new][n_q_heads][D] and [4]: sums by channel and maximum, sum of weights, exponent of own
-                                                             // tokens that one workgroup has had whole, and of those in common (workspace)
+    float *joint_rows[2], *joint_heads[2];                   // [n_new][n_q_heads][D] and [4]: sums by channel and maximum, sum of weights, exponent, where one
+                                                             // workgroup has had all of a row's own tokens [0], or of those in common [1] (workspace)
 };
 // Sums of a block of 32 rows that a segment leaves: [D / 8 float4][64 lanes], then per lane maximum, sum of weights and V's exponent.
 template <int D> constexpr int kPoolPart = 32 * D + 3 * 64;
@@ -101,6 +101,9 @@ __device__ __forceinline__ int pool_tiles(int seen, int full, int keys) {
     return (pages + keys - 1) / keys + (window + keys - 1) / keys;
 }
 __device__ __forceinline__ bool pool_is_decode(const pool_seq& q, int group, int rows) { return q.n_new * group <= rows; }
+template <int FORM> __device__ __forceinline__ bool pool_is_decode(const pool_attention_args& a, const pool_seq& q, int i) {
+    return pool_is_decode(q, a.group, FORM == kPoolShared && i >= a.s.n_seq ? a.common_rows : a.decode_rows);
+}
 // tokens that the rows of block rt (of `rows` rows) see at most
 __device__ __forceinline__ int pool_seen(const pool_seq& q, int group, int rows, int rt) {
     return q.before + (min((rt + 1) * rows, q.n_new * group) - 1) / group + 1;
@@ -149,6 +152,14 @@ template <int FORM>
 __device__ __forceinline__ int pool_chunk_tiles(const pool_attention_args& a, const pool_seq& q, int rows, int keys, int rt) {
     return pool_tiles(pool_chunk_seen<FORM>(a, q, rows, rt), q.full, keys) - pool_chunk_gap<FORM>(a, q, rows, keys, rt).skip;
 }
+// What a block of rows counts for when the work is shared out: its tiles, and the time that its start and its end take, in tiles, so that a
+// workgroup with many short segments has fewer tiles (chunks of 8 sequences, 40 to 300 tokens, behind 12,000 in common: the workgroups with the
+// own tokens' segments had 30 of them, 560 us).  The causal form counts tiles alone.
+template <int FORM> constexpr int kPoolChunkStart = FORM == kPoolCausal ? 0 : 6;
+template <int FORM> constexpr int kPoolDecodeStart = FORM == kPoolCausal ? 0 : 4;
+template <int FORM> constexpr int kPoolChunkLeast = FORM == kPoolCausal ? 1 : 8;             // of units, a workgroup's of pool_chunk
+template <int FORM> __device__ __forceinline__ int pool_chunk_cost(int tiles) { return tiles > 0 ? tiles + kPoolChunkStart<FORM> : 0; }
+template <int FORM> __device__ __forceinline__ int pool_decode_cost(int tiles) { return tiles > 0 ? tiles + kPoolDecodeStart<FORM> : 0; }
 // the same of pool_decode, whose blocks of a sequence have all the same tiles
 template <int FORM>
 __device__ __forceinline__ pool_gap<FORM> pool_decode_gap(const pool_attention_args& a, const pool_seq& q, int keys) {
@@ -162,16 +173,16 @@ __device__ __forceinline__ int pool_decode_tiles(const pool_attention_args& a, c
 struct pool_view {
     pool_seq q;
     int seq, first_page;
-    bool joint;                                              // its sums are joined with others: they are left unfinished
+    int group;                                               // whose tokens in common it has in front of its own, or -1
 };
 template <int FORM> __device__ __forceinline__ int pool_count(const pool_attention_args& a) { return FORM == kPoolShared ? a.s.n_seq + a.n_groups : a.s.n_seq; }
 template <int FORM>
 __device__ __forceinline__ pool_view pool_view_of(const pool_attention_args& a, int i) {
     if constexpr (FORM == kPoolShared) {
         const pool_item t = a.items[i];
-        return {{t.start, t.n_new, t.length, t.before, t.full}, t.seq, t.first_page, i >= a.s.n_seq || t.group >= 0};
+        return {{t.start, t.n_new, t.length, t.before, t.full}, t.seq, t.first_page, t.group};
     }
-    return {pool_seq_of(a.s, i), i, 0, false};
+    return {pool_seq_of(a.s, i), i, 0, -1};
 }
 // sum over the lanes of a wavefront, in all of them
 __device__ __forceinline__ int pool_wave_sum(int x) {
@@ -183,7 +194,7 @@ __device__ __forceinline__ int pool_wave_sum(int x) {
 template <int FORM>
 __device__ __forceinline__ int pool_chunk_units(const pool_attention_args& a, const pool_seq& q, int rows, int keys, int n) {
     int sum = 0;
-    for (int rt = threadIdx.x & 63; rt < n; rt += 64) sum += pool_chunk_tiles<FORM>(a, q, rows, keys, rt);
+    for (int rt = threadIdx.x & 63; rt < n; rt += 64) sum += pool_chunk_cost<FORM>(pool_chunk_tiles<FORM>(a, q, rows, keys, rt));
     return pool_wave_sum(sum);
 }
 // The workgroups that take part, and where the share of workgroup w begins: the first `more` have a unit more than the others.

@@ -30,6 +30,7 @@ constexpr int kChunkRows = kPoolBlock * kPoolChunkWaves;
 // Sequences that bring few rows a key head go to pool_decode, cb blocks of 16 of them a workgroup, the others to pool_chunk.  Two blocks where
 // a sequence may bring 17 to 32 rows and none brings more, up to d = 128 (beyond it two blocks' sums do not fit the registers: there a
 // workgroup takes one block, and the keys are read twice); else one, and 17 rows are a chunk.
+constexpr int kCommonRows = 48;                               // (up to three blocks of pool_decode)
 struct split {
     int cb, rows;
     bool chunk, decode;
@@ -39,7 +40,7 @@ split split_of(const srft_paged_seqs* s, const form_of_call& f, int64_t n_new, i
     const bool few = most > 16 && most <= kPoolDecodeRows;
     const int rows = few ? kPoolDecodeRows : 16;
     // (a group's tokens in common have the rows of all its sequences)
-    return {few && d <= 128 ? 2 : 1, rows, most > rows || (f.groups() > 0 && n_new * group > rows), most <= rows || s->n_seq > 1 || n_new * group <= rows};
+    return {few && d <= 128 ? 2 : 1, rows, most > rows || (f.groups() > 0 && n_new * group > kCommonRows), most <= rows || s->n_seq > 1 || n_new * group <= rows};
 }
 workspace layout(const srft_pool* p, const srft_paged_seqs* s, const form_of_call& f, int64_t n_new, int q_heads) {
     const int d = p->plan_k->d, group = q_heads / p->heads, items = s->n_seq + f.groups();
@@ -96,9 +97,9 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, const form_of_call
     if (q_heads < 1 || q_heads % pool->heads != 0 || q_heads > 64 * pool->heads || n_new * q_heads >= (1LL << 31) - 32) return SRFT_ERR_BAD_N;
     // units of work (kPoolMostUnits), tiles and workgroups are counted with 32 bits
     const int d = pool->plan_k->d, group = q_heads / pool->heads;
-    const int64_t most = kPoolMostUnits, tiles = seqs->max_length / 32 + 2, heads = (int64_t)seqs->n_seq * pool->heads;
+    const int64_t most = kPoolMostUnits, tiles = seqs->max_length / 32 + 2 + (f.form == kPoolCausal ? 0 : kPoolChunkStart<kPoolSliding>), heads = (int64_t)seqs->n_seq * pool->heads;
     const int64_t items = seqs->n_seq + f.groups(), blocks = (f.groups() > 0 ? 2 : 1) * n_new * group / kChunkRows + items;
-    if (2 * items * pool->heads * tiles >= most || blocks * pool->heads * std::max<int64_t>(tiles, kPoolChunkWaves) >= most ||
+    if ((f.groups() > 0 ? 3 : 2) * items * pool->heads * tiles >= most || blocks * pool->heads * std::max<int64_t>(tiles, kPoolChunkWaves) >= most ||
         (heads * pool->R / kTileVecs * 2 + pool->plan_k->compute_units * 3 + 1) * 2 * d > UINT32_MAX)        // (threads of pool_rotate)
         return SRFT_ERR_BAD_N;
     return SRFT_OK;
@@ -182,6 +183,7 @@ int attend(const srft_pool* pool, const srft_paged_seqs* seqs, form_of_call f, c
         a.groups = f.prefixes->groups_dev;
         a.shared = f.prefixes->tokens_dev;
         a.n_groups = f.groups();
+        a.common_rows = kCommonRows;
         a.bounds = (int*)(base + w.bounds);
         a.items = (pool_item*)(base + w.items);
         for (int i = 0; i < 2; ++i) {
@@ -194,15 +196,11 @@ int attend(const srft_pool* pool, const srft_paged_seqs* seqs, form_of_call f, c
     rc = srft_launch(srft_pick_pool_rotate(d, pk->bits, f.form), dim3((unsigned)(1 + a.q_grid + tail_tiles)), 2 * d, st, a);
     if (rc == SRFT_OK && sp.chunk) rc = srft_launch(srft_pool_chunk_kernel_of(pk, f.form), dim3((unsigned)a.chunk_grid), 64 * kPoolChunkWaves, st, a);
     if (rc == SRFT_OK && sp.decode) rc = srft_launch(srft_pool_decode_kernel_of(pk, sp.cb, f.form), dim3((unsigned)a.decode_grid), 64 * kPoolTeam, st, a);
-    // the merges: of the tokens in common first
-    for (int groups = f.groups() > 0 ? 1 : 0; groups >= 0 && rc == SRFT_OK; --groups) {
-        const int64_t n = groups ? f.groups() : seqs->n_seq, rows = n_new * group;
-        a.merge_groups = groups;
-        a.decode_merges = sp.decode ? (int)n * pool->heads * ((a.decode_rows + a.decode_block - 1) / a.decode_block) : 0;
-        a.merges = (unsigned)a.decode_merges +
-                   (sp.chunk ? (unsigned)((rows / kChunkRows + std::min(n, rows / (a.decode_rows + 1))) * pool->heads * kPoolChunkWaves) : 0);
-        if (a.merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb, f.form), srft_grid(a.merges), 64 * kPoolTeam, st, a);
-    }
+    const int64_t rows = n_new * group;
+    a.decode_merges = sp.decode ? seqs->n_seq * pool->heads * ((a.decode_rows + a.decode_block - 1) / a.decode_block) : 0;
+    a.merges = (unsigned)a.decode_merges +
+               (sp.chunk ? (unsigned)((rows / kChunkRows + std::min<int64_t>(seqs->n_seq, rows / (a.decode_rows + 1))) * pool->heads * kPoolChunkWaves) : 0);
+    if (rc == SRFT_OK && a.merges) rc = srft_launch(srft_pick_pool_merge(d, sp.cb, f.form), srft_grid(a.merges), 64 * kPoolTeam, st, a);
     return rc;
 }
 

@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
     const int n_seq = pool_count<FORM>(a), total = a.chunk_before[n_seq];
     const int w = srft_block_by_die();
-    const pool_shares shares(total, gridDim.x, 1);
+    const pool_shares shares(total, gridDim.x, kPoolChunkLeast<FORM>);
     if (total == 0 || w >= shares.groups) return;            // (uniform)
     const int end = shares.begin(w + 1);
     int unit = shares.begin(w);
@@ -68,12 +68,18 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
         const int per_head = __builtin_amdgcn_readfirstlane(pool_chunk_units<FORM>(a, q, ROWS, KEYS, blocks));
         const int rel = unit - a.chunk_before[seq], head = rel / per_head;
         int t0 = rel - head * per_head, rt = 0, tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, 0);
-        while (t0 >= tiles && rt + 1 < blocks) {             // the block of rows (those without a tile are passed over)
-            t0 -= tiles;
+        while (t0 >= pool_chunk_cost<FORM>(tiles) && rt + 1 < blocks) {      // the block of rows (those without a tile are passed over)
+            t0 -= pool_chunk_cost<FORM>(tiles);
             tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, ++rt);
         }
-        const int t1 = min(tiles, t0 + end - unit);
+        int t1 = min(pool_chunk_cost<FORM>(tiles), t0 + end - unit);
         if (t1 <= t0) return;                                // (only if the device arrays were written during the call)
+        unit += t1 - t0;
+        if constexpr (kPoolChunkStart<FORM> > 0) {           // the units in front are the start's
+            t0 = max(t0 - kPoolChunkStart<FORM>, 0);
+            t1 -= kPoolChunkStart<FORM>;
+            if (t1 <= t0) continue;
+        }
         const int seen = pool_chunk_seen<FORM>(a, q, ROWS, rt), all_page_tiles = (max(min(seen, q.full), 0) + KEYS - 1) / KEYS, tail = q.length - q.full;
         const pool_gap<FORM> gap = pool_chunk_gap<FORM>(a, q, ROWS, KEYS, rt);
         const int page_tiles = all_page_tiles - gap.in_pages(all_page_tiles);
@@ -306,7 +312,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
             }
         }
         b.den = pool_halves_sum(b.den);
-        if (FORM == kPoolShared && t0 == 0 && t1 == tiles && view.joint) {           // whole, but to be joined: by rows
+        if (FORM == kPoolShared && t0 == 0 && t1 == tiles && (seq >= a.s.n_seq || view.group >= 0)) {           // whole, but to be joined: by rows
             row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + l32);
             if (row.there) {
                 const int which = seq >= a.s.n_seq;
@@ -327,7 +333,6 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
         } else {
             b.put(a.chunk_parts + ((2LL * w + (at_begin ? 0 : 1)) * W + wave) * kPoolPart<D>, lane);
         }
-        unit += t1 - t0;
     }
 }
 

@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
         seq = min((int)__popcll(__ballot(lane <= n_seq && of_before <= unit)) - 1, n_seq - 1);
         units_before = __builtin_amdgcn_readlane(of_before, seq);
         view = {pool_seq_from(a.s, __builtin_amdgcn_readlane(of_start, seq), __builtin_amdgcn_readlane(of_start, seq + 1), __builtin_amdgcn_readlane(of_length, seq)),
-                seq, 0, false};
+                seq, 0, -1};
     } else {
         seq = __builtin_amdgcn_readfirstlane(pool_sequence_of(a.decode_before, n_seq, unit));
         units_before = a.decode_before[seq];
@@ -239,9 +239,16 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
         const pool_gap<FORM> gap = pool_decode_gap<FORM>(a, q, KEYS);
         const int all_page_tiles = (q.full + KEYS - 1) / KEYS, page_tiles = all_page_tiles - gap.in_pages(all_page_tiles), tail = q.length - q.full;
         const int tiles = pool_tiles(q.length, q.full, KEYS) - gap.skip;
-        const int rel = unit - units_before, item = rel / tiles, t0 = rel - item * tiles, t1 = min(tiles, t0 + end - unit);
+        const int cost = pool_decode_cost<FORM>(tiles), rel = unit - units_before, item = rel / cost;
+        int t0 = rel - item * cost, t1 = min(cost, t0 + end - unit);
         const int blocks_of_rows = (q.n_new * a.group + 16 * CB - 1) / (16 * CB), head = item / blocks_of_rows, r0 = 16 * CB * (item - head * blocks_of_rows);
         if (t1 <= t0) return;                                // (only if the device arrays were written during the call)
+        unit += t1 - t0;
+        if constexpr (kPoolDecodeStart<FORM> > 0) {          // the units in front are the start's
+            t0 = max(t0 - kPoolDecodeStart<FORM>, 0);
+            t1 -= kPoolDecodeStart<FORM>;
+            if (t1 <= t0) continue;
+        }
         const int32_t* const table = a.s.table + view.seq * a.s.max_pages + view.first_page;
         const int last_page_tile = min(t1, page_tiles) - 1;
         int t = t0 + wave;
@@ -625,7 +632,7 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
                     }
             }
             __syncthreads();
-            if (FORM == kPoolShared && whole && view.joint) {            // to be joined with others: by rows
+            if (FORM == kPoolShared && whole && (seq >= a.s.n_seq || view.group >= 0)) {            // to be joined with others: by rows
                 if (row[c].there) {
                     const int which = seq >= a.s.n_seq;
                     const long long at = (long long)row[c].token * (a.heads * a.group) + row[c].head;
@@ -650,26 +657,84 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
             }
         }
         __syncthreads();                                     // (the next segment's tiles go where the sums were, its queries where these are)
-        unit += t1 - t0;
     }
 }
 
+// ---- shared: where the sums of rows over the tokens that their group has in common lie
+struct pool_common {
+    pool_seq p;
+    int units_before, cost, blocks, rows;                    // of a block of rows: units, and how many rows it has
+    bool chunk, there;
+    pool_shares shares;
+    // rows r0 .. r0 + n - 1 of a key head of the sequence q, of this group (uniform)
+    __device__ __forceinline__ pool_common(const pool_attention_args& a, int group, int head, int chunk_keys)
+        : p(pool_view_of<kPoolShared>(a, a.s.n_seq + group).q),
+          chunk(!pool_is_decode<kPoolShared>(a, p, a.s.n_seq + group)),
+          shares(chunk ? a.chunk_before[a.s.n_seq + a.n_groups] : a.decode_before[a.s.n_seq + a.n_groups], chunk ? a.chunk_grid : a.decode_grid,
+                 chunk ? kPoolChunkLeast<kPoolShared> : kPoolTeam) {
+        rows = chunk ? kPoolBlock * kPoolChunkWaves : a.decode_block;
+        const int tiles = pool_tiles(p.length, p.full, chunk ? chunk_keys : a.decode_keys);
+        cost = chunk ? pool_chunk_cost<kPoolShared>(tiles) : pool_decode_cost<kPoolShared>(tiles);
+        blocks = (p.n_new * a.group + rows - 1) / rows;
+        units_before = (chunk ? a.chunk_before : a.decode_before)[a.s.n_seq + group] + head * blocks * cost;
+        there = shares.units > 0;
+    }
+    __device__ __forceinline__ int start() const { return chunk ? kPoolChunkStart<kPoolShared> : kPoolDecodeStart<kPoolShared>; }
+    __device__ __forceinline__ int first(int block) const { return shares.owner(units_before + block * cost + start()); }
+    __device__ __forceinline__ int last(int block) const { return shares.owner(units_before + (block + 1) * cost - 1); }
+    // what workgroup w (the first of its block, or not) has left of row r of a block: its sums, and maximum, sum of weights and exponent at
+    // heads[0], [64], [128]
+    template <int D>
+    __device__ __forceinline__ const float* part(const pool_attention_args& a, int block, int w, bool is_first, int r) const {
+        const int behind = is_first && shares.begin(w) < units_before + block * cost ? 1 : 0, slot = 2 * w + (is_first ? behind : 0);
+        if (chunk) return a.chunk_parts + ((long long)slot * kPoolChunkWaves + r / kPoolBlock) * kPoolPart<D>;
+        return a.decode_parts + ((long long)slot * (a.decode_block / 16) + r / 16) * kPoolPart16<D>;
+    }
+    template <int D>
+    __device__ __forceinline__ const float* heads(const float* part, int r) const {
+        return chunk ? part + 32 * D + r % kPoolBlock : part + 16 * D + r % 16;
+    }
+    // channels 16 c + 4 quarter .. + 3 of row r
+    __device__ __forceinline__ floatx4 channels(const float* part, int r, int c, int quarter, int bits) const {
+        const floatx4* const x = reinterpret_cast<const floatx4*>(part);
+        if (!chunk) return x[c * 64 + 16 * quarter + r % 16];
+        const int u = (2 * c + (quarter >> 1)) * 64 + r % kPoolBlock;        // (positions: see pool_block)
+        if (bits == 8) {
+            const floatx4 y = x[u + 32 * (quarter & 1)];
+            return floatx4{y[0], y[2], y[1], y[3]};
+        }
+        const floatx4 y = x[u], z = x[u + 32];
+        return quarter & 1 ? floatx4{y[1], y[3], z[1], z[3]} : floatx4{y[0], y[2], z[0], z[2]};
+    }
+    // positions 4 half .. + 3 of unit u of eight of row r
+    __device__ __forceinline__ floatx4 positions(const float* part, int r, int u, int half, int bits) const {
+        const floatx4* const x = reinterpret_cast<const floatx4*>(part);
+        if (chunk) return x[u * 64 + 32 * half + r % kPoolBlock];
+        const int c = (u >> 1) * 64 + 32 * (u & 1) + r % 16;                 // (channels)
+        if (bits == 8) {
+            const floatx4 y = x[c + 16 * half];
+            return floatx4{y[0], y[2], y[1], y[3]};
+        }
+        const floatx4 y = x[c], z = x[c + 16];
+        return half ? floatx4{y[2], z[2], y[3], z[3]} : floatx4{y[0], z[0], y[1], z[1]};
+    }
+};
+
 // The parts of a key head's rows that went to several workgroups, in the order of the keys; rows of sequences without a tile are zero.  One
 // workgroup of four wavefronts per sequence and key head, each with a quarter of the channels, all parts of them on their way at once
-// (up to AHEAD).
+// (up to AHEAD).  Shared: the parts of the tokens in common first.
 template <int D, int CB, int FORM>
 __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, unsigned block, unsigned char* lds) {
     constexpr int NB = D / 16, W = kPoolTeam, AHEAD = 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int all = (a.decode_rows + 16 * CB - 1) / (16 * CB), at = (int)(block / (unsigned)all), rb = (int)block - at * all;
-    const bool groups = FORM == kPoolShared && a.merge_groups;
-    const int seq = at / a.heads + (groups ? a.s.n_seq : 0), head = at - at / a.heads * a.heads;
+    const int seq = at / a.heads, head = at - seq * a.heads;
     const int units = a.decode_before[pool_count<FORM>(a)], units_before = a.decode_before[seq];     // (with the sequence's, in one round of loads)
     const pool_view view = pool_view_of<FORM>(a, seq);
     const pool_seq& q = view.q;
     const int rows = q.n_new * a.group, blocks_of_rows = (rows + 16 * CB - 1) / (16 * CB);
     if (rows == 0 || !pool_is_decode(q, a.group, a.decode_rows) || rb >= blocks_of_rows) return;
-    const int tiles = pool_decode_tiles<FORM>(a, q, a.decode_keys);
+    const int tiles = pool_decode_tiles<FORM>(a, q, a.decode_keys), cost = pool_decode_cost<FORM>(tiles);
     if (tiles == 0) {
         for (int i = threadIdx.x + rb * 16 * CB * (D / 8); i < min(rows, (rb + 1) * 16 * CB) * (D / 8); i += 64 * W) {
             const pool_row r = pool_row_of(q, head, a.group, i / (D / 8));
@@ -679,9 +744,10 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
     }
     if (units == 0) return;                                  // (too many of them: see kPoolMostUnits)
     const pool_shares shares(units, a.decode_grid, W);
-    const int first = units_before + (head * blocks_of_rows + rb) * tiles, w0 = shares.owner(first), w1 = shares.owner(first + tiles - 1);
-    if (w0 == w1 && (!view.joint || groups)) return;
-    const int behind = shares.begin(w0) != first ? 1 : 0;    // the first part's workgroup began with other rows
+    const int first = units_before + (head * blocks_of_rows + rb) * cost, w0 = shares.owner(first + kPoolDecodeStart<FORM>), w1 = shares.owner(first + cost - 1);
+    const bool joint = FORM == kPoolShared && view.group >= 0;
+    if (w0 == w1 && !joint) return;
+    const int behind = shares.begin(w0) < first ? 1 : 0;     // the first part's workgroup began with other rows
     const auto part = [&](int w, int c) __attribute__((always_inline)) {
         return a.decode_parts + ((2LL * w + (w == w0 ? behind : 0)) * CB + c) * kPoolPart16<D>;
     };
@@ -692,34 +758,15 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
 #pragma unroll
         for (int i = 0; i < kPoolOwn<D>; ++i) o[i] = floatx4{0, 0, 0, 0};
         const pool_row r = pool_row_of(q, head, a.group, (rb * CB + c) * 16 + (lane & 15));
-        const long long r_at = (long long)r.token * (a.heads * a.group) + r.head;
-        if (FORM == kPoolShared && view.joint && !groups) {
-            // the rows' sums over the tokens in common, and over their own where one workgroup has had all of these
-            floatx4 x[2][kPoolOwn<D>], head4[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int which = k == 0 || w0 != w1 ? 1 : 0;
-                head4[k] = reinterpret_cast<const floatx4*>(a.joint_heads[which])[r_at];
-#pragma unroll
-                for (int i = 0; i < kPoolOwn<D>; ++i)
-                    x[k][i] = *reinterpret_cast<const floatx4*>(a.joint_rows[which] + r_at * D + 16 * min(wave + W * i, NB - 1) + 4 * (lane >> 4));
-            }
-            pool_part_head h[2] = {{head4[0][0], head4[0][1], head4[0][2], 0.0f}, {head4[1][0], head4[1][1], head4[1][2], 0.0f}};
-            pool_join(t_all, den, e_all, h, 0, w0 == w1 ? 1 : 0);
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int i = 0; i < kPoolOwn<D>; ++i) o[i] += x[k][i] * h[k].factor;
-        }
-        for (int v = w0; v <= w1 && (FORM != kPoolShared || w0 != w1); v += AHEAD) {              // (one round of loads for AHEAD parts, the sums so far brought under their maximum)
+        // parts v .. v + AHEAD - 1, up to w1, whose sums and heads `sums` and `heads` give
+        const auto join = [&](int v, int w1, auto heads, auto sums) __attribute__((always_inline)) {
             floatx4 x[AHEAD][kPoolOwn<D>];
             pool_part_head h[AHEAD];
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const float* const at = part(min(v + k, w1), c);
-                h[k].load(at + 16 * D, lane);
+                heads(min(v + k, w1), h[k]);
 #pragma unroll
-                for (int i = 0; i < kPoolOwn<D>; ++i) x[k][i] = reinterpret_cast<const floatx4*>(at)[min(wave + W * i, NB - 1) * 64 + lane];
+                for (int i = 0; i < kPoolOwn<D>; ++i) x[k][i] = sums(min(v + k, w1), min(wave + W * i, NB - 1));
             }
             const float before = pool_join(t_all, den, e_all, h, v, w1);
 #pragma unroll
@@ -728,16 +775,52 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
             for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
                 for (int i = 0; i < kPoolOwn<D>; ++i) o[i] += x[k][i] * h[k].factor;
-        }
-        if (FORM == kPoolShared && groups) {                 // (uniform)
-            if (r.there) {
+        };
+        if (joint) {
+            const long long r_at = (long long)r.token * (a.heads * a.group) + r.head;
+            // rows whose tokens (own: 0, in common: 1) one workgroup has had all of; the others as they are
+            const auto whole = [&](int which, bool in) __attribute__((always_inline)) {
+                const floatx4 x = reinterpret_cast<const floatx4*>(a.joint_heads[which])[r_at];
+                pool_part_head h[1] = {{x[0], x[1], x[2], 0.0f}};
+                if (!in) h[0] = {kPoolLowest, 0.0f, __uint_as_float((uint32_t)kPoolNoExponent), 0.0f};
+                const float before = pool_join(t_all, den, e_all, h, 0, 0);
 #pragma unroll
-                for (int i = 0; i < kPoolOwn<D>; ++i)
-                    if (wave + W * i < NB) *reinterpret_cast<floatx4*>(a.joint_rows[1] + r_at * D + 16 * (wave + W * i) + 4 * (lane >> 4)) = o[i];
-                if (wave == 0 && lane < 16) reinterpret_cast<floatx4*>(a.joint_heads[1])[r_at] = floatx4{t_all, den, __uint_as_float((uint32_t)e_all), 0.0f};
-            }
-            continue;
+                for (int i = 0; i < kPoolOwn<D>; ++i) {
+                    const floatx4 y = *reinterpret_cast<const floatx4*>(a.joint_rows[which] + r_at * D + 16 * min(wave + W * i, NB - 1) + 4 * (lane >> 4));
+                    o[i] = o[i] * before + (in ? y : floatx4{0, 0, 0, 0}) * h[0].factor;
+                }
+            };
+            const pool_common p(a, view.group, head, kPoolChunkKeys<D>);
+            // the rows' numbers among those of the group
+            const int before_rows = (q.start - p.p.start) * a.group, from = before_rows + (rb * CB + c) * 16, to = min(from + 15, before_rows + rows - 1);
+            const int mine = min(from + (lane & 15), to);
+            if (p.there && from >= 0 && from <= to && to < p.p.n_new * a.group)          // (starts that are not ascending: anything)
+                for (int b = from / p.rows; b <= to / p.rows; ++b) {
+                    const int v0 = p.first(b), v1 = p.last(b);
+                    const bool in = mine / p.rows == b;
+                    const int row = in ? mine - b * p.rows : 0;
+                    if (v0 == v1) {
+                        whole(1, in);
+                        continue;
+                    }
+                    for (int v = v0; v <= v1; v += AHEAD)
+                        join(v, v1,
+                             [&](int w, pool_part_head& h) __attribute__((always_inline)) {
+                                 const float* const x = p.template heads<D>(p.template part<D>(a, b, w, w == v0, row), row);
+                                 h = {x[0], x[64], x[128], 0.0f};
+                                 if (!in) h = {kPoolLowest, 0.0f, __uint_as_float((uint32_t)kPoolNoExponent), 0.0f};
+                             },
+                             [&](int w, int n) __attribute__((always_inline)) {
+                                 const floatx4 x = p.channels(p.template part<D>(a, b, w, w == v0, row), row, n, lane >> 4, a.bits);
+                                 return in ? x : floatx4{0, 0, 0, 0};
+                             });
+                }
+            if (w0 == w1) whole(0, true);
         }
+        if (!joint || w0 != w1)
+            for (int v = w0; v <= w1; v += AHEAD)            // (one round of loads for AHEAD parts, the sums so far brought under their maximum)
+                join(v, w1, [&](int w, pool_part_head& h) __attribute__((always_inline)) { h.load(part(w, c) + 16 * D, lane); },
+                     [&](int w, int n) __attribute__((always_inline)) { return reinterpret_cast<const floatx4*>(part(w, c))[n * 64 + lane]; });
         char* const dst = r.there ? a.out + r.token * a.out_token + r.head * a.out_head : nullptr;
         if (c > 0) __syncthreads();
         pool_finish16<D, true>(o, den, e_all, lds, a.out_table16, a.out_unscale, dst, a.bf16, wave, lane);
