@@ -146,7 +146,9 @@ def lib() -> C.CDLL:
         entries = ("srft_kv_quantize", "srft_kv_dequantize", "srft_kv_quantize_batched", "srft_kv_dequantize_batched", "srft_kv_scores",
                    "srft_kv_decode_attention", "srft_kv_channel_absmax", "srft_cache_append", "srft_scores_workspace_bytes",
                    "srft_decode_attention_workspace_bytes", "srft_plan_d", "srft_rotary", "srft_pool_append", "srft_pool_attention",
-                   "srft_pool_copy", "srft_pool_append_workspace_bytes", "srft_pool_attention_workspace_bytes")
+                   "srft_pool_copy", "srft_pool_append_workspace_bytes", "srft_pool_attention_workspace_bytes", "srft_norm_rotary",
+                   "srft_norm_rotary_backward", "srft_norm_rotary_backward_workspace_bytes", "srft_pool_attention_sliding",
+                   "srft_pool_attention_sliding_workspace_bytes", "srft_pool_attention_shared", "srft_pool_attention_shared_workspace_bytes")
         if _marshal.bind(*[C.cast(getattr(L, name), vp).value for name in entries], vp, C.Array):
             _native_append(L)
             _native_calls()
@@ -165,11 +167,12 @@ def _not_made(*args):
 
 _fast_quantize = _fast_dequantize = _fast_scores = _fast_attention = _fast_absmax = _fast_quantize_batched = _fast_dequantize_batched = _not_made
 _fast_rotary = _fast_pool_append = _fast_pool_attention = _fast_pool_copy = _not_made
+_fast_norm_rotary = _fast_norm_backward = _fast_pool_sliding = _fast_pool_shared = _not_made
 
 
 def _native_calls() -> None:
     for name in ("quantize", "dequantize", "scores", "attention", "absmax", "quantize_batched", "dequantize_batched", "rotary",
-                 "pool_append", "pool_attention", "pool_copy"):
+                 "pool_append", "pool_attention", "pool_copy", "norm_rotary", "norm_backward", "pool_sliding", "pool_shared"):
         globals()["_fast_" + name] = getattr(_marshal, name)
 
 
@@ -560,6 +563,10 @@ def srft_norm_rotary(items, positions: torch.Tensor, freq: torch.Tensor, eps: fl
     items = list(items)
     if not items:
         return
+    if stream is None:
+        status = _fast_norm_rotary(items, positions, freq, ROTARY_LAYOUTS[layout], factor, eps)
+        if status is not None:
+            return _check(status, "srft_norm_rotary") if status else None
     items = [(x, out, weight) for x, weight, out in items]
     n, d = _norm_rows(items, positions, freq, 2)
     rows = (_NormRows * len(items))()
@@ -583,6 +590,10 @@ def srft_norm_rotary_backward(items, positions: torch.Tensor, freq: torch.Tensor
     items = list(items)
     if not items:
         return
+    if stream is None:
+        status = _fast_norm_backward(items, positions, freq, ROTARY_LAYOUTS[layout], factor, eps, workspace)
+        if status is not None:
+            return _check(status, "srft_norm_rotary_backward") if status else None
     items = [(dy, x, dx, weight, dweight) for dy, x, weight, dx, dweight in items]
     n, d = _norm_rows(items, positions, freq, 3)
     rows = (_NormGradRows * len(items))()
@@ -763,6 +774,10 @@ def srft_pool_attention_sliding_workspace_bytes(pool: PagePool, seqs: PagedSeqs,
 def srft_pool_attention_sliding(pool: PagePool, seqs: PagedSeqs, q: torch.Tensor, softmax_scale: float, recent: int, sinks: int, out: torch.Tensor,
                                 workspace: torch.Tensor, stream=None) -> None:
     """out <- causal attention of q [n_new, q heads, d] over each row's last `recent` tokens and its sequence's first `sinks`."""
+    if stream is None:
+        status = _fast_pool_sliding(pool.handle, seqs.address, pool.d, q, softmax_scale, recent, sinks, out, workspace)
+        if status is not None:
+            return _check(status, "srft_pool_attention_sliding") if status else None
     n, heads, _ = _attention_shape(pool, q, out)
     if not -1 << 63 <= recent < 1 << 63 or not -1 << 63 <= sinks < 1 << 63:          # (ctypes would keep the low bits)
         raise ValueError("recent and sinks must fit int64_t")
@@ -780,6 +795,10 @@ def srft_pool_attention_shared_workspace_bytes(pool: PagePool, seqs: PagedSeqs, 
 def srft_pool_attention_shared(pool: PagePool, seqs: PagedSeqs, prefixes: SharedPrefixes, q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
                                workspace: torch.Tensor, stream=None) -> None:
     """out <- srft_pool_attention's, where groups of sequences begin with the same pages: these are read once for all rows of a group."""
+    if stream is None:
+        status = _fast_pool_shared(pool.handle, seqs.address, prefixes.address, pool.d, q, softmax_scale, out, workspace)
+        if status is not None:
+            return _check(status, "srft_pool_attention_shared") if status else None
     n, heads, _ = _attention_shape(pool, q, out)
     (q_at, q_token, q_head), (o_at, o_token, o_head) = _rows(q, "q"), _rows(out, "out")
     space = _pool_workspace(workspace, srft_pool_attention_shared_workspace_bytes(pool, seqs, prefixes, n, heads))

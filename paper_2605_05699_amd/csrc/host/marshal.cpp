@@ -40,6 +40,13 @@ struct {
     decltype(&srft_pool_copy) pool_copy;
     decltype(&srft_pool_append_workspace_bytes) pool_append_bytes;
     decltype(&srft_pool_attention_workspace_bytes) pool_attention_bytes;
+    decltype(&srft_norm_rotary) norm_rotary;
+    decltype(&srft_norm_rotary_backward) norm_backward;
+    decltype(&srft_norm_rotary_backward_workspace_bytes) norm_backward_bytes;
+    decltype(&srft_pool_attention_sliding) pool_sliding;
+    decltype(&srft_pool_attention_sliding_workspace_bytes) pool_sliding_bytes;
+    decltype(&srft_pool_attention_shared) pool_shared;
+    decltype(&srft_pool_attention_shared_workspace_bytes) pool_shared_bytes;
     bool bound;
 } g;
 
@@ -303,6 +310,151 @@ PyObject* pool_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return true;
     });
 }
+// positions [tokens] and freq of a call on rows of tokens
+struct angles {
+    const int32_t* positions;
+    const double* freq;
+    int64_t tokens;
+    int rot;
+    bool of(PyObject* p, PyObject* f) {
+        const at::Tensor *pos = tensor_of(p, at::kInt), *fr = tensor_of(f, at::kDouble);
+        if (!pos || !fr || pos->dim() != 1 || fr->dim() != 1 || fr->size(0) > INT32_MAX / 2) return false;
+        positions = static_cast<const int32_t*>(pos->data_ptr()), freq = static_cast<const double*>(fr->data_ptr());
+        tokens = pos->size(0), rot = 2 * (int)fr->size(0);
+        return true;
+    }
+};
+// weights [d] of a tensor's channels, or None
+bool weight_of(PyObject* o, int64_t d, const void** p, int32_t* type) {
+    *p = nullptr, *type = 0;
+    if (o == Py_None) return true;
+    const at::Tensor* const w = space_of(o);
+    if (!w || type_of(*w) < 0 || w->dim() != 1 || w->size(0) != d) return false;
+    *p = w->data_ptr(), *type = type_of(*w);
+    return true;
+}
+// norm_rotary(items (x, weight, out), positions, freq, layout, factor, eps)
+PyObject* norm_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return made([&](int* rc) {
+        angles t;
+        if (n != 6 || !PyList_CheckExact(a[0]) || !t.of(a[1], a[2]) || !PyLong_CheckExact(a[3]) || !PyFloat_CheckExact(a[4]) || !PyFloat_CheckExact(a[5])) return false;
+        const int items = (int)PyList_GET_SIZE(a[0]);
+        if (items < 1 || items > SRFT_ROTARY_MAX) return false;
+        srft_norm_rows rows[SRFT_ROTARY_MAX] = {};
+        int64_t d = 0;
+        for (int i = 0; i < items; ++i) {
+            PyObject* const item = PyList_GET_ITEM(a[0], i);
+            if (!PyTuple_CheckExact(item) || PyTuple_GET_SIZE(item) != 3) return false;
+            const at::Tensor *x = rows_of(PyTuple_GET_ITEM(item, 0)), *y = rows_of(PyTuple_GET_ITEM(item, 2));
+            if (!x || !y || !x->sizes().equals(y->sizes()) || x->size(0) != t.tokens || type_of(*x) < 0 || type_of(*y) < 0) return false;
+            if (i == 0) d = x->size(2);
+            if (x->size(2) != d || d > INT32_MAX || x->size(1) > INT32_MAX || !weight_of(PyTuple_GET_ITEM(item, 1), d, &rows[i].weight_dev, &rows[i].weight_type)) return false;
+            srft_rotary_rows& r = rows[i].x;
+            r.in_dev = x->data_ptr(), r.in_token = step_of(*x, 0), r.in_head = step_of(*x, 1);
+            r.out_dev = y->data_ptr(), r.out_token = step_of(*y, 0), r.out_head = step_of(*y, 1);
+            r.n_heads = (int32_t)x->size(1), r.in_type = type_of(*x), r.out_type = type_of(*y);
+        }
+        const int layout = (int)PyLong_AsLong(a[3]);
+        const double factor = PyFloat_AS_DOUBLE(a[4]), eps = PyFloat_AS_DOUBLE(a[5]);
+        void* const st = current_stream();
+        *rc = without_gil([&] { return g.norm_rotary(rows, items, t.tokens, (int)d, t.rot, layout, t.positions, t.freq, factor, eps, st); });
+        return true;
+    });
+}
+// norm_backward(items (dy, x, weight, dx, dweight), positions, freq, layout, factor, eps, workspace)
+PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return made([&](int* rc) {
+        angles t;
+        if (n != 7 || !PyList_CheckExact(a[0]) || !t.of(a[1], a[2]) || !PyLong_CheckExact(a[3]) || !PyFloat_CheckExact(a[4]) || !PyFloat_CheckExact(a[5])) return false;
+        const int items = (int)PyList_GET_SIZE(a[0]);
+        if (items < 1 || items > SRFT_ROTARY_MAX) return false;
+        srft_norm_grad_rows rows[SRFT_ROTARY_MAX] = {};
+        int64_t d = 0;
+        for (int i = 0; i < items; ++i) {
+            PyObject* const item = PyList_GET_ITEM(a[0], i);
+            if (!PyTuple_CheckExact(item) || PyTuple_GET_SIZE(item) != 5) return false;
+            const at::Tensor *dy = rows_of(PyTuple_GET_ITEM(item, 0)), *x = rows_of(PyTuple_GET_ITEM(item, 1)), *dx = rows_of(PyTuple_GET_ITEM(item, 3));
+            if (!dy || !x || !dx || !x->sizes().equals(dy->sizes()) || !x->sizes().equals(dx->sizes()) || x->size(0) != t.tokens || type_of(*x) < 0 ||
+                type_of(*dy) < 0 || dx->scalar_type() != x->scalar_type())
+                return false;
+            if (i == 0) d = x->size(2);
+            srft_norm_grad_rows& r = rows[i];
+            if (x->size(2) != d || d > INT32_MAX || x->size(1) > INT32_MAX || !weight_of(PyTuple_GET_ITEM(item, 2), d, &r.weight_dev, &r.weight_type)) return false;
+            if (PyTuple_GET_ITEM(item, 4) != Py_None) {
+                const at::Tensor* const w = tensor_of(PyTuple_GET_ITEM(item, 4), at::kFloat);
+                if (!w || w->dim() != 1 || w->size(0) != d) return false;
+                r.dweight_dev = floats_of(w);
+            }
+            r.dy_dev = dy->data_ptr(), r.dy_token = step_of(*dy, 0), r.dy_head = step_of(*dy, 1);
+            r.x_dev = x->data_ptr(), r.x_token = step_of(*x, 0), r.x_head = step_of(*x, 1);
+            r.dx_dev = dx->data_ptr(), r.dx_token = step_of(*dx, 0), r.dx_head = step_of(*dx, 1);
+            r.n_heads = (int32_t)x->size(1), r.dy_type = type_of(*dy), r.x_type = type_of(*x);
+        }
+        void* wp = nullptr;
+        if (a[6] != Py_None) {
+            const at::Tensor* const w = space_of(a[6]);
+            const int64_t need = g.norm_backward_bytes(items, (int)d);
+            if (!w || need < 0 || bytes_of(*w) < need) return false;
+            wp = w->data_ptr();
+        }
+        const int layout = (int)PyLong_AsLong(a[3]);
+        const double factor = PyFloat_AS_DOUBLE(a[4]), eps = PyFloat_AS_DOUBLE(a[5]);
+        void* const st = current_stream();
+        *rc = without_gil([&] { return g.norm_backward(rows, items, t.tokens, (int)d, t.rot, layout, t.positions, t.freq, factor, eps, wp, st); });
+        return true;
+    });
+}
+// the tensors of a call of attention over pages
+struct attended {
+    void *q, *out, *space, *stream;
+    int64_t tokens, qt, qh, ot, oh, bytes;
+    int heads, type;
+    bool of(PyObject* d, PyObject* q_, PyObject* out_, PyObject* space_) {
+        const at::Tensor *x = rows_of(q_), *o = rows_of(out_), *w = space_of(space_);
+        if (!x || !o || !w || !PyLong_CheckExact(d) || type_of(*x) <= SRFT_F32 || o->scalar_type() != x->scalar_type() || !x->sizes().equals(o->sizes()) ||
+            x->size(2) != PyLong_AsLong(d) || x->size(1) > INT32_MAX)
+            return false;
+        q = x->data_ptr(), out = o->data_ptr(), space = w->data_ptr(), stream = current_stream();
+        tokens = x->size(0), qt = step_of(*x, 0), qh = step_of(*x, 1), ot = step_of(*o, 0), oh = step_of(*o, 1), bytes = bytes_of(*w);
+        heads = (int)x->size(1), type = type_of(*x);
+        return true;
+    }
+};
+// pool_sliding(pool, sequences, d, q, softmax_scale, recent, sinks, out, workspace)
+PyObject* pool_sliding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return made([&](int* rc) {
+        const srft_pool_t* pool;
+        const srft_paged_seqs* seqs;
+        attended t;
+        int overflow = 0, more = 0;
+        if (n != 9 || !handle_of(a[0], &pool) || !handle_of(a[1], &seqs) || !pool || !seqs || !PyFloat_CheckExact(a[4]) || !PyLong_CheckExact(a[5]) || !PyLong_CheckExact(a[6]) ||
+            !t.of(a[2], a[3], a[7], a[8]))
+            return false;
+        const int64_t recent = PyLong_AsLongLongAndOverflow(a[5], &overflow), sinks = PyLong_AsLongLongAndOverflow(a[6], &more);
+        const int64_t need = g.pool_sliding_bytes(pool, seqs, t.tokens, t.heads);
+        if (overflow || more || need < 0 || t.bytes < need) return false;
+        const float scale = (float)PyFloat_AS_DOUBLE(a[4]);
+        *rc = without_gil([&] { return g.pool_sliding(pool, seqs, t.q, t.type, t.tokens, t.heads, t.qt, t.qh, scale, recent, sinks, t.out, t.ot, t.oh, t.space, t.stream); });
+        return true;
+    });
+}
+// pool_shared(pool, sequences, prefixes, d, q, softmax_scale, out, workspace)
+PyObject* pool_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return made([&](int* rc) {
+        const srft_pool_t* pool;
+        const srft_paged_seqs* seqs;
+        const srft_shared_prefixes* prefixes;
+        attended t;
+        if (n != 8 || !handle_of(a[0], &pool) || !handle_of(a[1], &seqs) || !handle_of(a[2], &prefixes) || !pool || !seqs || !prefixes || !PyFloat_CheckExact(a[5]) ||
+            !t.of(a[3], a[4], a[6], a[7]))
+            return false;
+        const int64_t need = g.pool_shared_bytes(pool, seqs, prefixes, t.tokens, t.heads);
+        if (need < 0 || t.bytes < need) return false;
+        const float scale = (float)PyFloat_AS_DOUBLE(a[5]);
+        *rc = without_gil([&] { return g.pool_shared(pool, seqs, prefixes, t.q, t.type, t.tokens, t.heads, t.qt, t.qh, scale, t.out, t.ot, t.oh, t.space, t.stream); });
+        return true;
+    });
+}
 // pool_copy(handles, count, pages, windows)
 PyObject* pool_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return made([&](int* rc) {
@@ -366,10 +518,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // bind(addresses, c_void_p, Array): of the entry points, in the order of the struct above.  True: they are the ones called here; False: those
 // of another library are, which came first.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    constexpr int kCount = 17;
+    constexpr int kCount = 24;
     void* p[kCount];
     if (n != kCount + 2 || !PyType_Check(a[kCount]) || !PyType_Check(a[kCount + 1])) {
-        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of 17 entry points, c_void_p and Array");
+        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of 24 entry points, c_void_p and Array");
         return nullptr;
     }
     for (int i = 0; i < kCount; ++i) {
@@ -386,11 +538,11 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g.bound = true;
     Py_RETURN_TRUE;
 }
-static_assert(offsetof(decltype(g), bound) == 17 * sizeof(void*), "bind fills the pointers in order");
+static_assert(offsetof(decltype(g), bound) == 24 * sizeof(void*), "bind fills the pointers in order");
 
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(quantize), FAST(dequantize), FAST(scores), FAST(attention), FAST(absmax), FAST(append), FAST(bind),
-                         FAST(rotary), FAST(pool_append), FAST(pool_attention), FAST(pool_copy),
+                         FAST(rotary), FAST(pool_append), FAST(pool_attention), FAST(pool_copy), FAST(norm_rotary), FAST(norm_backward), FAST(pool_sliding), FAST(pool_shared),
                          {"quantize_batched", quantize_batched, METH_O, nullptr},
                          {"dequantize_batched", dequantize_batched, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

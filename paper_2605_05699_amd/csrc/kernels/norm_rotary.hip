@@ -12,13 +12,14 @@
 
 namespace {
 
-constexpr int kAngles = 2048;                                // pairs (cos, sin) of a workgroup's tokens
+constexpr int kAngles = 1024;                                // pairs (cos, sin) of a workgroup's tokens
+constexpr int kLeastBlocks = 2048;                           // workgroups of a tensor that several tokens in one shall leave
 constexpr int kGradBlocks = 512;                             // workgroups of a tensor whose sums of the weights' gradient meet
 
 struct norm_shape {
     int row_units[2];                                        // of a row: those with pairs, all
-    int d, rot, pairs_layout, log_lanes, tokens;             // tokens: of a workgroup at a time
-    float factor, sign, eps;
+    int d, rot, pairs_layout, log_lanes;
+    float factor, eps;
     unsigned n_tokens;
     const int32_t* positions;
     const double* freq;
@@ -26,10 +27,12 @@ struct norm_shape {
 struct norm_args {
     norm_shape s;
     srft_norm_rows t[SRFT_ROTARY_MAX];
+    int tokens[SRFT_ROTARY_MAX], wide[SRFT_ROTARY_MAX];      // tokens of a workgroup at a time; whether weights are read V at a time
 };
 struct grad_args {
     norm_shape s;
     srft_norm_grad_rows t[SRFT_ROTARY_MAX];
+    int tokens[SRFT_ROTARY_MAX], wide[SRFT_ROTARY_MAX], blocks[SRFT_ROTARY_MAX];         // (blocks: workgroups)
     float* parts[SRFT_ROTARY_MAX];                           // [blocks][d] of a tensor whose weights' gradient is asked for, else null
 };
 
@@ -94,20 +97,31 @@ __device__ __forceinline__ void turn_unit(const norm_shape& s, int p, const floa
         for (int i = 0; i < V; ++i) two(f[i], g[i], cs[V * p + i]);
     }
 }
-__device__ __forceinline__ float weight_of(const void* w, int type, int c) {
-    return type == SRFT_F32 ? ((const float*)w)[c] : type == SRFT_F16 ? (float)((const _Float16*)w)[c] : (float)((const bf16*)w)[c];
-}
 // a lane's weights: of its K units (1 where there are none)
+template <class T, int V>
+__device__ __forceinline__ void weights_at(const T* w, int wide, float (&x)[V]) {
+    if (wide) {
+        load<T, V>(x, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (float)w[i];
+    }
+}
 template <int V, int K>
-__device__ __forceinline__ void weights_of(const norm_shape& s, const void* w, int type, int lane, float (&a)[K][V], float (&b)[K][V]) {
+__device__ __forceinline__ void weights_of(const norm_shape& s, const void* w, int type, int wide, int lane, float (&a)[K][V], float (&b)[K][V]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const unit_at at = unit_of<V>(s, min(lane + (k << s.log_lanes), s.row_units[1] - 1));
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            a[k][i] = w ? weight_of(w, type, at.first + i) : 1.0f;
-            b[k][i] = w ? weight_of(w, type, at.second + i) : 1.0f;
-        }
+        for (int i = 0; i < V; ++i) a[k][i] = b[k][i] = 1.0f;
+        if (!w) continue;                                    // (uniform, as what follows)
+        const unit_at at = unit_of<V>(s, min(lane + (k << s.log_lanes), s.row_units[1] - 1));
+        const auto both = [&](auto* p) __attribute__((always_inline)) {
+            weights_at(p + at.first, wide, a[k]);
+            weights_at(p + at.second, wide, b[k]);
+        };
+        if (type == SRFT_F32) both((const float*)w);
+        else if (type == SRFT_F16) both((const _Float16*)w);
+        else both((const bf16*)w);
     }
 }
 // angles of tokens first .. first + n - 1 (a barrier of the caller's behind)
@@ -120,91 +134,111 @@ __device__ __forceinline__ void angles_of(const norm_shape& s, unsigned first, i
     }
 }
 
-// One workgroup for s.tokens tokens (srft_grid).
+// blockIdx.z: the tensor; one workgroup of it for a.tokens tokens (srft_grid).  The first rows and the weights are on their way before the angles are computed.
 template <class IN, class OUT, int V, int K>
-__global__ void __launch_bounds__(256) srft_norm_rotary_kernel(const norm_args a, int count) {
+__global__ void __launch_bounds__(256) srft_norm_rotary_kernel(const norm_args a) {
     __shared__ float2 cs[kAngles];
     const norm_shape& s = a.s;
-    const unsigned first = (blockIdx.y * gridDim.x + blockIdx.x) * (unsigned)s.tokens;
+    const srft_norm_rows& t = a.t[blockIdx.z];
+    const unsigned tokens = a.tokens[blockIdx.z], first = (blockIdx.y * gridDim.x + blockIdx.x) * tokens;
     if (first >= s.n_tokens) return;                         // (uniform)
-    const int n = min((unsigned)s.tokens, s.n_tokens - first), lane = threadIdx.x & ((1 << s.log_lanes) - 1), half = s.rot >> 1;
+    const int n = min(tokens, s.n_tokens - first), lane = threadIdx.x & ((1 << s.log_lanes) - 1), half = s.rot >> 1;
+    const int heads = t.x.n_heads, rows = n * heads, step = blockDim.x >> s.log_lanes;
+    float f[K][V], g[K][V], wa[K][V], wb[K][V];
+    int token = 0, head = 0;
+    const auto fetch = [&](int r) __attribute__((always_inline)) {           // (rows past the last: that one again)
+        const int row = min(r, rows - 1);
+        token = (unsigned)row / (unsigned)heads, head = row - token * heads;
+        const IN* const x = (const IN*)t.x.in_dev + (first + token) * t.x.in_token + head * t.x.in_head;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const unit_at at = unit_of<V>(s, min(lane + (k << s.log_lanes), s.row_units[1] - 1));
+            load<IN, V>(f[k], x + at.first);
+            load<IN, V>(g[k], x + at.second);
+        }
+    };
+    int r = threadIdx.x >> s.log_lanes;
+    fetch(r);
+    weights_of<V, K>(s, t.weight_dev, t.weight_type, a.wide[blockIdx.z], lane, wa, wb);
     angles_of(s, first, n, cs);
     __syncthreads();
-    for (int m = 0; m < count; ++m) {
-        const srft_norm_rows& t = a.t[m];
-        const int heads = t.x.n_heads, rows = n * heads;
-        float wa[K][V], wb[K][V];
-        weights_of<V, K>(s, t.weight_dev, t.weight_type, lane, wa, wb);
-        for (int r0 = 0; r0 < rows; r0 += blockDim.x >> s.log_lanes) {
-            const int r = r0 + (threadIdx.x >> s.log_lanes), row = min(r, rows - 1), token = (unsigned)row / (unsigned)heads, head = row - token * heads;
-            const IN* const x = (const IN*)t.x.in_dev + (first + token) * t.x.in_token + head * t.x.in_head;
-            OUT* const y = (OUT*)t.x.out_dev + (first + token) * t.x.out_token + head * t.x.out_head;
-            float f[K][V], g[K][V], sum = 0.0f;
+    for (int r0 = 0;;) {
+        float sum = 0.0f;
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int p = lane + (k << s.log_lanes);
-                const unit_at at = unit_of<V>(s, min(p, s.row_units[1] - 1));
-                load<IN, V>(f[k], x + at.first);
-                load<IN, V>(g[k], x + at.second);
-                float here = 0.0f;
+        for (int k = 0; k < K; ++k) {
+            float here = 0.0f;
 #pragma unroll
-                for (int i = 0; i < V; ++i) here = fmaf(f[k][i], f[k][i], fmaf(g[k][i], g[k][i], here));
-                sum += p < s.row_units[1] ? here : 0.0f;
+            for (int i = 0; i < V; ++i) here = fmaf(f[k][i], f[k][i], fmaf(g[k][i], g[k][i], here));
+            sum += lane + (k << s.log_lanes) < s.row_units[1] ? here : 0.0f;
+        }
+        const float scale = 1.0f / sqrtf(row_sum(sum, s.log_lanes) / (float)s.d + s.eps);
+        OUT* const y = (OUT*)t.x.out_dev + (first + token) * t.x.out_token + head * t.x.out_head;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int p = lane + (k << s.log_lanes);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                f[k][i] = f[k][i] * scale * wa[k][i];
+                g[k][i] = g[k][i] * scale * wb[k][i];
             }
-            const float scale = 1.0f / sqrtf(row_sum(sum, s.log_lanes) / (float)s.d + s.eps);
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int p = lane + (k << s.log_lanes);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    f[k][i] = f[k][i] * scale * wa[k][i];
-                    g[k][i] = g[k][i] * scale * wb[k][i];
-                }
-                turn_unit<V, false>(s, p, cs + token * half, f[k], g[k]);
-                if (r < rows && p < s.row_units[1]) {
-                    const unit_at at = unit_of<V>(s, p);
-                    store<OUT, V>(f[k], y + at.first);
-                    store<OUT, V>(g[k], y + at.second);
-                }
+            turn_unit<V, false>(s, p, cs + token * half, f[k], g[k]);
+            if (r < rows && p < s.row_units[1]) {
+                const unit_at at = unit_of<V>(s, p);
+                store<OUT, V>(f[k], y + at.first);
+                store<OUT, V>(g[k], y + at.second);
             }
         }
+        r0 += step;
+        r += step;
+        if (r0 >= rows) break;                               // (uniform)
+        fetch(r);
     }
 }
 
-// blockIdx.y: the tensor; workgroup x of X takes the tokens s.tokens x .., then X s.tokens further on, and so on.
+// blockIdx.y: the tensor; workgroup x of a.blocks takes the tokens a.tokens x .., then a.blocks a.tokens further on, and so on.
 template <class IN, class DY, int V, int K>
 __global__ void __launch_bounds__(256) srft_norm_rotary_backward_kernel(const grad_args a) {
-    __shared__ float2 cs[kAngles];
+    __shared__ union {
+        float2 cs[kAngles];
+        float sums[4][1024];                                 // [wavefront][channel]
+    } lds;
+    float2* const cs = lds.cs;
     const norm_shape& s = a.s;
     const srft_norm_grad_rows& t = a.t[blockIdx.y];
-    const int lane = threadIdx.x & ((1 << s.log_lanes) - 1), half = s.rot >> 1, heads = t.n_heads;
+    const unsigned tokens = a.tokens[blockIdx.y], blocks = a.blocks[blockIdx.y];
+    if (blockIdx.x >= blocks) return;                        // (uniform)
+    const int lane = threadIdx.x & ((1 << s.log_lanes) - 1), half = s.rot >> 1, heads = t.n_heads, step = blockDim.x >> s.log_lanes;
     float* const part = a.parts[blockIdx.y];
-    float wa[K][V], wb[K][V], da[K][V], db[K][V];
-    weights_of<V, K>(s, t.weight_dev, t.weight_type, lane, wa, wb);
+    float f[K][V], g[K][V], u[K][V], v[K][V], wa[K][V], wb[K][V], da[K][V], db[K][V];
+    int token = 0, head = 0;
+    const auto fetch = [&](unsigned first, int rows, int r) __attribute__((always_inline)) {
+        const int row = min(r, rows - 1);
+        token = (unsigned)row / (unsigned)heads, head = row - token * heads;
+        const IN* const x = (const IN*)t.x_dev + (first + token) * t.x_token + head * t.x_head;
+        const DY* const dy = (const DY*)t.dy_dev + (first + token) * t.dy_token + head * t.dy_head;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const unit_at at = unit_of<V>(s, min(lane + (k << s.log_lanes), s.row_units[1] - 1));
+            load<IN, V>(f[k], x + at.first);
+            load<IN, V>(g[k], x + at.second);
+            load<DY, V>(u[k], dy + at.first);
+            load<DY, V>(v[k], dy + at.second);
+        }
+    };
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) da[k][i] = db[k][i] = 0.0f;
-    for (unsigned first = blockIdx.x * s.tokens; first < s.n_tokens; first += gridDim.x * s.tokens) {
-        const int n = min((unsigned)s.tokens, s.n_tokens - first), rows = n * heads;
+    for (unsigned first = blockIdx.x * tokens; first < s.n_tokens; first += blocks * tokens) {
+        const int n = min(tokens, s.n_tokens - first), rows = n * heads;
+        int r = threadIdx.x >> s.log_lanes;
+        fetch(first, rows, r);
+        if (first == blockIdx.x * tokens) weights_of<V, K>(s, t.weight_dev, t.weight_type, a.wide[blockIdx.y], lane, wa, wb);
         __syncthreads();                                     // (the angles before have been read)
         angles_of(s, first, n, cs);
         __syncthreads();
-        for (int r0 = 0; r0 < rows; r0 += blockDim.x >> s.log_lanes) {
-            const int r = r0 + (threadIdx.x >> s.log_lanes), row = min(r, rows - 1), token = (unsigned)row / (unsigned)heads, head = row - token * heads;
-            const IN* const x = (const IN*)t.x_dev + (first + token) * t.x_token + head * t.x_head;
-            const DY* const dy = (const DY*)t.dy_dev + (first + token) * t.dy_token + head * t.dy_head;
-            IN* const dx = (IN*)t.dx_dev + (first + token) * t.dx_token + head * t.dx_head;
-            float f[K][V], g[K][V], u[K][V], v[K][V], sum = 0.0f, both = 0.0f;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int p = lane + (k << s.log_lanes);
-                const unit_at at = unit_of<V>(s, min(p, s.row_units[1] - 1));
-                load<IN, V>(f[k], x + at.first);
-                load<IN, V>(g[k], x + at.second);
-                load<DY, V>(u[k], dy + at.first);
-                load<DY, V>(v[k], dy + at.second);
-            }
+        for (int r0 = 0;;) {
+            float sum = 0.0f, both = 0.0f;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int p = lane + (k << s.log_lanes);
@@ -220,6 +254,7 @@ __global__ void __launch_bounds__(256) srft_norm_rotary_backward_kernel(const gr
             }
             const float scale = 1.0f / sqrtf(row_sum(sum, s.log_lanes) / (float)s.d + s.eps);
             const float along = row_sum(both, s.log_lanes) / (float)s.d * scale * scale;
+            IN* const dx = (IN*)t.dx_dev + (first + token) * t.dx_token + head * t.dx_head;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int p = lane + (k << s.log_lanes);
@@ -237,11 +272,16 @@ __global__ void __launch_bounds__(256) srft_norm_rotary_backward_kernel(const gr
                     store<IN, V>(g[k], dx + at.second);
                 }
             }
+            r0 += step;
+            r += step;
+            if (r0 >= rows) break;                           // (uniform)
+            fetch(first, rows, r);
         }
     }
     if (!part) return;                                       // (uniform)
     // ---- the workgroup's sums: a wavefront's lanes with the same channels, then its wavefronts
-    __shared__ float sums[4][1024];                          // [wavefront][channel]
+    __syncthreads();                                         // (the last angles have been read)
+    float (*const sums)[1024] = lds.sums;
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -268,22 +308,31 @@ __global__ void __launch_bounds__(256) srft_norm_rotary_backward_kernel(const gr
 struct grad_sums {
     const float* parts[SRFT_ROTARY_MAX];
     float* dweight[SRFT_ROTARY_MAX];
+    int blocks[SRFT_ROTARY_MAX];
 };
-__global__ void __launch_bounds__(256) srft_norm_rotary_sums_kernel(const grad_sums a, int blocks, int d) {
-    __shared__ float sums[16][17];
+__global__ void __launch_bounds__(1024) srft_norm_rotary_sums_kernel(const grad_sums a, int d) {
+    constexpr int TEAMS = 64;
+    __shared__ float sums[TEAMS][17];
     const float* const parts = a.parts[blockIdx.y];
-    const int c = blockIdx.x * 16 + (threadIdx.x & 15), from = threadIdx.x >> 4;
-    float x = 0.0f;
-#pragma unroll 8
-    for (int b = from; b < blocks; b += 16) x += parts[(long long)b * d + min(c, d - 1)];
-    sums[from][threadIdx.x & 15] = x;
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), from = threadIdx.x >> 4, blocks = a.blocks[blockIdx.y];
+    float x[kGradBlocks / TEAMS];
+#pragma unroll
+    for (int i = 0; i < kGradBlocks / TEAMS; ++i) {          // (all on their way together)
+        const int b = from + TEAMS * i;
+        x[i] = b < blocks ? parts[(long long)b * d + min(c, d - 1)] : 0.0f;
+    }
+    float sum = x[0];
+#pragma unroll
+    for (int i = 1; i < kGradBlocks / TEAMS; ++i) sum += x[i];
+    sums[from][threadIdx.x & 15] = sum;
     __syncthreads();
     if (from > 0 || c >= d) return;
-    for (int i = 1; i < 16; ++i) x += sums[i][threadIdx.x & 15];
-    a.dweight[blockIdx.y][c] = x;
+    float all = 0.0f;
+    for (int i = 0; i < TEAMS; ++i) all += sums[i][threadIdx.x & 15];
+    a.dweight[blockIdx.y][c] = all;
 }
 
-typedef void (*norm_kernel_t)(const norm_args, int);
+typedef void (*norm_kernel_t)(const norm_args);
 typedef void (*grad_kernel_t)(const grad_args);
 // the instance for V pairs a thread and K units a lane
 template <class A, class B> norm_kernel_t norm_of(int v, int k) {
@@ -340,8 +389,12 @@ int split_rows(norm_shape& s, int v) {
     while (s.log_lanes < 6 && (1 << s.log_lanes) < s.row_units[1]) ++s.log_lanes;
     return (s.row_units[1] + (1 << s.log_lanes) - 1) >> s.log_lanes;
 }
-int threads_of(const norm_shape& s, int heads) { return (int)std::min<int64_t>(256, (((int64_t)s.tokens * heads << s.log_lanes) + 63) / 64 * 64); }
-
+// Tokens of a workgroup of a tensor: up to four rows a lane, as far as that leaves `least` workgroups, and the LDS its angles.
+int tokens_of(const norm_shape& s, int heads, int least) {
+    const int64_t rows = 4 * (256 >> s.log_lanes), fit = s.rot > 0 ? kAngles / (s.rot / 2) : kAngles;
+    return (int)std::max<int64_t>(1, std::min({rows / heads, fit, (int64_t)s.n_tokens / least}));
+}
+int threads_of(const norm_shape& s, int tokens, int heads) { return (int)std::min<int64_t>(256, (((int64_t)tokens * heads << s.log_lanes) + 63) / 64 * 64); }
 }  // namespace
 
 extern "C" {
@@ -379,18 +432,24 @@ int srft_norm_rotary(const srft_norm_rows* rows, int count, int64_t n_tokens, in
         const srft_rotary_rows& x = rows[i].x;
         const int v = width(x);
         norm_args a = {};
-        int n = 0, heads = 0;
-        for (int k = i; k < count; ++k) {
-            const srft_rotary_rows& y = rows[k].x;
-            if (done[k] || y.in_type != x.in_type || y.out_type != x.out_type || width(y) != v) continue;
-            done[k] = true;
-            a.t[n++] = rows[k];
-            heads = std::max(heads, y.n_heads);
-        }
-        a.s = {{0, 0}, d, rot, layout == SRFT_ROTARY_PAIRS, 0, 1, (float)factor, 0.0f, (float)eps, (unsigned)n_tokens, positions_dev, freq_dev};
+        a.s = {{0, 0}, d, rot, layout == SRFT_ROTARY_PAIRS, 0, (float)factor, (float)eps, (unsigned)n_tokens, positions_dev, freq_dev};
         const int k = split_rows(a.s, v);
-        const norm_kernel_t kernel = norm_of(x.in_type, x.out_type, v, k);
-        rc = srft_launch(kernel, srft_grid((n_tokens + a.s.tokens - 1) / a.s.tokens), threads_of(a.s, heads), (hipStream_t)hip_stream, a, n);
+        int n = 0, threads = 64;
+        int64_t blocks = 0;
+        for (int j = i; j < count; ++j) {
+            const srft_rotary_rows& y = rows[j].x;
+            if (done[j] || y.in_type != x.in_type || y.out_type != x.out_type || width(y) != v) continue;
+            done[j] = true;
+            a.t[n] = rows[j];
+            a.wide[n] = srft_aligned(rows[j].weight_dev, std::min(16, v * type_bytes(rows[j].weight_type)));
+            a.tokens[n] = tokens_of(a.s, y.n_heads, kLeastBlocks);
+            threads = std::max(threads, threads_of(a.s, a.tokens[n], y.n_heads));
+            blocks = std::max(blocks, (n_tokens + a.tokens[n] - 1) / a.tokens[n]);
+            ++n;
+        }
+        dim3 grid = srft_grid(blocks);
+        grid.z = (unsigned)n;
+        rc = srft_launch(norm_of(x.in_type, x.out_type, v, k), grid, threads, (hipStream_t)hip_stream, a);
         if (rc != SRFT_OK) return rc;
     }
     return SRFT_OK;
@@ -440,25 +499,30 @@ int srft_norm_rotary_backward(const srft_norm_grad_rows* rows, int count, int64_
         });
     };
     const auto part = [&](int i) { return (float*)workspace_dev + (int64_t)i * kGradBlocks * d; };
-    const int tokens = 1, blocks = (int)std::min<int64_t>((n_tokens + tokens - 1) / tokens, kGradBlocks);
+    int part_blocks[SRFT_ROTARY_MAX] = {};
     bool done[SRFT_ROTARY_MAX] = {};
     for (int i = 0; i < count && n_tokens > 0; ++i) {
         if (done[i]) continue;
         const srft_norm_grad_rows& x = rows[i];
         const int v = width(x);
         grad_args a = {};
-        int n = 0, heads = 0;
-        for (int k = i; k < count; ++k) {
-            const srft_norm_grad_rows& y = rows[k];
-            if (done[k] || y.x_type != x.x_type || y.dy_type != x.dy_type || width(y) != v) continue;
-            done[k] = true;
-            a.parts[n] = y.dweight_dev ? part(k) : nullptr;
-            a.t[n++] = y;
-            heads = std::max(heads, y.n_heads);
-        }
-        a.s = {{0, 0}, d, rot, layout == SRFT_ROTARY_PAIRS, 0, tokens, (float)factor, 0.0f, (float)eps, (unsigned)n_tokens, positions_dev, freq_dev};
+        a.s = {{0, 0}, d, rot, layout == SRFT_ROTARY_PAIRS, 0, (float)factor, (float)eps, (unsigned)n_tokens, positions_dev, freq_dev};
         const int k = split_rows(a.s, v);
-        rc = srft_launch(grad_of(x.x_type, x.dy_type, v, k), dim3((unsigned)blocks, (unsigned)n), threads_of(a.s, heads), st, a);
+        int n = 0, threads = 64, blocks = 0;
+        for (int j = i; j < count; ++j) {
+            const srft_norm_grad_rows& y = rows[j];
+            if (done[j] || y.x_type != x.x_type || y.dy_type != x.dy_type || width(y) != v) continue;
+            done[j] = true;
+            a.t[n] = y;
+            a.wide[n] = srft_aligned(y.weight_dev, std::min(16, v * type_bytes(y.weight_type)));
+            a.tokens[n] = tokens_of(a.s, y.n_heads, kGradBlocks);
+            a.blocks[n] = part_blocks[j] = (int)std::min<int64_t>((n_tokens + a.tokens[n] - 1) / a.tokens[n], kGradBlocks);
+            a.parts[n] = y.dweight_dev ? part(j) : nullptr;
+            threads = std::max(threads, threads_of(a.s, a.tokens[n], y.n_heads));
+            blocks = std::max(blocks, a.blocks[n]);
+            ++n;
+        }
+        rc = srft_launch(grad_of(x.x_type, x.dy_type, v, k), dim3((unsigned)blocks, (unsigned)n), threads, st, a);
         if (rc != SRFT_OK) return rc;
     }
     if (!sums) return SRFT_OK;
@@ -467,9 +531,10 @@ int srft_norm_rotary_backward(const srft_norm_grad_rows* rows, int count, int64_
     for (int i = 0; i < count; ++i)
         if (rows[i].dweight_dev) {
             g.parts[n] = part(i);
+            g.blocks[n] = part_blocks[i];
             g.dweight[n++] = rows[i].dweight_dev;
         }
-    return srft_launch(srft_norm_rotary_sums_kernel, dim3((unsigned)((d + 15) / 16), (unsigned)n), 256, st, g, blocks, d);
+    return srft_launch(srft_norm_rotary_sums_kernel, dim3((unsigned)((d + 15) / 16), (unsigned)n), 1024, st, g, d);
 }
 
 }  // extern "C"

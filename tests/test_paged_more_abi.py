@@ -43,3 +43,15 @@ def test_binding_refuses_prefixes_that_are_not_on_the_device():
     for bad in ((groups, tokens), (groups, tokens[:1]), (groups[None], tokens), (groups, tokens.long())):
         with pytest.raises(ValueError):
             B.SharedPrefixes(*bad)
+
+
+@pytest.mark.parametrize("name, n", [("norm_rotary", 6), ("norm_backward", 7), ("pool_sliding", 9), ("pool_shared", 8)])
+def test_native_calls_leave_what_is_not_on_the_device_to_the_binding(L, name, n):
+    f, x = getattr(B._marshal, name), torch.zeros(4, 2, 64, dtype=torch.float16)
+    for a in (x, None, 0, "x", 1.0, True, [(x, x)], [x], [(x, None, x)], [(x, x, None, x, None)], torch.nn.Parameter(x), 1 << 70):
+        assert f(*([a] * n)) is None
+    assert f() is None and f(*[x] * (n + 1)) is None
+    pos, freq = torch.zeros(4, dtype=torch.int32), torch.zeros(32, dtype=torch.float64)
+    assert B._marshal.norm_rotary([(x, None, x)], pos, freq, 0, 1.0, 1e-6) is None
+    assert B._marshal.norm_backward([(x, x, None, x, None)], pos, freq, 0, 1.0, 1e-6, None) is None
+    assert B._marshal.pool_sliding(64, 64, 64, x, 0.1, 1, 1, x, x) is None and B._marshal.pool_shared(64, 64, 64, 64, x, 0.1, x, x) is None
