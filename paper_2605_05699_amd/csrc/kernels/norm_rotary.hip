@@ -389,10 +389,10 @@ int split_rows(norm_shape& s, int v) {
     while (s.log_lanes < 6 && (1 << s.log_lanes) < s.row_units[1]) ++s.log_lanes;
     return (s.row_units[1] + (1 << s.log_lanes) - 1) >> s.log_lanes;
 }
-// Tokens of a workgroup of a tensor: up to four rows a lane, as far as that leaves `least` workgroups, and the LDS its angles.
-int tokens_of(const norm_shape& s, int heads, int least) {
+// Tokens of a workgroup of a tensor: up to four rows a lane, up to `most`, and as many as the LDS has angles for.
+int tokens_of(const norm_shape& s, int heads, int64_t most) {
     const int64_t rows = 4 * (256 >> s.log_lanes), fit = s.rot > 0 ? kAngles / (s.rot / 2) : kAngles;
-    return (int)std::max<int64_t>(1, std::min({rows / heads, fit, (int64_t)s.n_tokens / least}));
+    return (int)std::max<int64_t>(1, std::min({rows / heads, fit, most}));
 }
 int threads_of(const norm_shape& s, int tokens, int heads) { return (int)std::min<int64_t>(256, (((int64_t)tokens * heads << s.log_lanes) + 63) / 64 * 64); }
 }  // namespace
@@ -442,7 +442,7 @@ int srft_norm_rotary(const srft_norm_rows* rows, int count, int64_t n_tokens, in
             done[j] = true;
             a.t[n] = rows[j];
             a.wide[n] = srft_aligned(rows[j].weight_dev, std::min(16, v * type_bytes(rows[j].weight_type)));
-            a.tokens[n] = tokens_of(a.s, y.n_heads, kLeastBlocks);
+            a.tokens[n] = tokens_of(a.s, y.n_heads, n_tokens / kLeastBlocks);
             threads = std::max(threads, threads_of(a.s, a.tokens[n], y.n_heads));
             blocks = std::max(blocks, (n_tokens + a.tokens[n] - 1) / a.tokens[n]);
             ++n;
@@ -515,7 +515,7 @@ int srft_norm_rotary_backward(const srft_norm_grad_rows* rows, int count, int64_
             done[j] = true;
             a.t[n] = y;
             a.wide[n] = srft_aligned(y.weight_dev, std::min(16, v * type_bytes(y.weight_type)));
-            a.tokens[n] = tokens_of(a.s, y.n_heads, kGradBlocks);
+            a.tokens[n] = tokens_of(a.s, y.n_heads, (n_tokens + kGradBlocks - 1) / kGradBlocks);
             a.blocks[n] = part_blocks[j] = (int)std::min<int64_t>((n_tokens + a.tokens[n] - 1) / a.tokens[n], kGradBlocks);
             a.parts[n] = y.dweight_dev ? part(j) : nullptr;
             threads = std::max(threads, threads_of(a.s, a.tokens[n], y.n_heads));

@@ -27,6 +27,8 @@ template <int NT>
 __device__ __forceinline__ void make_items(const pool_attention_args& a) {
     const pool_seqs& s = a.s;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    __shared__ int few[256];                                 // the bounds, where there are few
+    const bool is_few = a.n_groups < 256;
     if (wave == 0) {
         int before = 0;
         for (int g0 = 0; g0 <= a.n_groups; g0 += 64) {
@@ -36,7 +38,7 @@ __device__ __forceinline__ void make_items(const pool_attention_args& a) {
                 const int other = __shfl_up(x, d);
                 if (lane >= d) x = max(x, other);
             }
-            if (g0 + lane <= a.n_groups) a.bounds[g0 + lane] = x;
+            if (g0 + lane <= a.n_groups) (is_few ? few : a.bounds)[g0 + lane] = x;
             before = __shfl(x, 63);
         }
     }
@@ -46,7 +48,8 @@ __device__ __forceinline__ void make_items(const pool_attention_args& a) {
     }
     __syncthreads();
     for (int g = wave; g < a.n_groups; g += NT / 64) {
-        const int b0 = a.bounds[g], b1 = a.bounds[g + 1];
+        const int* const bounds = is_few ? few : a.bounds;
+        const int b0 = bounds[g], b1 = bounds[g + 1];
         int least = kPoolMaxLength, first = s.n_seq, end = 0, count = 0;
         for (int b = b0 + lane; b < b1; b += 64) {
             const pool_seq q = pool_seq_of(s, b);
@@ -79,15 +82,27 @@ __device__ __forceinline__ void count_units(const pool_attention_args& a) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     if constexpr (FORM == kPoolShared) make_items<NT>(a);
     const int n_seq = pool_count<FORM>(a);
-    // the sequences' own units first, then their sums in place
-    for (int b = wave; b < n_seq; b += NT / 64) {
+    // The sequences' own units first, then their sums in place.  A lane has a sequence; the tiles of those with many blocks of rows are added up by
+    // the whole wavefront (with a wavefront a sequence, a chain of loads each, 48 of them took 12 us).
+    for (int b0 = 64 * wave; b0 < n_seq; b0 += NT) {
+        const int b = min(b0 + lane, n_seq - 1);
         const pool_seq q = pool_view_of<FORM>(a, b).q;
         const bool decode = pool_is_decode<FORM>(a, q, b);
-        const int chunk = decode || q.n_new == 0 ? 0 : a.heads * pool_chunk_units<FORM>(a, q, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS);
-        if (lane == 0) {
-            if (a.blocks_before) a.blocks_before[b + 1] = decode ? 0 : (q.n_new * a.group + ROWS - 1) / ROWS;
+        const int blocks = decode ? 0 : (q.n_new * a.group + ROWS - 1) / ROWS;
+        int chunk = 0;
+        if (blocks <= 4)
+            for (int rt = 0; rt < blocks; ++rt) chunk += pool_chunk_cost<FORM>(pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, rt));
+        for (uint64_t many = __ballot(blocks > 4 && b0 + lane < n_seq); many; many &= many - 1) {
+            const int i = __builtin_ctzll(many);
+            const pool_seq p{__builtin_amdgcn_readlane(q.start, i), __builtin_amdgcn_readlane(q.n_new, i), __builtin_amdgcn_readlane(q.length, i),
+                             __builtin_amdgcn_readlane(q.before, i), __builtin_amdgcn_readlane(q.full, i)};
+            const int units = pool_chunk_units<FORM>(a, p, ROWS, KEYS, __builtin_amdgcn_readlane(blocks, i));
+            chunk = lane == i ? units : chunk;
+        }
+        if (b0 + lane < n_seq) {
+            if (a.blocks_before) a.blocks_before[b + 1] = blocks;
             a.decode_before[b + 1] = decode ? a.heads * ((q.n_new * a.group + a.decode_block - 1) / a.decode_block) * pool_decode_cost<FORM>(pool_decode_tiles<FORM>(a, q, a.decode_keys)) : 0;
-            a.chunk_before[b + 1] = chunk;
+            a.chunk_before[b + 1] = a.heads * chunk;
         }
     }
     __syncthreads();
