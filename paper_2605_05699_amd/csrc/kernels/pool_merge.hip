@@ -10,6 +10,13 @@
 
 namespace {
 
+// positions 4 half .. + 3 of a unit of eight channels
+__device__ __forceinline__ floatx4 by_position(const float* unit, int half, int bits) {
+    const floatx4 y = reinterpret_cast<const floatx4*>(unit)[0], z = reinterpret_cast<const floatx4*>(unit)[1];
+    if (bits == 8) return half ? floatx4{z[0], z[2], z[1], z[3]} : floatx4{y[0], y[2], y[1], y[3]};
+    return half ? floatx4{y[2], z[2], y[3], z[3]} : floatx4{y[0], z[0], y[1], z[1]};
+}
+
 template <int D, int FORM>
 __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsigned workgroup, uint4* ops, float (*tops)[32]) {
     constexpr int BLOCKS = kPoolChunkWaves, ROWS = kPoolBlock * BLOCKS, KEYS = kPoolChunkKeys<D>, G = D / 32, T = D / 16, OWN = (G + kPoolTeam - 1) / kPoolTeam, AHEAD = 2;
@@ -74,22 +81,24 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     };
     if (joint) {
         const long long r_at = (long long)row.token * (a.heads * a.group) + row.head;
+        const pool_common p(a, view, head, KEYS);
+        const bool common_chunk = p.chunk;
         // rows whose tokens (own: 0, in common: 1) one workgroup has had all of; the others as they are
         const auto whole = [&](int which, bool in) __attribute__((always_inline)) {
-            const floatx4 x = reinterpret_cast<const floatx4*>(a.joint_heads[which])[r_at];
-            pool_part_head h[1] = {{x[0], x[1], x[2], 0.0f}};
-            if (!in) h[0] = {kPoolLowest, 0.0f, __uint_as_float((uint32_t)kPoolNoExponent), 0.0f};
+            pool_part_head h[1];
+            h[0].load4(a.joint_heads[which] + 4 * r_at, in);
             const float before = pool_join(t_all, den, e_all, h, 0, 0);
 #pragma unroll
             for (int i = 0; i < OWN; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const floatx4 y = pool_block<D>::get4(a.joint_rows[which] + r_at * D, 4 * min(wave + kPoolTeam * i, G - 1) + j, half, a.bits);
+                    const int u = 4 * min(wave + kPoolTeam * i, G - 1) + j;
+                    const floatx4 y = which == 1 && !common_chunk ? by_position(a.joint_rows[1] + r_at * D + 8 * u, half, a.bits)
+                                                                  : *reinterpret_cast<const floatx4*>(a.joint_rows[which] + r_at * D + 8 * u + 4 * half);
 #pragma unroll
                     for (int m = 0; m < 4; ++m) sums[i][4 * j + m] = fmaf(in ? y[m] : 0.0f, h[0].factor, sums[i][4 * j + m] * before);
                 }
         };
-        const pool_common p(a, view.group, head, KEYS);
         const int before_rows = (q.start - p.p.start) * a.group, n_rows = q.n_new * a.group, from = before_rows + r0, to = before_rows + min(r0 + 31, n_rows - 1);
         const int mine = min(from + (lane & 31), to);
         if (p.there && from >= 0 && to < p.p.n_new * a.group)       // (starts that are not ascending: anything)
@@ -104,9 +113,7 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
                 for (int v = v0; v <= v1; v += AHEAD)
                     join(v, v1,
                          [&](int w, pool_part_head& h) __attribute__((always_inline)) {
-                             const float* const x = p.template heads<D>(p.template part<D>(a, b, w, w == v0, r), r);
-                             h = {x[0], x[64], x[128], 0.0f};
-                             if (!in) h = {kPoolLowest, 0.0f, __uint_as_float((uint32_t)kPoolNoExponent), 0.0f};
+                             h.load4(p.template heads<D>(p.template part<D>(a, b, w, w == v0, r), r), in);
                          },
                          [&](int w, int n) __attribute__((always_inline)) {
                              const floatx4 x = p.positions(p.template part<D>(a, b, w, w == v0, r), r, n, half, a.bits);

@@ -44,7 +44,7 @@ __device__ __forceinline__ void make_items(const pool_attention_args& a) {
     }
     for (int b = threadIdx.x; b < s.n_seq; b += NT) {
         const pool_seq q = pool_seq_of(s, b);
-        a.items[b] = {q.start, q.n_new, q.length, q.before, q.full, b, 0, -1};
+        a.items[b] = {q.start, q.n_new, q.length, q.before, q.full, b, 0, -1, 0, 0, 0, 0};
     }
     __syncthreads();
     for (int g = wave; g < a.n_groups; g += NT / 64) {
@@ -65,11 +65,12 @@ __device__ __forceinline__ void make_items(const pool_attention_args& a) {
         count = pool_wave_sum(count);
         const int common = count > 1 ? min(max(a.shared[g], 0), max(least, 0)) >> s.log_R << s.log_R : 0;            // (uniform)
         const int start = common > 0 ? pool_seq_of(s, first).start : 0;
-        if (lane == 0) a.items[s.n_seq + g] = {start, common > 0 ? max(end - start, 0) : 0, common, common, common, common > 0 ? first : 0, 0, -1};
+        const int n_new = common > 0 ? max(end - start, 0) : 0;
+        if (lane == 0) a.items[s.n_seq + g] = {start, n_new, common, common, common, common > 0 ? first : 0, 0, -1, 0, 0, 0, 0};
         if (common > 0)
             for (int b = b0 + lane; b < b1; b += 64) {
                 const pool_seq q = pool_seq_of(s, b);
-                if (q.n_new > 0) a.items[b] = {q.start, q.n_new, q.length - common, q.before - common, q.full - common, b, common >> s.log_R, g};
+                if (q.n_new > 0) a.items[b] = {q.start, q.n_new, q.length - common, q.before - common, q.full - common, b, common >> s.log_R, g, start, n_new, common, 0};
             }
     }
     __syncthreads();

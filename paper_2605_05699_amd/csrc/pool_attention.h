@@ -51,8 +51,10 @@ struct pool_item {
     int start, n_new, length, before, full;                  // as pool_seq, without the tokens in front of first_page
     int seq, first_page;                                     // whose page table and windows; the first page of the item in it
     int group;                                               // the group that a sequence shares pages with, or -1
+    int common_start, common_n_new, common;                  // of that group: rows of its new tokens, tokens in common
+    int unused;
 };
-static_assert(sizeof(pool_item) == 32, "two loads");
+static_assert(sizeof(pool_item) == 48, "three loads");
 
 struct pool_attention_args {
     pool_seqs s;
@@ -85,8 +87,9 @@ struct pool_attention_args {
     int common_rows;                                         // a group's rows up to which its tokens in common go to pool_decode
     int* bounds;                                             // [n_groups + 1]: groups, ascending and within n_seq (workspace)
     pool_item* items;                                        // [n_seq + n_groups] (workspace)
-    float *joint_rows[2], *joint_heads[2];                   // [n_new][n_q_heads][D] and [4]: sums by channel and maximum, sum of weights, exponent, where one
-                                                             // workgroup has had all of a row's own tokens [0], or of those in common [1] (workspace)
+    float *joint_rows[2], *joint_heads[2];                   // [n_new][n_q_heads][D] and [4]: sums (by position from pool_chunk, by channel from pool_decode) and
+                                                             // maximum, sum of weights, exponent, where one workgroup has had all of a row's own
+                                                             // tokens [0], or of those in common [1] (workspace)
 };
 // Sums of a block of 32 rows that a segment leaves: [D / 8 float4][64 lanes], then per lane maximum, sum of weights and V's exponent.
 template <int D> constexpr int kPoolPart = 32 * D + 3 * 64;
@@ -174,15 +177,16 @@ struct pool_view {
     pool_seq q;
     int seq, first_page;
     int group;                                               // whose tokens in common it has in front of its own, or -1
+    pool_seq of_group;                                       // these, as a sequence (start, n_new, length and full are looked at)
 };
 template <int FORM> __device__ __forceinline__ int pool_count(const pool_attention_args& a) { return FORM == kPoolShared ? a.s.n_seq + a.n_groups : a.s.n_seq; }
 template <int FORM>
 __device__ __forceinline__ pool_view pool_view_of(const pool_attention_args& a, int i) {
     if constexpr (FORM == kPoolShared) {
         const pool_item t = a.items[i];
-        return {{t.start, t.n_new, t.length, t.before, t.full}, t.seq, t.first_page, t.group};
+        return {{t.start, t.n_new, t.length, t.before, t.full}, t.seq, t.first_page, t.group, {t.common_start, t.common_n_new, t.common, t.common, t.common}};
     }
-    return {pool_seq_of(a.s, i), i, 0, -1};
+    return {pool_seq_of(a.s, i), i, 0, -1, {}};
 }
 // sum over the lanes of a wavefront, in all of them
 __device__ __forceinline__ int pool_wave_sum(int x) {
@@ -234,6 +238,12 @@ __device__ __forceinline__ float pool_power(int e) { return __uint_as_float((uin
 struct pool_part_head {
     float top, den, e, factor;
     __device__ __forceinline__ void load(const float* p, int lane) { top = p[lane], den = p[64 + lane], e = p[128 + lane]; }
+    __device__ __forceinline__ void load4(const float* p, bool in) {         // (a row that is not there counts for nothing)
+        const floatx4 x = *reinterpret_cast<const floatx4*>(p);
+        top = in ? x[0] : kPoolLowest;
+        den = in ? x[1] : 0.0f;
+        e = __uint_as_float(in ? __float_as_uint(x[2]) : (uint32_t)kPoolNoExponent);
+    }
 };
 // Parts v .. v + N - 1 (those behind the last, w1, are it again and count for nothing) under one maximum with what has been added so far; what its
 // sums are to be multiplied with.
@@ -318,32 +328,19 @@ template <int D> struct pool_block {
 #pragma unroll
         for (int b = 0; b < D / 32; ++b) sums[b] *= f;
     }
-    // Four positions of the lane's row, 4 (l / 32) on in unit u of eight, to and from the row's channels (see "Order of channels").
-    static __device__ __forceinline__ void put4(float* row, int u, int half, floatx4 x, int bits) {
-        typedef float pair __attribute__((ext_vector_type(2)));
-        if (bits == 8) {
-            *reinterpret_cast<floatx4*>(row + 8 * u + 4 * half) = floatx4{x[0], x[2], x[1], x[3]};
-        } else {
-            *reinterpret_cast<pair*>(row + 8 * u + 2 * half) = pair{x[0], x[2]};
-            *reinterpret_cast<pair*>(row + 8 * u + 2 * half + 4) = pair{x[1], x[3]};
-        }
-    }
-    static __device__ __forceinline__ floatx4 get4(const float* row, int u, int half, int bits) {
-        typedef float pair __attribute__((ext_vector_type(2)));
-        if (bits == 8) {
-            const floatx4 x = *reinterpret_cast<const floatx4*>(row + 8 * u + 4 * half);
-            return floatx4{x[0], x[2], x[1], x[3]};
-        }
-        const pair x = *reinterpret_cast<const pair*>(row + 8 * u + 2 * half), y = *reinterpret_cast<const pair*>(row + 8 * u + 2 * half + 4);
-        return floatx4{x[0], y[0], x[1], y[1]};
-    }
+    // of tokens in common: the three numbers of a row next to each other
+    __device__ __forceinline__ floatx4 head() const { return floatx4{top, den, __uint_as_float((uint32_t)e), 0.0f}; }
     // p: kPoolPart<D> floats in memory or LDS
-    __device__ __forceinline__ void put(float* p, int lane) const {
+    __device__ __forceinline__ void put(float* p, int lane, bool common = false) const {
 #pragma unroll
         for (int b = 0; b < D / 32; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 reinterpret_cast<floatx4*>(p)[(4 * b + i) * 64 + lane] = floatx4{sums[b][4 * i], sums[b][4 * i + 1], sums[b][4 * i + 2], sums[b][4 * i + 3]};
+        if (common) {                                        // (uniform)
+            if (lane < 32) reinterpret_cast<floatx4*>(p + 32 * D)[lane] = head();
+            return;
+        }
         p[32 * D + lane] = top;
         p[32 * D + 64 + lane] = den;
         p[32 * D + 128 + lane] = __uint_as_float((uint32_t)e);

@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
 #pragma unroll
             for (int j = 0; j < kPoolAhead; ++j) f[j] = read_v(j);
             const int last = min(row_last, last_key) - key0;
-            if (FORM == kPoolSliding && __ballot(row_first > key0)) {        // (a row's recent tokens begin in the tile: `last` as below)
+            if (FORM == kPoolSliding && key0 <= wave_last - a.recent) {        // (a row's recent tokens begin in the tile: `last` as below)
                 const int limit = last - 4 * half, from = row_first - key0 - 4 * half, sinks = a.sinks - key0 - 4 * half;
 #pragma unroll
                 for (int n = 0; n < KB; ++n)
@@ -321,8 +321,9 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
                 for (int k = 0; k < D / 32; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        b.put4(a.joint_rows[which] + at * D, 4 * k + i, half, floatx4{b.sums[k][4 * i], b.sums[k][4 * i + 1], b.sums[k][4 * i + 2], b.sums[k][4 * i + 3]}, BITS);
-                if (half == 0) reinterpret_cast<floatx4*>(a.joint_heads[which])[at] = floatx4{b.top, b.den, __uint_as_float((uint32_t)b.e), 0.0f};
+                        *reinterpret_cast<floatx4*>(a.joint_rows[which] + at * D + 8 * (4 * k + i) + 4 * half) =
+                            floatx4{b.sums[k][4 * i], b.sums[k][4 * i + 1], b.sums[k][4 * i + 2], b.sums[k][4 * i + 3]};
+                if (half == 0) reinterpret_cast<floatx4*>(a.joint_heads[which])[at] = b.head();
             }
         } else if (t0 == 0 && t1 == tiles) {
             int again = lane;                                // (computed again: kept, the row took registers that the loop lacks at 256 dimensions)
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
             char* const to = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
             pool_finish<D>(b, a.out_table, a.out_unscale, to, a.bf16, lane);
         } else {
-            b.put(a.chunk_parts + ((2LL * w + (at_begin ? 0 : 1)) * W + wave) * kPoolPart<D>, lane);
+            b.put(a.chunk_parts + ((2LL * w + (at_begin ? 0 : 1)) * W + wave) * kPoolPart<D>, lane, FORM == kPoolShared && seq >= a.s.n_seq);
         }
     }
 }

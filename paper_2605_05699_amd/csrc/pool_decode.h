@@ -182,14 +182,19 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
     // The first segment's sequence: where the sequences fit the lanes, all that it takes comes with one round of loads (a step of 4
     // sequences up to 1000 tokens: 12.6 us with this and with the first tile's loads before the queries are in LDS, 13.5 to 14 one after the other).
     const int n_seq = pool_count<FORM>(a);
-    const bool few = FORM != kPoolShared && n_seq < 64;
-    int of_before = 0, of_start = 0, of_length = 0;          // lane b: of sequence b
+    const bool few = n_seq < (FORM == kPoolShared ? 128 : 64);
+    int of_before = 0, of_start = 0, of_length = 0;          // lane b: of sequence b (shared: of_start, the units in front of item 64 + b)
     if (few) {
         of_before = a.decode_before[min(lane, n_seq)];
-        of_start = a.s.starts[min(lane, n_seq)];
-        of_length = a.s.lengths[min(lane, n_seq - 1)];
+        if constexpr (FORM == kPoolShared) {
+            of_start = a.decode_before[min(64 + lane, n_seq)];
+        } else {
+            of_start = a.s.starts[min(lane, n_seq)];
+            of_length = a.s.lengths[min(lane, n_seq - 1)];
+        }
     }
-    const int total = few ? __builtin_amdgcn_readlane(of_before, n_seq) : a.decode_before[n_seq];
+    const int total = !few ? a.decode_before[n_seq]
+                      : FORM == kPoolShared && n_seq >= 64 ? __builtin_amdgcn_readlane(of_start, n_seq - 64) : __builtin_amdgcn_readlane(of_before, n_seq);
     const int w = srft_block_by_die();
     const pool_shares shares(total, gridDim.x, W);
     if (total == 0 || w >= shares.groups) return;            // (uniform)
@@ -197,11 +202,15 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
     int unit = shares.begin(w), seq, units_before;
     pool_view view{};
     pool_seq& q = view.q;
-    if (few) {
+    if (FORM == kPoolShared && few) {
+        seq = min((int)(__popcll(__ballot(lane <= n_seq && of_before <= unit)) + __popcll(__ballot(64 + lane <= n_seq && of_start <= unit))) - 1, n_seq - 1);
+        units_before = seq < 64 ? __builtin_amdgcn_readlane(of_before, seq) : __builtin_amdgcn_readlane(of_start, seq - 64);
+        view = pool_view_of<FORM>(a, seq);
+    } else if (few) {
         seq = min((int)__popcll(__ballot(lane <= n_seq && of_before <= unit)) - 1, n_seq - 1);
         units_before = __builtin_amdgcn_readlane(of_before, seq);
         view = {pool_seq_from(a.s, __builtin_amdgcn_readlane(of_start, seq), __builtin_amdgcn_readlane(of_start, seq + 1), __builtin_amdgcn_readlane(of_length, seq)),
-                seq, 0, -1};
+                seq, 0, -1, {}};
     } else {
         seq = __builtin_amdgcn_readfirstlane(pool_sequence_of(a.decode_before, n_seq, unit));
         units_before = a.decode_before[seq];
@@ -649,7 +658,9 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
 #pragma unroll
                 for (int i = 0; i < kPoolOwn<D>; ++i)
                     if (wave + W * i < NB) reinterpret_cast<floatx4*>(part)[(wave + W * i) * 64 + lane] = mine[i];
-                if (wave == 0) {
+                if (FORM == kPoolShared && seq >= a.s.n_seq) {               // (of tokens in common: next to each other)
+                    if (wave == 0 && quarter == 0) reinterpret_cast<floatx4*>(part + 16 * D)[l16] = floatx4{t_all, d_all, __uint_as_float((uint32_t)e_all), 0.0f};
+                } else if (wave == 0) {
                     part[16 * D + lane] = t_all;
                     part[16 * D + 64 + lane] = d_all;
                     part[16 * D + 128 + lane] = __uint_as_float((uint32_t)e_all);
@@ -667,23 +678,22 @@ struct pool_common {
     bool chunk, there;
     pool_shares shares;
     // rows r0 .. r0 + n - 1 of a key head of the sequence q, of this group (uniform)
-    __device__ __forceinline__ pool_common(const pool_attention_args& a, int group, int head, int chunk_keys)
-        : p(pool_view_of<kPoolShared>(a, a.s.n_seq + group).q),
-          chunk(!pool_is_decode<kPoolShared>(a, p, a.s.n_seq + group)),
+    __device__ __forceinline__ pool_common(const pool_attention_args& a, const pool_view& view, int head, int chunk_keys)
+        : p(view.of_group),
+          chunk(!pool_is_decode<kPoolShared>(a, p, a.s.n_seq)),
           shares(chunk ? a.chunk_before[a.s.n_seq + a.n_groups] : a.decode_before[a.s.n_seq + a.n_groups], chunk ? a.chunk_grid : a.decode_grid,
                  chunk ? kPoolChunkLeast<kPoolShared> : kPoolTeam) {
         rows = chunk ? kPoolBlock * kPoolChunkWaves : a.decode_block;
         const int tiles = pool_tiles(p.length, p.full, chunk ? chunk_keys : a.decode_keys);
         cost = chunk ? pool_chunk_cost<kPoolShared>(tiles) : pool_decode_cost<kPoolShared>(tiles);
         blocks = (p.n_new * a.group + rows - 1) / rows;
-        units_before = (chunk ? a.chunk_before : a.decode_before)[a.s.n_seq + group] + head * blocks * cost;
+        units_before = (chunk ? a.chunk_before : a.decode_before)[a.s.n_seq + view.group] + head * blocks * cost;
         there = shares.units > 0;
     }
     __device__ __forceinline__ int start() const { return chunk ? kPoolChunkStart<kPoolShared> : kPoolDecodeStart<kPoolShared>; }
     __device__ __forceinline__ int first(int block) const { return shares.owner(units_before + block * cost + start()); }
     __device__ __forceinline__ int last(int block) const { return shares.owner(units_before + (block + 1) * cost - 1); }
-    // what workgroup w (the first of its block, or not) has left of row r of a block: its sums, and maximum, sum of weights and exponent at
-    // heads[0], [64], [128]
+    // what workgroup w (the first of its block, or not) has left of row r of a block: its sums, and at `heads` maximum, sum of weights and exponent
     template <int D>
     __device__ __forceinline__ const float* part(const pool_attention_args& a, int block, int w, bool is_first, int r) const {
         const int behind = is_first && shares.begin(w) < units_before + block * cost ? 1 : 0, slot = 2 * w + (is_first ? behind : 0);
@@ -692,19 +702,11 @@ struct pool_common {
     }
     template <int D>
     __device__ __forceinline__ const float* heads(const float* part, int r) const {
-        return chunk ? part + 32 * D + r % kPoolBlock : part + 16 * D + r % 16;
+        return chunk ? part + 32 * D + 4 * (r % kPoolBlock) : part + 16 * D + 4 * (r % 16);
     }
-    // channels 16 c + 4 quarter .. + 3 of row r
-    __device__ __forceinline__ floatx4 channels(const float* part, int r, int c, int quarter, int bits) const {
-        const floatx4* const x = reinterpret_cast<const floatx4*>(part);
-        if (!chunk) return x[c * 64 + 16 * quarter + r % 16];
-        const int u = (2 * c + (quarter >> 1)) * 64 + r % kPoolBlock;        // (positions: see pool_block)
-        if (bits == 8) {
-            const floatx4 y = x[u + 32 * (quarter & 1)];
-            return floatx4{y[0], y[2], y[1], y[3]};
-        }
-        const floatx4 y = x[u], z = x[u + 32];
-        return quarter & 1 ? floatx4{y[1], y[3], z[1], z[3]} : floatx4{y[0], y[2], z[0], z[2]};
+    // 4 of the 16 channels of block c of row r: those from 4 quarter on; of pool_chunk by position, unit quarter / 2 of two and half of it quarter % 2
+    __device__ __forceinline__ floatx4 channels(const float* part, int r, int c, int quarter) const {
+        return reinterpret_cast<const floatx4*>(part)[chunk ? (2 * c + (quarter >> 1)) * 64 + 32 * (quarter & 1) + r % kPoolBlock : c * 64 + 16 * quarter + r % 16];
     }
     // positions 4 half .. + 3 of unit u of eight of row r
     __device__ __forceinline__ floatx4 positions(const float* part, int r, int u, int half, int bits) const {
@@ -719,6 +721,14 @@ struct pool_common {
         return half ? floatx4{y[2], z[2], y[3], z[3]} : floatx4{y[0], z[0], y[1], z[1]};
     }
 };
+
+// Four of a unit's positions in the quarters 2 k (the first four) and 2 k + 1 of a wavefront -> its channels 0 .. 3 and 4 .. 7 there (see "Order of
+// channels").
+__device__ __forceinline__ floatx4 pool_by_channel(const floatx4& x, int bits) {
+    if (bits == 8) return floatx4{x[0], x[2], x[1], x[3]};
+    const uint2 a = swap16(__float_as_uint(x[0]), __float_as_uint(x[1])), b = swap16(__float_as_uint(x[2]), __float_as_uint(x[3]));
+    return floatx4{__uint_as_float(a.x), __uint_as_float(b.x), __uint_as_float(a.y), __uint_as_float(b.y)};
+}
 
 // The parts of a key head's rows that went to several workgroups, in the order of the keys; rows of sequences without a tile are zero.  One
 // workgroup of four wavefronts per sequence and key head, each with a quarter of the channels, all parts of them on their way at once
@@ -780,9 +790,8 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
             const long long r_at = (long long)r.token * (a.heads * a.group) + r.head;
             // rows whose tokens (own: 0, in common: 1) one workgroup has had all of; the others as they are
             const auto whole = [&](int which, bool in) __attribute__((always_inline)) {
-                const floatx4 x = reinterpret_cast<const floatx4*>(a.joint_heads[which])[r_at];
-                pool_part_head h[1] = {{x[0], x[1], x[2], 0.0f}};
-                if (!in) h[0] = {kPoolLowest, 0.0f, __uint_as_float((uint32_t)kPoolNoExponent), 0.0f};
+                pool_part_head h[1];
+                h[0].load4(a.joint_heads[which] + 4 * r_at, in);
                 const float before = pool_join(t_all, den, e_all, h, 0, 0);
 #pragma unroll
                 for (int i = 0; i < kPoolOwn<D>; ++i) {
@@ -790,7 +799,7 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
                     o[i] = o[i] * before + (in ? y : floatx4{0, 0, 0, 0}) * h[0].factor;
                 }
             };
-            const pool_common p(a, view.group, head, kPoolChunkKeys<D>);
+            const pool_common p(a, view, head, kPoolChunkKeys<D>);
             // the rows' numbers among those of the group
             const int before_rows = (q.start - p.p.start) * a.group, from = before_rows + (rb * CB + c) * 16, to = min(from + 15, before_rows + rows - 1);
             const int mine = min(from + (lane & 15), to);
@@ -806,15 +815,16 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
                     for (int v = v0; v <= v1; v += AHEAD)
                         join(v, v1,
                              [&](int w, pool_part_head& h) __attribute__((always_inline)) {
-                                 const float* const x = p.template heads<D>(p.template part<D>(a, b, w, w == v0, row), row);
-                                 h = {x[0], x[64], x[128], 0.0f};
-                                 if (!in) h = {kPoolLowest, 0.0f, __uint_as_float((uint32_t)kPoolNoExponent), 0.0f};
+                                 h.load4(p.template heads<D>(p.template part<D>(a, b, w, w == v0, row), row), in);
                              },
                              [&](int w, int n) __attribute__((always_inline)) {
-                                 const floatx4 x = p.channels(p.template part<D>(a, b, w, w == v0, row), row, n, lane >> 4, a.bits);
+                                 const floatx4 x = p.channels(p.template part<D>(a, b, w, w == v0, row), row, n, lane >> 4);
                                  return in ? x : floatx4{0, 0, 0, 0};
                              });
                 }
+            if (p.chunk)                                     // (uniform)
+#pragma unroll
+                for (int i = 0; i < kPoolOwn<D>; ++i) o[i] = pool_by_channel(o[i], a.bits);
             if (w0 == w1) whole(0, true);
         }
         if (!joint || w0 != w1)
