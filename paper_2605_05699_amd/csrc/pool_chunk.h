@@ -35,7 +35,6 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
     constexpr int KROW = 2 * D + 16, VROW = 2 * D + 32;      // bytes of a row in LDS: 16-byte reads of 32 rows, transposed reads of 8, on different banks
     constexpr int UNITS = KEYS * T;                          // of 16 channels, of K and of V each
     constexpr int N = 2 * UNITS <= NT ? 1 : 2;               // a thread's: one of K or of V (then all of the wavefront's), or one place of both
-    static_assert(kPoolSlab<D> * 16 <= 2 * KEYS * KROW, "room for the end");
     static_assert(UNITS % 64 == 0 && UNITS <= NT && (N == 2 || 64 * W % UNITS == 0), "whole wavefronts");
     typedef typename pool_codes<BITS>::type code_t;
     __shared__ __align__(16) unsigned char k_lds[2][KEYS * KROW], v_lds[2][KEYS * VROW];
@@ -68,19 +67,10 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
         const int blocks = (q.n_new * a.group + ROWS - 1) / ROWS;
         const int per_head = __builtin_amdgcn_readfirstlane(pool_chunk_units<FORM>(a, q, ROWS, KEYS, blocks));
         const int rel = unit - a.chunk_before[seq], head = rel / per_head;
-        int t0 = rel - head * per_head, rt = 0, tiles;
-        if constexpr (FORM == kPoolCausal) {                 // the block of rows (those without a tile are passed over)
-            tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, 0);
-            while (t0 >= tiles && rt + 1 < blocks) {
-                t0 -= tiles;
-                tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, ++rt);
-            }
-        } else {
-            t0 = __builtin_amdgcn_readfirstlane(t0);
-            const pool_block_at at = pool_chunk_block_of<FORM>(a, q, ROWS, KEYS, blocks, t0);
-            rt = at.rt;
-            t0 -= at.before;
-            tiles = __builtin_amdgcn_readfirstlane(pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, rt));
+        int t0 = rel - head * per_head, rt = 0, tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, 0);
+        while (t0 >= pool_chunk_cost<FORM>(tiles) && rt + 1 < blocks) {      // the block of rows (those without a tile are passed over)
+            t0 -= pool_chunk_cost<FORM>(tiles);
+            tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, ++rt);
         }
         int t1 = min(pool_chunk_cost<FORM>(tiles), t0 + end - unit);
         if (t1 <= t0) return;                                // (only if the device arrays were written during the call)
@@ -146,7 +136,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
 #pragma unroll
             for (int j = 0; j < kPoolAhead; ++j) f[j] = read_v(j);
             const int last = min(row_last, last_key) - key0;
-            if (FORM == kPoolSliding && (key0 <= wave_last - a.recent || __ballot(last < KEYS - 1) || missing)) {
+            if (FORM == kPoolSliding && key0 <= wave_last - a.recent) {        // (a row's recent tokens begin in the tile: `last` as below)
                 const int limit = last - 4 * half, from = row_first - key0 - 4 * half, sinks = a.sinks - key0 - 4 * half;
 #pragma unroll
                 for (int n = 0; n < KB; ++n)
@@ -155,7 +145,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
                         const int key = 32 * n + 8 * (v / 4) + v % 4;
                         s[n][v] = key <= limit && (key >= from || key < sinks) && !(missing >> (key >> 4) & 1) ? s[n][v] : -__builtin_inff();
                     }
-            } else if (FORM != kPoolSliding && (__ballot(last < KEYS - 1) || missing)) {
+            } else if (__ballot(last < KEYS - 1) || missing) {
                 const int limit = last - 4 * half;           // (compared with constants)
 #pragma unroll
                 for (int n = 0; n < KB; ++n)
@@ -340,10 +330,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
             asm("" : "+v"(again));
             row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + (again & 31));
             char* const to = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
-            if constexpr (FORM == kPoolCausal)               // (long scans: the end counts for little, and registers for more)
-                pool_finish<D>(b, a.out_table, a.out_unscale, to, a.bf16, lane);
-            else
-                pool_finish_together<D, NT>(b, a.out_table, a.out_unscale, to, a.bf16, tid, reinterpret_cast<uint4*>(k_lds), reinterpret_cast<uint4*>(v_lds));
+            pool_finish<D>(b, a.out_table, a.out_unscale, to, a.bf16, lane);
         } else {
             b.put(a.chunk_parts + ((2LL * w + (at_begin ? 0 : 1)) * W + wave) * kPoolPart<D>, lane, FORM == kPoolShared && seq >= a.s.n_seq);
         }
