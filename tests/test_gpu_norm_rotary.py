@@ -59,7 +59,7 @@ def check(got, x, weight, positions, freq, layout, factor):
     assert float(worst) <= 0.0, float(worst)
 
 
-SHAPES = [(128, 128), (96, 64), (64, 32), (256, 256), (80, 20), (6, 2), (128, 0), (2, 2), (34, 34), (1024, 1024), (512, 64), (192, 96)]
+SHAPES = [(258, 130), (128, 128), (96, 64), (64, 32), (256, 256), (80, 20), (6, 2), (128, 0), (2, 2), (34, 34), (1024, 1024), (512, 64), (192, 96)]
 
 
 def inputs(n, d, rot, heads, types, seed, weights=(F32, F16, None)):
