@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
             row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + (again & 31));
             char* const to = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
             pool_finish<D>(b, a.out_table, a.out_unscale, to, a.bf16, lane);
-        } else {
+        } else if (FORM == kPoolCausal || rt * ROWS + wave * kPoolBlock < q.n_new * a.group) {     // (sums of no row: nobody reads them)
             b.put(a.chunk_parts + ((2LL * w + (at_begin ? 0 : 1)) * W + wave) * kPoolPart<D>, lane, FORM == kPoolShared && seq >= a.s.n_seq);
         }
     }

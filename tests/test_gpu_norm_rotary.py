@@ -269,3 +269,20 @@ def test_no_tokens_and_refusals(B):
         with pytest.raises(B.SrftError) as e:
             call()
         assert e.value.status == status
+
+
+def test_native_marshalling_and_ctypes_make_the_same_calls(B):
+    """With a stream named the binding goes through ctypes."""
+    gen, x, w, positions, freq = inputs(33, 96, 64, (4, 2), (BF16, BF16), 21, (F32, None))
+    dy, stream = [torch.randn(t.shape, device="cuda", generator=gen).to(F16) for t in x], torch.cuda.current_stream()
+    space = torch.empty(B.srft_norm_rotary_backward_workspace_bytes(2, 96), dtype=torch.uint8, device="cuda")
+    results = []
+    for s in (None, stream):
+        y, dx, dw = [torch.full_like(t, float("nan")) for t in x], [torch.full_like(t, float("nan")) for t in x], [torch.full((96,), float("nan"), device="cuda") for _ in x]
+        B.srft_norm_rotary(list(zip(x, w, y)), positions, freq, EPS, layout="pairs", factor=1.5, stream=s)
+        B.srft_norm_rotary_backward(list(zip(dy, x, w, dx, [dw[0], None])), positions, freq, EPS, space, layout="pairs", factor=1.5, stream=s)
+        torch.cuda.synchronize()
+        results.append([*y, *dx, dw[0]])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    for a, b, c in zip(x, w, results[0][:2]):
+        check(c, a, b, positions, freq, "pairs", 1.5)
