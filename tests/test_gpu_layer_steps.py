@@ -125,3 +125,62 @@ def test_chunks_and_decode_steps_in_turn(B):
         steps.calls()
         steps.check()
     s.close()
+
+
+def test_calls_on_two_streams_at_once(B):
+    """Sliding and shared attention of decode steps and chunks over one pool, a workspace to each stream."""
+    s = conversations(B, 128, 32, 4, 16, 2, 6, 1000, seed=3)
+    new = [1, 90, 1, 40, 2, 1]
+    s.append(new)
+    gen = torch.Generator("cuda")
+    gen.manual_seed(9)
+    q = torch.randn(sum(new), 8, 128, device="cuda", generator=gen).half()
+    seqs, to = s.seqs(new), lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")      # noqa: E731
+    prefixes = B.SharedPrefixes(to([0, 6]), to([992]))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    sizes = [B.srft_pool_attention_sliding_workspace_bytes(s.pool, seqs, *q.shape[:2]), B.srft_pool_attention_shared_workspace_bytes(s.pool, seqs, prefixes, *q.shape[:2])]
+    space = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+    out = [[torch.full_like(q, float("nan")) for _ in range(8)] for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(8):
+        B.srft_pool_attention_sliding(s.pool, seqs, q, 0.1, 300, 4, out[0][i], space[0], streams[0])
+        B.srft_pool_attention_shared(s.pool, seqs, prefixes, q, 0.1, out[1][i], space[1], streams[1])
+    torch.cuda.synchronize()
+    for got, hidden in zip(out, (hidden_of(300, 4), None)):
+        assert all(torch.equal(t, got[0]) for t in got)
+        want, err = s.attention(q.double().cpu().numpy(), new, 0.1, 4, HALF_STEP[torch.float16], hidden=hidden)
+        off = np.abs(got[0].double().cpu().numpy() - want) - err
+        assert np.isfinite(off).all() and off.max() <= 0.0, float(off.max())
+    s.close()
+
+
+@pytest.mark.parametrize("new,group", [([1, 1, 1], 4), ([70, 1, 100], 4)])
+def test_pages_past_four_gibibytes(B, new, group):
+    """Page numbers whose records begin past 2^32 bytes of codes (8 KB a page), the two kinds of pages in turn."""
+    pages = 530_000
+    s = Serving(B, 128, 32, 4, 16, 8, n=3, max_length=600, seed=4, spare=pages)
+    high = sorted(p for p in s.free if p * 8192 >= 1 << 32)
+    assert len(high) > 120
+    s.free = [p for pair in zip(range(120), high) for p in pair]
+    s.append([400, 0, 0])
+    for b in (1, 2):
+        s.table[b, :25] = s.table[0, :25]
+        s.length[b] = 400
+        for i in range(2):
+            s.tokens[i][b] = s.tokens[i][0].copy()
+    s.append([a + 20 for a in new])
+    assert int(s.table[0, :25].max()) * 8192 >= 1 << 32
+    q = torch.from_numpy(s.rng.standard_normal((sum(new), 8 * group, 128))).half().cuda()
+    seqs, to = s.seqs(new), lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")      # noqa: E731
+    prefixes = B.SharedPrefixes(to([0, 3]), to([400]))
+    space = torch.empty(max(B.srft_pool_attention_sliding_workspace_bytes(s.pool, seqs, *q.shape[:2]),
+                            B.srft_pool_attention_shared_workspace_bytes(s.pool, seqs, prefixes, *q.shape[:2])), dtype=torch.uint8, device="cuda")
+    sliding, shared = torch.full_like(q, float("nan")), torch.full_like(q, float("nan"))
+    B.srft_pool_attention_sliding(s.pool, seqs, q, 0.1, 150, 20, sliding, space)
+    B.srft_pool_attention_shared(s.pool, seqs, prefixes, q, 0.1, shared, space)
+    torch.cuda.synchronize()
+    for out, hidden in ((sliding, hidden_of(150, 20)), (shared, None)):
+        want, err = s.attention(q.double().cpu().numpy(), new, 0.1, group, HALF_STEP[torch.float16], hidden=hidden)
+        off = np.abs(out.double().cpu().numpy() - want) - err
+        assert np.isfinite(off).all() and off.max() <= 0.0, float(off.max())
+    s.close()

@@ -286,3 +286,35 @@ def test_native_marshalling_and_ctypes_make_the_same_calls(B):
     assert all(torch.equal(a, b) for a, b in zip(*results))
     for a, b, c in zip(x, w, results[0][:2]):
         check(c, a, b, positions, freq, "pairs", 1.5)
+
+
+def test_captured_gradients_of_a_step_after_another(B):
+    """Forward and backward in one graph, replayed with other rows and positions, an eager backward with a workspace of its own between the replays."""
+    n, d, heads = 300, 128, (6, 2)
+    gen, x, w, positions, freq = inputs(n, d, 128, heads, (BF16, F32), 21, (F32, F32))
+    dy = [torch.randn(t.shape, device="cuda", generator=gen) for t in x]
+    y, dx, dw = [torch.empty_like(t) for t in dy], [torch.empty_like(t) for t in x], [torch.empty(d, device="cuda") for _ in x]
+    space = torch.empty(B.srft_norm_rotary_backward_workspace_bytes(2, d), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        B.srft_norm_rotary(zip(x, w, y), positions, freq, EPS, layout="pairs")
+        B.srft_norm_rotary_backward(zip(dy, x, w, dx, dw), positions, freq, EPS, space, layout="pairs")
+    calls()                                                  # (first launches load the kernels)
+    torch.cuda.synchronize()
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        calls()
+    for step in range(5):
+        for t in (*x, *dy):
+            t.copy_(torch.randn(t.shape, device="cuda", generator=gen))
+        positions.add_(1000 * step + 1)
+        for t in (*y, *dx, *dw):
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        eager = backward(B, dy, x, w, positions, freq, "pairs", 1.0)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(dx[i], eager[0][i]) and torch.equal(dw[i], eager[1][i]), (step, i)
+            check(y[i], x[i], w[i], positions, freq, "pairs", 1.0)
+            check_gradients(dx[i], dw[i], dy[i], x[i], w[i], positions, freq, "pairs", 1.0)
