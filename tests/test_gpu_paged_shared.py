@@ -16,13 +16,13 @@ def B():
     return binding
 
 
-def fork(s, groups, pages):
+def fork(s, groups, pages, gain=1.0):
     """The first pages[g] pages of the sequences groups[g] .. groups[g + 1] are those of the first of them."""
     first = np.zeros(s.n, int)
     for g, p in enumerate(pages):
         if groups[g] < groups[g + 1]:
             first[groups[g]] = p * s.R
-    s.append(list(first))
+    s.append(list(first), gain)
     for g, p in enumerate(pages):
         for b in range(groups[g] + 1, groups[g + 1]):
             s.table[b, :p] = s.table[groups[g], :p]
@@ -229,6 +229,31 @@ def test_strides_streams_and_repeats(B):
     check(s, out[:, :8, :64], q, new, -0.13, group)
     assert bool((out[:, 8] == 7.0).all()) and bool((out[..., 64:] == 7.0).all())
     assert torch.equal(share(s, q, new, -0.13, prefixes, fill=0), out[:, :8, :64])
+    s.close()
+
+
+@pytest.mark.parametrize("gains", [(1000.0, 1e-3), (1e-3, 300.0), (1e-4, 1e-4)])
+@pytest.mark.parametrize("q_gain,dtype", [(1.0, torch.float16), (1e5, torch.bfloat16), (1e-8, torch.bfloat16)])
+@pytest.mark.parametrize("new", [[1, 1, 3], [1, 70, 20]])
+def test_magnitudes_of_what_is_common_and_of_what_is_not(B, gains, q_gain, dtype, new):
+    s = fork(Serving(B, 128, 32, 4, 16, 2, n=3, max_length=500, seed=17, lam_spread=1.5), [0, 3], [12], gains[0])
+    s.append([a + b for a, b in zip(new, (7, 100, 44))], gains[1])
+    q = q_gain * queries(s, new, 4, torch.float32)
+    q = q.to(dtype)
+    scale = 0.09 / (max(gains) * q_gain)
+    out = share(s, q, new, scale, prefixes_of(B, [0, 3], [192]))
+    check(s, out, q, new, scale, 4)
+    s.close()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.1, 3.0, 1e-30])
+def test_softmax_scales(B, scale):
+    s = fork(Serving(B, 64, 32, 8, 16, 2, n=4, max_length=500, seed=18), [0, 2, 4], [12, 9])
+    new = [1, 60, 2, 1]
+    s.append([a + b for a, b in zip(new, (7, 100, 44, 1))])
+    q = queries(s, new, 2, torch.float16)
+    out = share(s, q, new, scale, prefixes_of(B, [0, 2, 4], [192, 144]))
+    check(s, out, q, new, scale, 2)
     s.close()
 
 

@@ -192,6 +192,33 @@ def test_strides_streams_and_repeats(B):
     s.close()
 
 
+@pytest.mark.parametrize("gains", [(1000.0, 1e-3, 1.0), (1e-3, 300.0, 0.1), (1e-4, 1e-4, 1e-4)])
+@pytest.mark.parametrize("q_gain,dtype", [(1.0, torch.float16), (1e5, torch.bfloat16), (1e-8, torch.bfloat16)])
+@pytest.mark.parametrize("new", [[1, 3], [1, 70]])
+def test_magnitudes_of_first_and_last_tokens(B, gains, q_gain, dtype, new):
+    """What lies between them is of another size, and seen by no row."""
+    s = Serving(B, 128, 32, 4, 16, 2, n=2, max_length=500, seed=17, lam_spread=1.5)
+    for gain, tokens in zip(gains, ([16, 16], [160, 240], [80, 150])):
+        s.append(tokens, gain)
+    s.append(new, gains[2])
+    q = (q_gain * queries(s, new, 4, torch.float32)).to(dtype)
+    scale = 0.09 / (max(gains[0], gains[2]) * q_gain)
+    out = slide(s, q, new, scale, 70, 16)
+    check(s, out, q, new, scale, 4, 70, 16)
+    s.close()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.1, 3.0, 1e-30])
+def test_softmax_scales(B, scale):
+    s = Serving(B, 64, 32, 8, 16, 2, n=2, max_length=300, seed=18)
+    s.append([100, 200])
+    new = [1, 60]
+    s.append(new)
+    q = queries(s, new, 2, torch.float16)
+    check(s, slide(s, q, new, scale, 33, 20), q, new, scale, 2, 33, 20)
+    s.close()
+
+
 def test_refusals(B):
     s = Serving(B, 64, 32, 4, 16, 2, n=2, max_length=64, seed=8)
     s.append([20, 30])
