@@ -5,7 +5,8 @@
 // prompt of 4096 tokens, 64 query heads, were a million workgroups, nearly all of them empty: 1376 us, now 36), each with every fourth
 // run of 32 positions of the sums and then of the outputs (one wavefront per 32 rows read every part, and the matrix, one after
 // the other: 104 us at d = 256, 28 at d = 128).  Bound by the chain of loads where parts are few (a first round for the maxima alone: 6.9 us,
-// now 5.5, for a step of 4 sequences), by the parts' bytes where they are many (23 us for 67 MB at d = 128; more of them in flight is slower).  Rows that their scan has finished have nothing to do here.
+// now 5.5, for a step of 4 sequences), by the parts' bytes where they are many (23 us for 67 MB at d = 128; more of them in flight is slower).  Shared forms: the parts
+// of the tokens in common first, read by row; 64 conversations' 512 rows 16 us (28 with channels gathered one by one).  Rows that their scan has finished have nothing to do here.
 #include "../pool_decode.h"
 
 namespace {

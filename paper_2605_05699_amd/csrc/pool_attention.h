@@ -157,7 +157,9 @@ __device__ __forceinline__ int pool_chunk_tiles(const pool_attention_args& a, co
 }
 // What a block of rows counts for when the work is shared out: its tiles, and the time that its start and its end take, in tiles, so that a
 // workgroup with many short segments has fewer tiles (chunks of 8 sequences, 40 to 300 tokens, behind 12,000 in common: the workgroups with the
-// own tokens' segments had 30 of them, 560 us).  The causal form counts tiles alone.
+// own tokens' segments had 30 of them, 560 us; now 275, with 3 and 10 for a start of pool_chunk 300 and 284, with 2 and 8 for one of pool_decode a batch
+// of 8 groups 76 and 60 where 4 takes 59).  Shares of pool_chunk are at least kPoolChunkLeast, a start and two tiles: with 16, 500 tokens and less of 8 sequences
+// of up to 4096 at d = 256, 1000 of them seen, take 128 instead of 110 us.  The causal form counts tiles alone.
 template <int FORM> constexpr int kPoolChunkStart = FORM == kPoolCausal ? 0 : 6;
 template <int FORM> constexpr int kPoolDecodeStart = FORM == kPoolCausal ? 0 : 4;
 template <int FORM> constexpr int kPoolChunkLeast = FORM == kPoolCausal ? 1 : 8;             // of units, a workgroup's of pool_chunk

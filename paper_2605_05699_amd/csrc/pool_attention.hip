@@ -30,7 +30,9 @@ constexpr int kChunkRows = kPoolBlock * kPoolChunkWaves;
 // Sequences that bring few rows a key head go to pool_decode, cb blocks of 16 of them a workgroup, the others to pool_chunk.  Two blocks where
 // a sequence may bring 17 to 32 rows and none brings more, up to d = 128 (beyond it two blocks' sums do not fit the registers: there a
 // workgroup takes one block, and the keys are read twice); else one, and 17 rows are a chunk.
-constexpr int kCommonRows = 48;                               // (up to three blocks of pool_decode)
+// A group's tokens in common go to pool_decode up to kCommonRows rows, in up to three blocks that each read the keys.  With up to 16 six samples of 800
+// tokens take 40 us (now 22) and five prompts with 2 to 11 samples at d = 256 96 (now 67); with up to 96 these stay as they are.
+constexpr int kCommonRows = 48;
 struct split {
     int cb, rows;
     bool chunk, decode;
