@@ -30,11 +30,13 @@ constexpr int kChunkRows = kPoolBlock * kPoolChunkWaves;
 // Sequences that bring few rows a key head go to pool_decode, cb blocks of 16 of them a workgroup, the others to pool_chunk.  Two blocks where
 // a sequence may bring 17 to 32 rows and none brings more, up to d = 128 (beyond it two blocks' sums do not fit the registers: there a
 // workgroup takes one block, and the keys are read twice); else one, and 17 rows are a chunk.
-// A group's tokens in common go to pool_decode up to kCommonRows rows, in up to three blocks that each read the keys.  With up to 16 six samples of 800
-// tokens take 40 us (now 22) and five prompts with 2 to 11 samples at d = 256 96 (now 67); with up to 96 these stay as they are.
-constexpr int kCommonRows = 48;
+// A group's tokens in common go to pool_decode, in blocks that each read the keys, up to kCommonRows rows; and in calls of up to kFewRows rows, which
+// need no launch for chunks then.  With up to 16 in place of kCommonRows six samples of 800 tokens take 40 us (now 22) and five prompts with 2 to 11 samples at d = 256
+// 96 (now 67); with up to 96 six groups of 96 rows behind 4000 tokens take 85 (now 78; d = 256 134, now 115), one alone 27 (as now; as a chunk 45) and behind 16,384 tokens
+// 49 (56).  128 rows in one group: 30 us behind 2000 tokens (as a chunk 46), 58 (58) behind 16,384, at d = 256 52 (73) and 107 (100); 192: 31 (51), 72 (64), 54 (79), 133 (106).
+constexpr int kCommonRows = 48, kFewRows = 128;
 struct split {
-    int cb, rows;
+    int cb, rows, common_rows;
     bool chunk, decode;
 };
 split split_of(const srft_paged_seqs* s, const form_of_call& f, int64_t n_new, int group, int d) {
@@ -42,7 +44,8 @@ split split_of(const srft_paged_seqs* s, const form_of_call& f, int64_t n_new, i
     const bool few = most > 16 && most <= kPoolDecodeRows;
     const int rows = few ? kPoolDecodeRows : 16;
     // (a group's tokens in common have the rows of all its sequences)
-    return {few && d <= 128 ? 2 : 1, rows, most > rows || (f.groups() > 0 && n_new * group > kCommonRows), most <= rows || s->n_seq > 1 || n_new * group <= rows};
+    const int common = n_new * group <= kFewRows ? kFewRows : kCommonRows;
+    return {few && d <= 128 ? 2 : 1, rows, common, most > rows || (f.groups() > 0 && n_new * group > common), most <= rows || s->n_seq > 1 || n_new * group <= rows};
 }
 workspace layout(const srft_pool* p, const srft_paged_seqs* s, const form_of_call& f, int64_t n_new, int q_heads) {
     const int d = p->plan_k->d, group = q_heads / p->heads, items = s->n_seq + f.groups();
@@ -101,7 +104,7 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, const form_of_call
     const int d = pool->plan_k->d, group = q_heads / pool->heads;
     const int64_t most = kPoolMostUnits, tiles = seqs->max_length / 32 + 2 + (f.form == kPoolCausal ? 0 : kPoolChunkStart<kPoolSliding>), heads = (int64_t)seqs->n_seq * pool->heads;
     const int64_t items = seqs->n_seq + f.groups(), blocks = (f.groups() > 0 ? 2 : 1) * n_new * group / kChunkRows + items;
-    if ((f.groups() > 0 ? 3 : 2) * items * pool->heads * tiles >= most || blocks * pool->heads * std::max<int64_t>(tiles, kPoolChunkWaves) >= most ||
+    if ((f.groups() > 0 ? 3 * items + kFewRows / 16 : 2 * items) * pool->heads * tiles >= most || blocks * pool->heads * std::max<int64_t>(tiles, kPoolChunkWaves) >= most ||
         (heads * pool->R / kTileVecs * 2 + pool->plan_k->compute_units * 3 + 1) * 2 * d > UINT32_MAX)        // (threads of pool_rotate)
         return SRFT_ERR_BAD_N;
     return SRFT_OK;
@@ -185,7 +188,7 @@ int attend(const srft_pool* pool, const srft_paged_seqs* seqs, form_of_call f, c
         a.groups = f.prefixes->groups_dev;
         a.shared = f.prefixes->tokens_dev;
         a.n_groups = f.groups();
-        a.common_rows = kCommonRows;
+        a.common_rows = sp.common_rows;
         a.bounds = (int*)(base + w.bounds);
         a.items = (pool_item*)(base + w.items);
         for (int i = 0; i < 2; ++i) {

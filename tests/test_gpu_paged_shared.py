@@ -60,8 +60,9 @@ FORMATS = [(128, 32, 4, 16, 2, "dft", torch.float16), (64, 32, 4, 32, 1, "dft", 
            (192, 64, 4, 16, 2, "dft", torch.float16), (32, 32, 8, 32, 2, "dft", torch.float16), (128, 32, 4, 16, 2, "hadamard", torch.float16),
            (160, 32, 8, 256, 1, "dft", torch.bfloat16), (224, 16, 4, 16, 2, "dft", torch.float16)]
 #: new tokens of nine sequences in the groups 0 .. 2, 2 .. 3, 3 .. 3, 3 .. 8 (the last one in none): decode steps, steps of a few tokens, one of whose
-#: sequences has none, chunks and both; rows of a chunk in a group that has few of them
-STEPS = [((5, 1, 3, 60, 1, 0, 1, 1, 2), 4), ((1,) * 9, 4), ((1,) * 9, 1), ((2, 1, 4, 0, 3, 1, 5, 1, 1), 3), ((3,) * 9, 8), ((40, 1, 2, 70, 1, 0, 150, 1, 20), 3), ((1,) * 9, 24)]
+#: sequences has none, chunks and both; rows of a chunk in a group that has few of them; groups of many rows in calls of few
+STEPS = [((5, 1, 3, 60, 1, 0, 1, 1, 2), 4), ((1,) * 9, 4), ((1,) * 9, 1), ((2, 1, 4, 0, 3, 1, 5, 1, 1), 3), ((3,) * 9, 8), ((40, 1, 2, 70, 1, 0, 150, 1, 20), 3), ((1,) * 9, 24),
+         ((1,) * 9, 14), ((1, 1, 1, 1, 1, 0, 1, 0, 1), 18)]
 GROUPS = [0, 2, 3, 3, 8]
 
 
