@@ -203,6 +203,28 @@ __device__ __forceinline__ int pool_chunk_units(const pool_attention_args& a, co
     for (int rt = threadIdx.x & 63; rt < n; rt += 64) sum += pool_chunk_cost<FORM>(pool_chunk_tiles<FORM>(a, q, rows, keys, rt));
     return pool_wave_sum(sum);
 }
+// The block of rows, of n, that unit u of one key head belongs to, and the units in front of it there (by the whole wavefront, a block a lane).
+struct pool_block_at { int rt, before; };
+template <int FORM>
+__device__ __forceinline__ pool_block_at pool_chunk_block_of(const pool_attention_args& a, const pool_seq& q, int rows, int keys, int n, int u) {
+    const int lane = (int)threadIdx.x & 63;
+    int before = 0;
+    for (int rt = 0;; rt += 64) {
+        const int units = rt + lane < n ? pool_chunk_cost<FORM>(pool_chunk_tiles<FORM>(a, q, rows, keys, rt + lane)) : 0;
+        int sum = units;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int other = __shfl_up(sum, d);
+            if (lane >= d) sum += other;
+        }
+        const int below = (int)__popcll(__ballot(before + sum <= u));        // (ascending: the first ones)
+        if (below < 64 || rt + 64 >= n) {
+            const int i = max(min(below, min(n - rt, 64) - 1), 0);
+            return {rt + i, before + __builtin_amdgcn_readlane(sum - units, i)};
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+}
 // The workgroups that take part, and where the share of workgroup w begins: the first `more` have a unit more than the others.
 struct pool_shares {
     int units, groups, each, more;

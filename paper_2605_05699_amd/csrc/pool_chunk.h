@@ -28,6 +28,21 @@
 constexpr int kPoolAhead = 2;                                    // reads of LDS ahead of the matrix instructions (739 us without); 4 and 6 measure the same up to d = 128 and spill above
 constexpr int kPoolRoom = 2;                                     // powers of two that scales may grow before the exponent changes
 
+// How a workgroup goes through its blocks of rows (see there), and what is the same in all lanes then in scalar registers.  Not so in the causal form above 192
+// dimensions: in the registers that are left there its loop takes 6 % longer for it (8192 new tokens behind 8192, 2 query heads to each of 4: 947 -> 1010 us).
+template <int D, int FORM> constexpr bool kPoolWalk = FORM != kPoolCausal || D <= 192;
+template <bool WALK> __device__ __forceinline__ int pool_same(int x) { return WALK ? __builtin_amdgcn_readfirstlane(x) : x; }
+template <bool WALK> __device__ __forceinline__ pool_view pool_same(pool_view v) {
+    v.q.start = pool_same<WALK>(v.q.start), v.q.n_new = pool_same<WALK>(v.q.n_new), v.q.length = pool_same<WALK>(v.q.length);
+    v.q.before = pool_same<WALK>(v.q.before), v.q.full = pool_same<WALK>(v.q.full);
+    v.seq = pool_same<WALK>(v.seq), v.first_page = pool_same<WALK>(v.first_page), v.group = pool_same<WALK>(v.group);
+    return v;
+}
+template <bool WALK, int FORM> __device__ __forceinline__ pool_gap<FORM> pool_same(pool_gap<FORM> g) {
+    g.begin = pool_same<WALK>(g.begin), g.skip = pool_same<WALK>(g.skip), g.low = pool_same<WALK>(g.low), g.sinks = pool_same<WALK>(g.sinks);
+    return g;
+}
+
 template <int D, int BITS, int FORM>
 __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kernel(const pool_attention_args a) {
     constexpr int W = kPoolChunkWaves, NT = 64 * W, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * W, KB = KEYS / 32;
@@ -46,9 +61,9 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
     const int w = srft_block_by_die();
     const pool_shares shares(total, gridDim.x, kPoolChunkLeast<FORM>);
     if (total == 0 || w >= shares.groups) return;            // (uniform)
-    const int end = shares.begin(w + 1);
-    int unit = shares.begin(w);
-    int seq = __builtin_amdgcn_readfirstlane(pool_sequence_of(a.chunk_before, n_seq, unit));
+    constexpr bool WALK = kPoolWalk<D, FORM>;
+    const int end = pool_same<WALK>(shares.begin(w + 1));
+    int unit = pool_same<WALK>(shares.begin(w));
     const int R = 1 << a.s.log_R, n_scales = D / a.g;
 
     // a thread's units: which key of the tile, which 16 channels (wavefronts beyond the last unit take units that others have too)
@@ -60,18 +75,60 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
     const uint32_t off_code = (u_key & 15) * CB + u_at * (int)sizeof(code_t), off_scale = 4 * ((u_key & 15) * n_scales + 16 * u_at / a.g);
     unsigned char *const k_dst = k_lds[0] + u_key * KROW + 32 * u_at, *const v_dst = v_lds[0] + u_key * VROW + 32 * u_at;    // in the first buffer
 
-    for (bool at_begin = true; unit < end; at_begin = false) {
-        while (seq + 1 < n_seq && a.chunk_before[seq + 1] <= unit) ++seq;
-        const pool_view view = pool_view_of<FORM>(a, seq);
-        const pool_seq& q = view.q;
-        const int blocks = (q.n_new * a.group + ROWS - 1) / ROWS;
-        const int per_head = __builtin_amdgcn_readfirstlane(pool_chunk_units<FORM>(a, q, ROWS, KEYS, blocks));
-        const int rel = unit - a.chunk_before[seq], head = rel / per_head;
-        int t0 = rel - head * per_head, rt = 0, tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, 0);
-        while (t0 >= pool_chunk_cost<FORM>(tiles) && rt + 1 < blocks) {      // the block of rows (those without a tile are passed over)
-            t0 -= pool_chunk_cost<FORM>(tiles);
-            tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, ++rt);
+    // The block of rows that a share begins in is found by a lane each, and the next ones in their order.  (Found by counting from a key head's first one
+    // every time, 8192 new tokens that see 64, 8 query heads to each of 4 of 64 channels, took 388 us, now 118; that see 1024, 4 to each of 8 of 128, 394, now 291.)
+    int seq = pool_sequence_of(a.chunk_before, n_seq, unit), head = 0, rt = 0, t0 = 0, blocks = 0, tiles = 0;
+    pool_view view;
+    const auto take = [&]() __attribute__((always_inline)) {
+        view = pool_same<WALK>(pool_view_of<FORM>(a, seq));
+        blocks = pool_same<WALK>((view.q.n_new * a.group + ROWS - 1) / ROWS);
+    };
+    const auto tiles_of = [&](int rt) __attribute__((always_inline)) { return pool_same<WALK>(pool_chunk_tiles<FORM>(a, view.q, ROWS, KEYS, rt)); };
+    const auto locate = [&]() __attribute__((always_inline)) {
+        take();
+        const int per_head = __builtin_amdgcn_readfirstlane(pool_chunk_units<FORM>(a, view.q, ROWS, KEYS, blocks));
+        const int rel = pool_same<WALK>(unit - a.chunk_before[seq]);
+        head = pool_same<WALK>(rel / per_head);
+        t0 = rel - head * per_head;
+        rt = 0;
+        if constexpr (WALK) {
+            const pool_block_at at = pool_chunk_block_of<FORM>(a, view.q, ROWS, KEYS, blocks, t0);
+            rt = at.rt;
+            t0 -= at.before;
+            tiles = tiles_of(rt);
+        } else {
+            tiles = tiles_of(0);
+            while (t0 >= pool_chunk_cost<FORM>(tiles) && rt + 1 < blocks) {
+                t0 -= pool_chunk_cost<FORM>(tiles);
+                tiles = tiles_of(++rt);
+            }
         }
+    };
+    const auto next = [&]() __attribute__((always_inline)) {                 // whether there is another (those without a tile are passed over)
+        t0 = 0;
+        do {
+            if (++rt < blocks) continue;
+            rt = 0;
+            if (++head == a.heads) {
+                head = 0;
+                do
+                    if (++seq >= n_seq) return false;
+                while (pool_same<WALK>(a.chunk_before[seq + 1]) <= unit);
+                take();
+            }
+        } while ((tiles = tiles_of(rt)) == 0);
+        return true;
+    };
+    if constexpr (WALK) locate();
+    for (bool at_begin = true;; at_begin = false) {
+        if (!at_begin && unit >= end) return;
+        if constexpr (WALK) {
+            if (!at_begin && !next()) return;
+        } else {
+            while (seq + 1 < n_seq && a.chunk_before[seq + 1] <= unit) ++seq;
+            locate();
+        }
+        const pool_seq& q = view.q;
         int t1 = min(pool_chunk_cost<FORM>(tiles), t0 + end - unit);
         if (t1 <= t0) return;                                // (only if the device arrays were written during the call)
         unit += t1 - t0;
@@ -80,8 +137,8 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
             t1 -= kPoolChunkStart<FORM>;
             if (t1 <= t0) continue;
         }
-        const int seen = pool_chunk_seen<FORM>(a, q, ROWS, rt), all_page_tiles = (max(min(seen, q.full), 0) + KEYS - 1) / KEYS, tail = q.length - q.full;
-        const pool_gap<FORM> gap = pool_chunk_gap<FORM>(a, q, ROWS, KEYS, rt);
+        const int seen = pool_same<WALK>(pool_chunk_seen<FORM>(a, q, ROWS, rt)), all_page_tiles = (max(min(seen, q.full), 0) + KEYS - 1) / KEYS, tail = q.length - q.full;
+        const pool_gap<FORM> gap = pool_same<WALK>(pool_chunk_gap<FORM>(a, q, ROWS, KEYS, rt));
         const int page_tiles = all_page_tiles - gap.in_pages(all_page_tiles);
         pool_row row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + l32);
         const long long q_row = (long long)row.token * (a.heads * a.group) + row.head;
