@@ -24,30 +24,47 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     // ops: [k-step][hi, lo][lane]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int of = (int)(workgroup / BLOCKS), block = (int)workgroup - of * BLOCKS, at = of / a.heads, head = of - at * a.heads;
+    const int* const before = a.chunk_before;
+    const int units = before[pool_count<FORM>(a)];           // (in one round of loads)
     if (at >= a.blocks_before[a.s.n_seq]) return;
     const int seq = a.s.n_seq == 1 ? 0 : __builtin_amdgcn_readfirstlane(pool_sequence_of(a.blocks_before, a.s.n_seq, at)), rt = at - a.blocks_before[seq];
     const pool_view view = pool_view_of<FORM>(a, seq);
     const pool_seq& q = view.q;
+    const int units_before = before[seq];
     const int r0 = rt * ROWS + block * kPoolBlock;
     if (r0 >= q.n_new * a.group) return;
     const int tiles = pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, rt);
-    const pool_row row = pool_row_of(q, head, a.group, r0 + (lane & 31));
-    char* const dst = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
+    const auto row_here = [&]() __attribute__((always_inline)) { return pool_row_of(q, head, a.group, r0 + (lane & 31)); };
+    const auto to = [&](const pool_row& r) __attribute__((always_inline)) { return r.there ? a.out + r.token * a.out_token + r.head * a.out_head : nullptr; };
     if (tiles == 0) {
-        if (dst)
+        if (char* const dst = to(row_here()))
             for (int i = 2 * wave + half; i < D / 8; i += 2 * kPoolTeam) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0, 0, 0, 0);
         return;
     }
-    const int* const before = a.chunk_before;
-    const int units = before[pool_count<FORM>(a)];
     if (units == 0) return;                                  // (too many of them: see kPoolMostUnits)
-    const int first = before[seq] + head * pool_chunk_units<FORM>(a, q, ROWS, KEYS, (q.n_new * a.group + ROWS - 1) / ROWS) +
-                      pool_chunk_units<FORM>(a, q, ROWS, KEYS, rt);
+    // Units of a key head's blocks of rows, and of those in front of this one: by one wavefront.  (By all four, each for itself, 8192 workgroups with nothing to merge
+    // were 23 us, the vector ALU's time.)
+    __shared__ int2 units_of;
+    if (wave == 0) {
+        int all = 0, in_front = 0;
+        for (int i = lane; i * ROWS < q.n_new * a.group; i += 64) {
+            const int cost = pool_chunk_cost<FORM>(pool_chunk_tiles<FORM>(a, q, ROWS, KEYS, i));
+            all += cost;
+            in_front += i < rt ? cost : 0;
+        }
+        all = pool_wave_sum(all);
+        in_front = pool_wave_sum(in_front);
+        if (lane == 0) units_of = make_int2(all, in_front);
+    }
+    __syncthreads();
+    const int first = units_before + head * units_of.x + units_of.y;
     const pool_shares shares(units, a.chunk_grid, kPoolChunkLeast<FORM>);
     const int w0 = shares.owner(first + kPoolChunkStart<FORM>), w1 = shares.owner(first + pool_chunk_cost<FORM>(tiles) - 1);
     const bool joint = FORM == kPoolShared && view.group >= 0;
     if (w0 == w1 && !joint) return;
     const int behind = shares.begin(w0) < first ? 1 : 0;    // the first part's workgroup began with other rows
+    const pool_row row = row_here();
+    char* const dst = to(row);
     const auto part = [&](int w) __attribute__((always_inline)) {
         return a.chunk_parts + ((2LL * w + (w == w0 ? behind : 0)) * BLOCKS + block) * kPoolPart<D>;
     };
@@ -174,8 +191,9 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
     }
 }
 
+// (four wavefronts a SIMD, as the registers allow but at 256 dimensions by themselves)
 template <int D, int CB, int FORM>
-__global__ void __launch_bounds__(64 * kPoolTeam) srft_pool_merge_kernel(const pool_attention_args a) {
+__global__ void __launch_bounds__(64 * kPoolTeam, FORM == kPoolShared ? 1 : 4) srft_pool_merge_kernel(const pool_attention_args a) {
     constexpr int OPS = D / 16 * 2 * 64;
     __shared__ __align__(16) unsigned char lds[std::max(kPoolFinishBytes<D>, OPS * 16 + kPoolTeam * 32 * 4)];
     const unsigned workgroup = blockIdx.y * gridDim.x + blockIdx.x;          // (what follows is uniform)
