@@ -157,12 +157,13 @@ __device__ __forceinline__ int pool_chunk_tiles(const pool_attention_args& a, co
 }
 // What a block of rows counts for when the work is shared out: its tiles, and the time that its start and its end take, in tiles, so that a
 // workgroup with many short segments has fewer tiles (chunks of 8 sequences, 40 to 300 tokens, behind 12,000 in common: the workgroups with the
-// own tokens' segments had 30 of them, 560 us; now 275, with 3 and 10 for a start of pool_chunk 300 and 284, with 2 and 8 for one of pool_decode a batch
-// of 8 groups 76 and 60 where 4 takes 59).  Shares of pool_chunk are at least kPoolChunkLeast, a start and two tiles: with 16, 500 tokens and less of 8 sequences
-// of up to 4096 at d = 256, 1000 of them seen, take 128 instead of 110 us.  The causal form counts tiles alone.
+// own tokens' segments had 30 of them, 560 us; now 275, and with 4 or 8 for a start of pool_chunk 271 and 278; with 2 and 8 for one of pool_decode a batch
+// of 8 groups takes 76 and 60 us where 4 takes 59).  Shares of pool_chunk are at least kPoolChunkLeast units: with 16, 500 tokens and less of 8 sequences
+// of up to 4096 at d = 256, 1000 of them seen, take 128 instead of 110 us, with 8, 512 tokens there that see 64 or 1024 94 and 74 instead of 55 and 64, and with 2, 64 tokens
+// that see 4096 at d = 128 51 instead of 45 (4 query heads on each of 8).  The causal form counts tiles alone.
 template <int FORM> constexpr int kPoolChunkStart = FORM == kPoolCausal ? 0 : 6;
 template <int FORM> constexpr int kPoolDecodeStart = FORM == kPoolCausal ? 0 : 4;
-template <int FORM> constexpr int kPoolChunkLeast = FORM == kPoolCausal ? 1 : 8;             // of units, a workgroup's of pool_chunk
+template <int FORM> constexpr int kPoolChunkLeast = FORM == kPoolCausal ? 1 : 4;             // of units, a workgroup's of pool_chunk
 template <int FORM> __device__ __forceinline__ int pool_chunk_cost(int tiles) { return tiles > 0 ? tiles + kPoolChunkStart<FORM> : 0; }
 template <int FORM> __device__ __forceinline__ int pool_decode_cost(int tiles) { return tiles > 0 ? tiles + kPoolDecodeStart<FORM> : 0; }
 // the same of pool_decode, whose blocks of a sequence have all the same tiles
