@@ -15,7 +15,9 @@ namespace {
 
 constexpr int kAngles = 1024;                                // pairs (cos, sin) of a workgroup's tokens
 constexpr int kLeastBlocks = 2048;                           // workgroups of a tensor that several tokens in one shall leave
-constexpr int kGradBlocks = 512;                             // workgroups of a tensor whose sums of the weights' gradient meet: two to a compute unit
+// Workgroups of a tensor whose sums of the weights' gradient meet: two to a compute unit.  8192 tokens with 32 and 8 heads of 128, bf16: 59 us, with 256 of them 72, with 1024 62;
+// 1777 with 10 and 5 of 96, fp32: 14.8, 18.4 and 18.3.
+constexpr int kGradBlocks = 512;
 
 struct norm_shape {
     int row_units[2];                                        // of a row: those with pairs, all
