@@ -1,6 +1,6 @@
 // pool_chunk.h -- attention over a pool for many rows a key head (a chunk of a prompt): 256 rows (tokens x query heads of the group) a workgroup.
 //
-// 2048 new tokens behind 14,336, 32 query heads on 8 key heads, d = 128, 4 bits: 584 to 616 us the call in a row of calls (boxes differ), 39 of
+// 2048 new tokens behind 14,336, 32 query heads on 8 key heads, d = 128, 4 bits: 572 to 616 us the call in a row of calls (boxes differ), 39 of
 // them the transform and the merge; in the profiler, which lets no launches overlap, the scan has 588 to 678.  The two products alone, the same loop
 // without softmax, decoding and reads of LDS, took 370 (the rate of a large library product, 1.4 PFLOP/s, at the power limit).  What bounds it is that
 // matrix and vector instructions hardly overlap: of a SIMD's 1.11 M clocks the matrix unit is busy for 0.49 M and the vector ALU for 0.60 M,
