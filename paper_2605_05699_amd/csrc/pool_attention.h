@@ -429,39 +429,75 @@ __device__ __forceinline__ void pool_store16(const floatx16& acc, float down, fl
 
 // The end of 32 rows: division by the sum of weights (over both halves' keys already) and R_v.  The sums are taken as fp16 hi + lo
 // under a power of two per row, the matrix as hi + lo, so that nothing is lost here.  dst: the lane's row (l % 32), or null.
-template <int D>
-__device__ __forceinline__ void pool_finish(pool_block<D>& b, const uint4* __restrict__ table, float unscale, char* dst, int bf16, int lane) {
-    float m = 0.0f;
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) m = fmaxf(m, fabsf(b.sums[k][v]));
-    m = other_half_max(m);
-    const int e = max((int)((__float_as_uint(m) >> 23) & 0xFF) - 127, -100);
-    const float up = pool_power(14 - e);
-    const float down = (b.den > 0.0f ? 1.0f / b.den : 0.0f) * unscale, p0 = pool_power(e - 14), p1 = pool_power(b.e);
+template <int D> struct pool_ending {
     half8 hi[D / 16], lo[D / 16];
+    float down, p0, p1;
+    __device__ __forceinline__ pool_ending(const pool_block<D>& b, float unscale) {
+        float m = 0.0f;
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k)
+        for (int k = 0; k < D / 32; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float x = b.sums[k / 2][8 * (k % 2) + i] * up;
-            hi[k][i] = (_Float16)x;
-            lo[k][i] = (_Float16)(x - (float)hi[k][i]);
-        }
-    const int h = lane >> 5;
-#pragma unroll 1
-    for (int j = 0; j < D / 32; ++j) {
+            for (int v = 0; v < 16; ++v) m = fmaxf(m, fabsf(b.sums[k][v]));
+        m = other_half_max(m);
+        const int e = max((int)((__float_as_uint(m) >> 23) & 0xFF) - 127, -100);
+        const float up = pool_power(14 - e);
+        down = (b.den > 0.0f ? 1.0f / b.den : 0.0f) * unscale, p0 = pool_power(e - 14), p1 = pool_power(b.e);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = b.sums[k / 2][8 * (k % 2) + i] * up;
+                hi[k][i] = (_Float16)x;
+                lo[k][i] = (_Float16)(x - (float)hi[k][i]);
+            }
+    }
+    // the outputs from 32 j on; at: the lane's units of the matrix's rows for them, [D / 16][hi, lo][64]
+    __device__ __forceinline__ void rows(const uint4* at, int j, char* dst, int bf16, int half) const {
         floatx16 acc{0};
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-            const half8 ah = __builtin_bit_cast(half8, table[((j * (D / 16) + k) * 2 + 0) * 64 + lane]);
-            const half8 al = __builtin_bit_cast(half8, table[((j * (D / 16) + k) * 2 + 1) * 64 + lane]);
+            const half8 ah = __builtin_bit_cast(half8, at[(2 * k + 0) * 64]), al = __builtin_bit_cast(half8, at[(2 * k + 1) * 64]);
             acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, hi[k], acc, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, hi[k], acc, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, lo[k], acc, 0, 0, 0);
         }
-        pool_store16(acc, down, p0, p1, dst, 32 * j + 16 * h, bf16);
+        pool_store16(acc, down, p0, p1, dst, 32 * j + 16 * half, bf16);
+    }
+};
+template <int D> constexpr int kPoolSlab = D / 16 * 2 * 64;      // units of the matrix for 32 outputs
+template <int D>
+__device__ __forceinline__ void pool_finish(const pool_block<D>& b, const uint4* __restrict__ table, float unscale, char* dst, int bf16, int lane) {
+    const pool_ending<D> end(b, unscale);
+#pragma unroll 1
+    for (int j = 0; j < D / 32; ++j) end.rows(table + j * kPoolSlab<D> + lane, j, dst, bf16, lane >> 5);
+}
+// The same by all NT / 64 wavefronts of a workgroup, the matrix by way of LDS, 32 outputs of it at a time in one of two buffers (read by every wavefront
+// for itself, it is 512 KB a workgroup at d = 128).  lds0, lds1: kPoolSlab<D> units each, free behind a barrier that is here.
+template <int D, int NT>
+__device__ __forceinline__ void pool_finish_together(const pool_block<D>& b, const uint4* __restrict__ table, float unscale, char* dst, int bf16, int tid, uint4* lds0,
+                                                     uint4* lds1) {
+    constexpr int N = (kPoolSlab<D> + NT - 1) / NT;
+    u32x4 x[N];
+    const auto fetch = [&](int j) __attribute__((always_inline)) {           // (threads beyond the last unit load it again)
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = reinterpret_cast<const u32x4*>(table)[j * kPoolSlab<D> + min(tid + NT * i, kPoolSlab<D> - 1)];
+    };
+    const auto put = [&](uint4* to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (kPoolSlab<D> % NT == 0 || tid + NT * i < kPoolSlab<D>) to[tid + NT * i] = __builtin_bit_cast(uint4, x[i]);
+    };
+    fetch(0);
+    const pool_ending<D> end(b, unscale);
+    __syncthreads();                                         // (the buffers have been read)
+    put(lds0);
+#pragma unroll 1
+    for (int j = 0; j < D / 32; ++j) {
+        __syncthreads();                                     // (these rows are there, those before have been read)
+        const bool more = j + 1 < D / 32;                    // uniform
+        if (more) fetch(j + 1);
+        end.rows((j & 1 ? lds1 : lds0) + (tid & 63), j, dst, bf16, tid >> 5 & 1);
+        if (more) put(j & 1 ? lds0 : lds1);
     }
 }
 

@@ -43,6 +43,10 @@ template <bool WALK, int FORM> __device__ __forceinline__ pool_gap<FORM> pool_sa
     return g;
 }
 
+// Rows end with the matrix by way of LDS (pool_finish_together) where segments are short, in the sliding form, and registers allow it: at 192 dimensions and more the
+// loop spills for it.  8192 tokens, 4 query heads to each of 8, that see 64: 164 us, now 153 (d = 128), that see 1024: 300, now 288; d = 160, 4 heads: 127 and 118.
+template <int D, int FORM> constexpr bool kPoolTogether = FORM == kPoolSliding && D <= 160;
+
 template <int D, int BITS, int FORM>
 __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kernel(const pool_attention_args a) {
     constexpr int W = kPoolChunkWaves, NT = 64 * W, KEYS = kPoolChunkKeys<D>, ROWS = kPoolBlock * W, KB = KEYS / 32;
@@ -51,6 +55,7 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
     constexpr int UNITS = KEYS * T;                          // of 16 channels, of K and of V each
     constexpr int N = 2 * UNITS <= NT ? 1 : 2;               // a thread's: one of K or of V (then all of the wavefront's), or one place of both
     static_assert(UNITS % 64 == 0 && UNITS <= NT && (N == 2 || 64 * W % UNITS == 0), "whole wavefronts");
+    static_assert(!kPoolTogether<D, FORM> || kPoolSlab<D> * 16 <= 2 * KEYS * KROW, "room for the end");
     typedef typename pool_codes<BITS>::type code_t;
     __shared__ __align__(16) unsigned char k_lds[2][KEYS * KROW], v_lds[2][KEYS * VROW];
     __shared__ uint4 ring[4];                                // of tile t % 4: largest scales (bits) of K, of V where they outgrew the exponents; blocks of 16
@@ -387,7 +392,10 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
             asm("" : "+v"(again));
             row = pool_row_of(q, head, a.group, rt * ROWS + wave * kPoolBlock + (again & 31));
             char* const to = row.there ? a.out + row.token * a.out_token + row.head * a.out_head : nullptr;
-            pool_finish<D>(b, a.out_table, a.out_unscale, to, a.bf16, lane);
+            if constexpr (kPoolTogether<D, FORM>)
+                pool_finish_together<D, NT>(b, a.out_table, a.out_unscale, to, a.bf16, tid, reinterpret_cast<uint4*>(k_lds), reinterpret_cast<uint4*>(v_lds));
+            else
+                pool_finish<D>(b, a.out_table, a.out_unscale, to, a.bf16, lane);
         } else if (FORM == kPoolCausal || rt * ROWS + wave * kPoolBlock < q.n_new * a.group) {     // (sums of no row: nobody reads them)
             b.put(a.chunk_parts + ((2LL * w + (at_begin ? 0 : 1)) * W + wave) * kPoolPart<D>, lane, FORM == kPoolShared && seq >= a.s.n_seq);
         }
