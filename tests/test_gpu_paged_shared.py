@@ -97,6 +97,20 @@ def test_any_number_of_workgroups(B, workgroups, group):
     s.close()
 
 
+@pytest.mark.parametrize("workgroups", [1, 3, 40, 0])
+def test_more_blocks_of_rows_than_lanes(B, workgroups):
+    """75 blocks of 256 rows to a key head of one sequence's own tokens, and 80 of what its group has in common."""
+    s = fork(Serving(B, 64, 32, 4, 16, 2, n=5, max_length=400, seed=19), [0, 3, 5], [4, 3])
+    new, group = [17, 300, 3, 1, 40], 64
+    s.append([a + b for a, b in zip(new, (0, 7, 30, 20, 0))])
+    q = queries(s, new, group, torch.float16)
+    B.srft_plan_set_max_workgroups(s.plans[0].handle, workgroups)
+    out = share(s, q, new, 0.1, prefixes_of(B, [0, 3, 5], [64, 48]))
+    check(s, out, q, new, 0.1, group)
+    B.srft_plan_set_max_workgroups(s.plans[0].handle, 0)
+    s.close()
+
+
 def test_only_the_first_sequence_of_a_group_has_its_table_read_for_the_pages_in_common(B):
     s = fork(Serving(B, 128, 32, 4, 16, 2, n=6, max_length=700, seed=9), [0, 3, 6], [20, 30])
     s.append([1, 40, 20, 7, 16, 5])

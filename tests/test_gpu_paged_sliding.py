@@ -142,6 +142,40 @@ def test_any_number_of_workgroups(B, workgroups):
     s.close()
 
 
+@pytest.mark.parametrize("workgroups", [1, 3, 40, 0])
+@pytest.mark.parametrize("recent", [33, 1000])
+def test_more_blocks_of_rows_than_lanes(B, workgroups, recent):
+    """75 blocks of 256 rows to a key head of the second sequence, behind and in front of others; with 1000 seen, everything."""
+    s = Serving(B, 64, 32, 4, 16, 2, n=5, max_length=400, seed=19)
+    new, group = [17, 300, 0, 1, 40], 64
+    s.append([a + b for a, b in zip(new, (20, 70, 30, 100, 0))])
+    q = queries(s, new, group, torch.float16)
+    B.srft_plan_set_max_workgroups(s.plans[0].handle, workgroups)
+    out = slide(s, q, new, 0.1, recent, 5)
+    check(s, out, q, new, 0.1, group, recent, 5)
+    B.srft_plan_set_max_workgroups(s.plans[0].handle, 0)
+    s.close()
+
+
+@pytest.mark.parametrize("workgroups", [1, 7, 0])
+@pytest.mark.parametrize("recent", [20, 1000])
+def test_blocks_of_rows_that_see_nothing(B, workgroups, recent):
+    """More new tokens than tokens, in chunks of several key heads and sequences: the rows in front of the first token are zero, the others as ever."""
+    s = Serving(B, 64, 32, 4, 16, 2, n=3, max_length=400, seed=20)
+    s.append([60, 70, 33])
+    new, group = [150, 300, 33], 16
+    seqs, q = s.seqs(new), queries(s, new, group, torch.float16)
+    B.srft_plan_set_max_workgroups(s.plans[0].handle, workgroups)
+    out = slide(s, q, new, 0.1, recent, 3, seqs)
+    B.srft_plan_set_max_workgroups(s.plans[0].handle, 0)
+    seeing = torch.cat([torch.arange(a + n - m, a + n) for a, n, m in zip((0, 150, 450), new, (60, 70, 33))]).cuda()
+    nothing = torch.ones(sum(new), dtype=torch.bool, device="cuda")
+    nothing[seeing] = False
+    assert not out[nothing].any()
+    check(s, out[seeing], q[seeing], [60, 70, 33], 0.1, group, recent, 3)
+    s.close()
+
+
 def test_captured_steps_over_growing_sequences(B):
     """One graph, replayed with the next step's table, windows and lengths, beside eager calls on another stream and workspace."""
     s = Serving(B, 128, 32, 4, 16, 2, n=4, max_length=300, seed=6)
