@@ -248,8 +248,8 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
                 uint64_t at[2];
 #pragma unroll
                 for (int k = 0; k < (ONE ? 1 : 2); ++k) {
-                    const int page = __builtin_amdgcn_readlane(pages, k), slot = min(gap.tile(tile) * KEYS + 16 * (u_block + k), q.full - 16) & (R - 1);
-                    const bool ok = pool_there(page, a.s.n_pages) && !gap.hides(gap.tile(tile) * KEYS + 16 * (u_block + k));
+                    const int page = __builtin_amdgcn_readlane(pages, k), key = min(gap.tile(tile) * KEYS + 16 * (u_block + k), q.full - 16), slot = key & (R - 1);
+                    const bool ok = pool_there(page, a.s.n_pages) && !gap.hides(key);    // (of the block that is read)
                     there |= (ok ? 1u : 0u) << k;
                     at[k] = ((uint64_t)((ok ? page : 0) * (uint64_t)a.heads + head) << a.s.log_R) + slot;
                 }

@@ -284,8 +284,8 @@ __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB,
             uint32_t known = 0;
             uint64_t f0, f1, f2 = 0, f3 = 0;
             const auto address = [&](int i, uint64_t& code, uint64_t& scale) __attribute__((always_inline)) {
-                const int page = __builtin_amdgcn_readlane(pages, i), slot = min(gap.tile(tile) * KEYS + 16 * i, q.full - 16) & (R - 1);
-                const bool ok = pool_there(page, a.s.n_pages) && !gap.hides(gap.tile(tile) * KEYS + 16 * i);
+                const int page = __builtin_amdgcn_readlane(pages, i), key = min(gap.tile(tile) * KEYS + 16 * i, q.full - 16), slot = key & (R - 1);
+                const bool ok = pool_there(page, a.s.n_pages) && !gap.hides(key);        // (of the block that is read)
                 known |= (ok ? 1u : 0u) << i;
                 const uint64_t row = ((uint64_t)((ok ? page : 0) * (uint64_t)a.heads + head) << a.s.log_R) + slot;
                 code = row * CBY;
