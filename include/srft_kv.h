@@ -432,8 +432,10 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
  * Sliding attention: srft_pool_attention where a token sees, of the tokens up to itself, the last `recent` ones (itself among them) and the
  * sequence's first `sinks` ones.  Pages that no row of the call sees are not read: they may be another sequence's by then, and their entries in
  * the page table may hold anything.
- *   recent, sinks   recent >= 1, sinks >= 0 (else SRFT_ERR_BAD_N).  With recent + sinks >= max_length it is srft_pool_attention.
- *   workspace_dev   srft_pool_attention_sliding_workspace_bytes bytes, 256-byte aligned, overwritten.
+ *   recent, sinks   recent >= 1, sinks >= 0 (else SRFT_ERR_BAD_N).  With recent + sinks >= max_length it is srft_pool_attention, in its sizes and with
+ *                   its workspace too.
+ *   workspace_dev   srft_pool_attention_sliding_workspace_bytes bytes (enough for any reach), 256-byte aligned, overwritten.
+ * The sizes named at srft_pool_attention stay below the same bounds with tiles = max_length / 32 + 8 (else SRFT_ERR_BAD_N, of the workspace's size too).
  */
 int64_t srft_pool_attention_sliding_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, int64_t n_new, int n_q_heads);
 int srft_pool_attention_sliding(const srft_pool_t* pool, const srft_paged_seqs* seqs, const void* q_dev, int type, int64_t n_new, int n_q_heads,
@@ -451,7 +453,8 @@ int srft_pool_attention_sliding(const srft_pool_t* pool, const srft_paged_seqs* 
  * in front of it, or past n_seq, is taken as that.
  *   prefixes        0 <= n_groups <= n_seq (else SRFT_ERR_BAD_N); without groups the pointers may be NULL.
  *   workspace_dev   srft_pool_attention_shared_workspace_bytes bytes, 256-byte aligned, overwritten.
- * With 2 n_new in the place of n_new and n_seq + n_groups in that of n_seq the sizes named at srft_pool_attention stay below the same bounds.
+ * With groups, tiles = max_length / 32 + 8 and N = n_seq + n_groups the sizes named at srft_pool_attention are (3 N + 8) * n_heads * tiles in the place of
+ * 2 S tiles, and (2 n_new * G / 256 + N) * n_heads * max(tiles, 8); without groups the call is srft_pool_attention, in its sizes and with its workspace too.
  */
 typedef struct srft_shared_prefixes {
     int32_t n_groups;

@@ -782,7 +782,8 @@ def srft_pool_attention_sliding(pool: PagePool, seqs: PagedSeqs, q: torch.Tensor
     if not -1 << 63 <= recent < 1 << 63 or not -1 << 63 <= sinks < 1 << 63:          # (ctypes would keep the low bits)
         raise ValueError("recent and sinks must fit int64_t")
     (q_at, q_token, q_head), (o_at, o_token, o_head) = _rows(q, "q"), _rows(out, "out")
-    space = _pool_workspace(workspace, srft_pool_attention_sliding_workspace_bytes(pool, seqs, n, heads))
+    sized = srft_pool_attention_workspace_bytes if recent + sinks >= seqs.max_length else srft_pool_attention_sliding_workspace_bytes
+    space = _pool_workspace(workspace, sized(pool, seqs, n, heads))
     _check(lib().srft_pool_attention_sliding(pool.handle, seqs.address, q_at, DTYPES[q.dtype], n, heads, q_token, q_head, softmax_scale, recent, sinks,
                                              o_at, o_token, o_head, space, _stream_handle(stream)), "srft_pool_attention_sliding")
 

@@ -94,11 +94,18 @@ pool_attention_kernel_t srft_pool_chunk_kernel_of(const srft_plan* p, int form) 
            : form == kPoolShared ? srft_pick_pool_chunk_shared(p->d, p->bits) : srft_pick_pool_chunk(p->d, p->bits);
 }
 
-int check(const srft_pool* pool, const srft_paged_seqs* seqs, const form_of_call& f, int64_t n_new, int q_heads) {
+int check(const srft_pool* pool, const srft_paged_seqs* seqs, const form_of_call& f, int64_t n_new) {
     if (f.form == kPoolShared && !f.prefixes) return SRFT_ERR_NULL;
     const int rc = srft_pool_check(pool, seqs, n_new);
     if (rc != SRFT_OK) return rc;
-    if (f.recent < 1 || f.sinks < 0 || f.groups() < 0 || f.groups() > seqs->n_seq || (f.prefixes && f.prefixes->reserved != 0)) return SRFT_ERR_BAD_N;
+    return f.recent < 1 || f.sinks < 0 || f.groups() < 0 || f.groups() > seqs->n_seq || (f.prefixes && f.prefixes->reserved != 0) ? SRFT_ERR_BAD_N : SRFT_OK;
+}
+// The form that answers a call: what sees everything, and groups of none, are the causal form.
+form_of_call answering(const srft_paged_seqs* s, const form_of_call& f) {
+    const bool all = f.form == kPoolSliding && std::min(f.recent, kPoolMaxLength) + std::min(f.sinks, kPoolMaxLength) >= s->max_length;
+    return all || (f.form == kPoolShared && f.groups() == 0) ? form_of_call{} : f;
+}
+int check_sizes(const srft_pool* pool, const srft_paged_seqs* seqs, const form_of_call& f, int64_t n_new, int q_heads) {
     if (q_heads < 1 || q_heads % pool->heads != 0 || q_heads > 64 * pool->heads || n_new * q_heads >= (1LL << 31) - 32) return SRFT_ERR_BAD_N;
     // units of work (kPoolMostUnits), tiles and workgroups are counted with 32 bits
     const int d = pool->plan_k->d, group = q_heads / pool->heads;
@@ -111,13 +118,19 @@ int check(const srft_pool* pool, const srft_paged_seqs* seqs, const form_of_call
 }
 
 int64_t bytes_of(const srft_pool* pool, const srft_paged_seqs* seqs, const form_of_call& f, int64_t n_new, int q_heads) {
-    const int rc = check(pool, seqs, f, n_new, q_heads);
-    return rc != SRFT_OK ? rc : layout(pool, seqs, f, n_new, q_heads).bytes;
+    int rc = check(pool, seqs, f, n_new);
+    if (rc != SRFT_OK) return rc;
+    const form_of_call by = answering(seqs, f);
+    rc = check_sizes(pool, seqs, by, n_new, q_heads);
+    return rc != SRFT_OK ? rc : layout(pool, seqs, by, n_new, q_heads).bytes;
 }
 
 int attend(const srft_pool* pool, const srft_paged_seqs* seqs, form_of_call f, const void* q_dev, int type, int64_t n_new, int n_q_heads, int64_t q_token,
            int64_t q_head, float softmax_scale, void* out_dev, int64_t out_token, int64_t out_head, void* workspace_dev, void* hip_stream) {
-    int rc = check(pool, seqs, f, n_new, n_q_heads);
+    int rc = check(pool, seqs, f, n_new);
+    if (rc != SRFT_OK) return rc;
+    f = answering(seqs, f);
+    rc = check_sizes(pool, seqs, f, n_new, n_q_heads);
     if (rc != SRFT_OK) return rc;
     if ((type != SRFT_F16 && type != SRFT_BF16) || !std::isfinite(softmax_scale)) return SRFT_ERR_BAD_N;
     if (q_token % 8 || q_head % 8 || out_token % 8 || out_head % 8) return SRFT_ERR_ALIGN;
@@ -132,9 +145,6 @@ int attend(const srft_pool* pool, const srft_paged_seqs* seqs, form_of_call f, c
     if (!srft_aligned(q_dev, 16) || !srft_aligned(out_dev, 16) || !srft_aligned(workspace_dev, 256)) return SRFT_ERR_ALIGN;
     const srft_plan *pk = pool->plan_k, *pv = pool->plan_v;
     const int d = pk->d, group = n_q_heads / pool->heads;
-    // what sees everything, and groups of none, are the causal form
-    if ((f.form == kPoolSliding && std::min(f.recent, kPoolMaxLength) + std::min(f.sinks, kPoolMaxLength) >= seqs->max_length) || (f.form == kPoolShared && f.groups() == 0))
-        f = form_of_call{};
     const workspace w = layout(pool, seqs, f, n_new, n_q_heads);
     const split sp = split_of(seqs, f, n_new, group, d);
     char* const base = (char*)workspace_dev;
@@ -288,9 +298,9 @@ int srft_pool_attention(const srft_pool_t* pool, const srft_paged_seqs* seqs, co
 }
 
 int64_t srft_pool_attention_sliding_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, int64_t n_new, int n_q_heads) {
-    // (with few tokens to see the call is the causal form, whose scan may have more workgroups)
-    const int64_t all = bytes_of(pool, seqs, {}, n_new, n_q_heads), some = bytes_of(pool, seqs, {kPoolSliding}, n_new, n_q_heads);
-    return all < 0 ? all : std::max(all, some);
+    // (of the least reach, and of one that sees everything: that is the causal form, whose scan may have more workgroups)
+    const int64_t all = bytes_of(pool, seqs, {}, n_new, n_q_heads), some = bytes_of(pool, seqs, {kPoolSliding, 1, 0}, n_new, n_q_heads);
+    return std::min(all, some) < 0 ? std::min(all, some) : std::max(all, some);
 }
 int srft_pool_attention_sliding(const srft_pool_t* pool, const srft_paged_seqs* seqs, const void* q_dev, int type, int64_t n_new, int n_q_heads,
                                 int64_t q_token, int64_t q_head, float softmax_scale, int64_t recent, int64_t sinks, void* out_dev,
@@ -301,8 +311,7 @@ int srft_pool_attention_sliding(const srft_pool_t* pool, const srft_paged_seqs* 
 
 int64_t srft_pool_attention_shared_workspace_bytes(const srft_pool_t* pool, const srft_paged_seqs* seqs, const srft_shared_prefixes* prefixes,
                                                    int64_t n_new, int n_q_heads) {
-    const int64_t bytes = bytes_of(pool, seqs, {kPoolShared, kPoolMaxLength, 0, prefixes}, n_new, n_q_heads);
-    return bytes < 0 || prefixes->n_groups > 0 ? bytes : bytes_of(pool, seqs, {}, n_new, n_q_heads);
+    return bytes_of(pool, seqs, {kPoolShared, kPoolMaxLength, 0, prefixes}, n_new, n_q_heads);
 }
 int srft_pool_attention_shared(const srft_pool_t* pool, const srft_paged_seqs* seqs, const srft_shared_prefixes* prefixes, const void* q_dev, int type,
                                int64_t n_new, int n_q_heads, int64_t q_token, int64_t q_head, float softmax_scale, void* out_dev,
