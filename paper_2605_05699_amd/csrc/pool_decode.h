@@ -767,7 +767,9 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
         floatx4 o[kPoolOwn<D>];
 #pragma unroll
         for (int i = 0; i < kPoolOwn<D>; ++i) o[i] = floatx4{0, 0, 0, 0};
-        const pool_row r = pool_row_of(q, head, a.group, (rb * CB + c) * 16 + (lane & 15));
+        const auto row = [&]() __attribute__((always_inline)) { return pool_row_of(q, head, a.group, (rb * CB + c) * 16 + (lane & 15)); };
+        pool_row r{};
+        if constexpr (FORM == kPoolShared) r = row();
         // parts v .. v + AHEAD - 1, up to w1, whose sums and heads `sums` and `heads` give
         const auto join = [&](int v, int w1, auto heads, auto sums) __attribute__((always_inline)) {
             floatx4 x[AHEAD][kPoolOwn<D>];
@@ -831,6 +833,7 @@ __device__ __forceinline__ void pool_decode_merge(const pool_attention_args& a, 
             for (int v = w0; v <= w1; v += AHEAD)            // (one round of loads for AHEAD parts, the sums so far brought under their maximum)
                 join(v, w1, [&](int w, pool_part_head& h) __attribute__((always_inline)) { h.load(part(w, c) + 16 * D, lane); },
                      [&](int w, int n) __attribute__((always_inline)) { return reinterpret_cast<const floatx4*>(part(w, c))[n * 64 + lane]; });
+        if constexpr (FORM != kPoolShared) r = row();        // (a division, behind the loads)
         char* const dst = r.there ? a.out + r.token * a.out_token + r.head * a.out_head : nullptr;
         if (c > 0) __syncthreads();
         pool_finish16<D, true>(o, den, e_all, lds, a.out_table16, a.out_unscale, dst, a.bf16, wave, lane);
