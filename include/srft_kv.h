@@ -446,7 +446,8 @@ int srft_pool_attention_sliding(const srft_pool_t* pool, const srft_paged_seqs* 
  * Attention of sequences that begin with the same pages (samples of one prompt, conversations behind one long instruction: forks whose full
  * pages are not copied).  The outputs are srft_pool_attention's; the pages in common are read once for up to 256 rows of a key head, of whichever
  * of the group's sequences (for 16 or 32 in groups that bring no more than 48, or in calls of no more than 128).  Roundings are those named there,
- * where the rows of a group count together, as those of a sequence that brings many, if they are more than that.
+ * where the rows of a group count together, as those of a sequence that brings many, if they are more than that (a step of 64 conversations with 8 rows
+ * a key head each: 1.3e-3 of an output's size, where srft_pool_attention has 3e-4).
  * Group g is the sequences groups[g] .. groups[g + 1] - 1, whose first tokens[g] tokens lie in the same pages; of these, whole pages count
  * that all of the group's sequences with new tokens hold without them, and the entries of its first such sequence name them (those of the
  * others are not read).  Sequences outside of all groups are as in srft_pool_attention.  Groups are ascending: a bound below the one

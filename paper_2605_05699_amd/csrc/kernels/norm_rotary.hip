@@ -4,9 +4,12 @@
 // Sums are fp32; an output is rounded once.
 //
 // Bound by memory: x is read once and y written once (dy and x, and dx).  8192 tokens, 40 heads of 128, bf16 -> fp16: 168 MB in 36 us, 4.7 TB/s
-// (norm and positions one after the other would move 336 MB); the gradients, 252 MB, 47 us, 5.4 TB/s, and 5 more in the second kernel.  A row belongs to 2^log_lanes neighbouring lanes of a wavefront, K units
-// of 2 V channels to each (rotary_rows.h), so that a row's sums meet within the wavefront and its values stay in registers between
-// the loads and the stores.  A workgroup has `tokens` tokens with all their heads; their angles are computed once, into LDS.
+// (norm and positions one after the other would move 336 MB); fp32, 336 MB, 58 us; the gradients, 252 MB, 47 us, 5.4 TB/s, and 5 more in the second
+// kernel.  Rows that are not aligned to four of their elements, or whose pairs do not come in fours, go a channel an access: the same bf16 rows one
+// element further on 65 us, rows of 80 channels with 10 pairs 64 (105 MB), their gradients 137 (157 MB).
+// A row belongs to 2^log_lanes neighbouring lanes of a wavefront, K units of 2 V channels to each (rotary_rows.h), so that a row's sums meet
+// within the wavefront and its values stay in registers between the loads and the stores.  A workgroup has `tokens` tokens with all their heads;
+// their angles are computed once, into LDS.
 // The weights' gradient: a lane has the same channels of every row, adds its rows up in registers, a workgroup its lanes in LDS, and a second
 // kernel the workgroups: always in the same order.
 #include "../rotary_rows.h"
@@ -15,8 +18,8 @@ namespace {
 
 constexpr int kAngles = 1024;                                // pairs (cos, sin) of a workgroup's tokens
 constexpr int kLeastBlocks = 2048;                           // workgroups of a tensor that several tokens in one shall leave
-// Workgroups of a tensor whose sums of the weights' gradient meet: two to a compute unit.  8192 tokens with 32 and 8 heads of 128, bf16: 59 us, with 256 of them 72, with 1024 62;
-// 1777 with 10 and 5 of 96, fp32: 14.8, 18.4 and 18.3.
+// Workgroups of a tensor whose sums of the weights' gradient meet: two to a compute unit.  8192 tokens with 32 and 8 heads of 128, bf16: 59 us,
+// with 256 of them 72, with 1024 62; 1777 with 10 and 5 of 96, fp32: 14.8, 18.4 and 18.3.
 constexpr int kGradBlocks = 512;
 
 struct norm_shape {
@@ -137,7 +140,8 @@ __device__ __forceinline__ void angles_of(const norm_shape& s, unsigned first, i
     }
 }
 
-// blockIdx.z: the tensor; one workgroup of it for a.tokens tokens (srft_grid).  The first rows and the weights are on their way before the angles are computed.
+// blockIdx.z: the tensor; one workgroup of it for a.tokens tokens (srft_grid).  The first rows and the weights are on their way before the
+// angles are computed.
 template <class IN, class OUT, int V, int K>
 __global__ void __launch_bounds__(256) srft_norm_rotary_kernel(const norm_args a) {
     __shared__ float2 cs[kAngles];

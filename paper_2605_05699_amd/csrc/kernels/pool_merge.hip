@@ -1,12 +1,13 @@
 // Attention over a pool, the end: the sums of rows whose keys went to several workgroups are added in the order of the keys and
 // finished; rows of sequences without a tile are zero.  The first a.decode_merges workgroups take the rows of the scan for few rows
 // (pool_decode_merge), the others those of chunks, in one launch: apart, the first took 17 us beside the 29 of the others (d = 256).
-// Chunks: one workgroup of four wavefronts per 32 rows of a key head, of the blocks of 256 rows that there are (by the longest sequence for each, 255 decode steps beside a
-// prompt of 4096 tokens, 64 query heads, were a million workgroups, nearly all of them empty: 1376 us, now 36), each with every fourth
-// run of 32 positions of the sums and then of the outputs (one wavefront per 32 rows read every part, and the matrix, one after
-// the other: 104 us at d = 256, 28 at d = 128).  Bound by the chain of loads where parts are few (a first round for the maxima alone: 6.9 us,
-// now 5.5, for a step of 4 sequences), by the parts' bytes where they are many (23 us for 67 MB at d = 128; more of them in flight is slower).  Shared forms: the parts
-// of the tokens in common first, read by row; 64 conversations' 512 rows 16 us (28 with channels gathered one by one).  Rows that their scan has finished have nothing to do here.
+// Chunks: one workgroup of four wavefronts per 32 rows of a key head, of the blocks of 256 rows that there are (by the longest sequence for each, 255
+// decode steps beside a prompt of 4096 tokens, 64 query heads, were a million workgroups, nearly all of them empty: 1376 us, now 36), each with every
+// fourth run of 32 positions of the sums and then of the outputs (one wavefront per 32 rows read every part, and the matrix, one after the other: 104
+// us at d = 256, 28 at d = 128).  Bound by the chain of loads where parts are few (a first round for the maxima alone: 6.9 us, now 5.5, for a step of
+// 4 sequences), by the parts' bytes where they are many (23 us for 67 MB at d = 128; more of them in flight is slower).  Shared forms: the parts of
+// the tokens in common first, read by row; 64 conversations' 512 rows 16 us (28 with channels gathered one by one).  Rows that their scan has
+// finished have nothing to do here.
 #include "../pool_decode.h"
 
 namespace {
@@ -42,8 +43,8 @@ __device__ __forceinline__ void chunk_merge(const pool_attention_args& a, unsign
         return;
     }
     if (units == 0) return;                                  // (too many of them: see kPoolMostUnits)
-    // Units of a key head's blocks of rows, and of those in front of this one: by one wavefront.  (By all four, each for itself, 8192 workgroups with nothing to merge
-    // were 23 us, the vector ALU's time.)
+    // Units of a key head's blocks of rows, and of those in front of this one: by one wavefront.  (By all four, each for itself, 8192 workgroups with
+    // nothing to merge were 23 us, the vector ALU's time.)
     __shared__ int2 units_of;
     if (wave == 0) {
         int all = 0, in_front = 0;

@@ -14,8 +14,9 @@
 // hi + lo, scales on the results in fp32; a weight times the scale of its key and group is rounded to fp16 once.  pool_chunk, which the matrix
 // cores bound, has one matrix instruction where that would take two: q', the dequantized w (code * scale, the scale rounded first) and
 // the weights p are fp16, half a step (2^-11) each at most.  Against 64 bits that is 3e-4 and 1.2e-3 of an output's size (1.5e-3 where one scale
-// serves a whole row), the output's own rounding to fp16 included.  Sums, maxima and exponents are fp32.  None of the operands can leave fp16's range: q' has a power of two per
-// row, w a running one taken from the scales, the weights are at most 2^(kLazy + kHigh) in pool_chunk, and times a scale 2^(kLazy + 7) in pool_decode.
+// serves a whole row), the output's own rounding to fp16 included.  Sums, maxima and exponents are fp32.  None of the operands can leave fp16's
+// range: q' has a power of two per row, w a running one taken from the scales, the weights are at most 2^(kLazy + kHigh) in pool_chunk, and times a
+// scale 2^(kLazy + 7) in pool_decode.
 //
 // Forms.  Causal: srft_pool_attention.  Sliding: rows see the last `recent` tokens and the first `sinks` ones; of a block's tiles those between its
 // sinks and its first row's recent tokens are left out (pool_gap), what is left is numbered through.  Shared: sequences that have pages in
@@ -35,8 +36,9 @@ constexpr float kPoolLowest = -3.0e38f;                      // "no key yet": fi
 constexpr int kPoolNoExponent = -200;                        // of V: "no value yet"
 constexpr float kLazy = 8.0f;                                // how far (in powers of two) weights may grow past the maximum that they are taken from
 // pool_chunk rounds weights to fp16, so it takes them as large as that allows: up to 2^(kLazy + kHigh).  What is lost then are weights below
-// 2^-32 of a row's largest; under the maximum itself they were those below 2^-25, and behind one dominant key the others lost up to 2^-25 of it each (3 %
-// of the output over 2^20 keys).  From kNear on, where an exponent's own rounding could take a weight past fp16's range, they have the older room.
+// 2^-32 of a row's largest; under the maximum itself they were those below 2^-25, and behind one dominant key the others lost up to 2^-25 of it each
+// (3 % of the output over 2^20 keys).  From kNear on, where an exponent's own rounding could take a weight past fp16's range, they have the older
+// room.
 constexpr float kHigh = 7.0f, kNear = 1048576.0f;
 constexpr int kPoolDecodeRows = 32;                          // most rows of one key head that pool_decode takes, in blocks of 16
 constexpr int kPoolTeam = 4;                                 // wavefronts of a workgroup of pool_decode and pool_merge
@@ -157,10 +159,10 @@ __device__ __forceinline__ int pool_chunk_tiles(const pool_attention_args& a, co
 }
 // What a block of rows counts for when the work is shared out: its tiles, and the time that its start and its end take, in tiles, so that a
 // workgroup with many short segments has fewer tiles (chunks of 8 sequences, 40 to 300 tokens, behind 12,000 in common: the workgroups with the
-// own tokens' segments had 30 of them, 560 us; now 275, and with 4 or 8 for a start of pool_chunk 271 and 278; with 2 and 8 for one of pool_decode a batch
-// of 8 groups takes 76 and 60 us where 4 takes 59).  Shares of pool_chunk are at least kPoolChunkLeast units: with 16, 500 tokens and less of 8 sequences
-// of up to 4096 at d = 256, 1000 of them seen, take 128 instead of 110 us, with 8, 512 tokens there that see 64 or 1024 94 and 74 instead of 55 and 64, and with 2, 64 tokens
-// that see 4096 at d = 128 51 instead of 45 (4 query heads on each of 8).  The causal form counts tiles alone.
+// own tokens' segments had 30 of them, 560 us; now 275, and with 4 or 8 for a start of pool_chunk 271 and 278; with 2 and 8 for one of pool_decode a
+// batch of 8 groups takes 76 and 60 us where 4 takes 59).  Shares of pool_chunk are at least kPoolChunkLeast units: with 16, 500 tokens and less of 8
+// sequences of up to 4096 at d = 256, 1000 of them seen, take 128 instead of 110 us, with 8, 512 tokens there that see 64 or 1024 94 and 74 instead
+// of 55 and 64, and with 2, 64 tokens that see 4096 at d = 128 51 instead of 45 (4 query heads on each of 8).  The causal form counts tiles alone.
 template <int FORM> constexpr int kPoolChunkStart = FORM == kPoolCausal ? 0 : 6;
 template <int FORM> constexpr int kPoolDecodeStart = FORM == kPoolCausal ? 0 : 4;
 template <int FORM> constexpr int kPoolChunkLeast = FORM == kPoolCausal ? 1 : 4;             // of units, a workgroup's of pool_chunk
@@ -471,8 +473,8 @@ __device__ __forceinline__ void pool_finish(const pool_block<D>& b, const uint4*
 #pragma unroll 1
     for (int j = 0; j < D / 32; ++j) end.rows(table + j * kPoolSlab<D> + lane, j, dst, bf16, lane >> 5);
 }
-// The same by all NT / 64 wavefronts of a workgroup, the matrix by way of LDS, 32 outputs of it at a time in one of two buffers (read by every wavefront
-// for itself, it is 512 KB a workgroup at d = 128).  lds0, lds1: kPoolSlab<D> units each, free behind a barrier that is here.
+// The same by all NT / 64 wavefronts of a workgroup, the matrix by way of LDS, 32 outputs of it at a time in one of two buffers (read by every
+// wavefront for itself, it is 512 KB a workgroup at d = 128).  lds0, lds1: kPoolSlab<D> units each, free behind a barrier that is here.
 template <int D, int NT>
 __device__ __forceinline__ void pool_finish_together(const pool_block<D>& b, const uint4* __restrict__ table, float unscale, char* dst, int bf16, int tid, uint4* lds0,
                                                      uint4* lds1) {

@@ -31,9 +31,10 @@ constexpr int kChunkRows = kPoolBlock * kPoolChunkWaves;
 // a sequence may bring 17 to 32 rows and none brings more, up to d = 128 (beyond it two blocks' sums do not fit the registers: there a
 // workgroup takes one block, and the keys are read twice); else one, and 17 rows are a chunk.
 // A group's tokens in common go to pool_decode, in blocks that each read the keys, up to kCommonRows rows; and in calls of up to kFewRows rows, which
-// need no launch for chunks then.  With up to 16 in place of kCommonRows six samples of 800 tokens take 40 us (now 22) and five prompts with 2 to 11 samples at d = 256
-// 96 (now 67); with up to 96 six groups of 96 rows behind 4000 tokens take 85 (now 78; d = 256 134, now 115), one alone 27 (as now; as a chunk 45) and behind 16,384 tokens
-// 49 (56).  128 rows in one group: 30 us behind 2000 tokens (as a chunk 46), 58 (58) behind 16,384, at d = 256 52 (73) and 107 (100); 192: 31 (51), 72 (64), 54 (79), 133 (106).
+// need no launch for chunks then.  With up to 16 in place of kCommonRows six samples of 800 tokens take 40 us (now 22) and five prompts with 2 to 11
+// samples at d = 256 96 (now 67); with up to 96 six groups of 96 rows behind 4000 tokens take 85 (now 78; d = 256 134, now 115), one alone 27 (as
+// now; as a chunk 45) and behind 16,384 tokens 49 (56).  128 rows in one group: 30 us behind 2000 tokens (as a chunk 46), 58 (58) behind 16,384, at d
+// = 256 52 (73) and 107 (100); 192: 31 (51), 72 (64), 54 (79), 133 (106).
 constexpr int kCommonRows = 48, kFewRows = 128;
 struct split {
     int cb, rows, common_rows;

@@ -2,17 +2,17 @@
 //
 // 2048 new tokens behind 14,336, 32 query heads on 8 key heads, d = 128, 4 bits: 572 to 616 us the call in a row of calls (boxes differ), 39 of
 // them the transform and the merge; in the profiler, which lets no launches overlap, the scan has 588 to 678.  The two products alone, the same loop
-// without softmax, decoding and reads of LDS, took 370 (the rate of a large library product, 1.4 PFLOP/s, at the power limit).  What bounds it is that
-// matrix and vector instructions hardly overlap: of a SIMD's 1.11 M clocks the matrix unit is busy for 0.49 M and the vector ALU for 0.60 M,
-// 98 % together.  The energy of data that toggle comes on top: on zeros, the same instructions, the scan takes 500 to 513 us.
-// Tried on that without a gain: priorities (s_setprio) for either half of the wavefronts, decoding before the products in one half and
-// behind them in the other, a softmax spread between the matrix instructions of the values, and rows of LDS without bank conflicts at
-// the writes.  Each of these left the order within a wavefront to the fences (sched_barrier) around the matrix instructions.
+// without softmax, decoding and reads of LDS, took 370 (the rate of a large library product, 1.4 PFLOP/s, at the power limit).  What bounds it is
+// that matrix and vector instructions hardly overlap: of a SIMD's 1.11 M clocks the matrix unit is busy for 0.49 M and the vector ALU for 0.60 M, 98
+// % together.  The energy of data that toggle comes on top: on zeros, the same instructions, the scan takes 500 to 513 us.  Tried on that without a
+// gain: priorities (s_setprio) for either half of the wavefronts, decoding before the products in one half and behind them in the other, a softmax
+// spread between the matrix instructions of the values, and rows of LDS without bank conflicts at the writes.  Each of these left the order within a
+// wavefront to the fences (sched_barrier) around the matrix instructions.
 //
 // A tile of keys is
 // decoded once for all the workgroup's rows, by all its wavefronts, into LDS (two buffers: the next tile is decoded while this one is
-// used, one barrier a tile); each of the eight wavefronts (four: 946 us against 838 then) takes 32 rows through it with the scheme of pool_decode.h: keys on the
-// rows of the score product, so that scores, weights and the running softmax of a row stay in one lane and its neighbour across the
+// used, one barrier a tile); each of the eight wavefronts (four: 946 us against 838 then) takes 32 rows through it with the scheme of pool_decode.h:
+// keys on the rows of the score product, so that scores, weights and the running softmax of a row stay in one lane and its neighbour across the
 // wavefront, and weights go into the second product as they are.
 //
 // A tile is decoded under powers of two of K's and of V's scales that all wavefronts share.  They are running: they change only where a scale
@@ -20,7 +20,10 @@
 // comparison; only then it tells the others, through a ring in LDS that all look into before they decode.
 // Loads are straight-line, two tiles ahead of their use; a wavefront's part of a tile lies in one or two blocks of 16 keys, whose pages
 // make scalar addresses, the same for K and V.  At d = 256 the registers are full: a reload of a spilled address behind loads in
-// flight waited for these (119 us, now 78, for two prompts' chunks of 500 and 386 tokens among others, 8 query heads).
+// flight waited for these (119 us, then 78, for two prompts' chunks of 500 and 386 tokens among others, 8 query heads).
+// Registers spilled, causal / sliding / shared form: 192 dimensions 0 / 2 / 25, 224 9 / 26 / 56, 256 36 / 51 / 90; of the shared form's at 256 ten
+// are read again for every tile (causal four), at 192 none.  8 questions of 40 to 300 tokens behind 12,000 in common, 32 query heads on 8 key heads,
+// the shared call and the causal one over the same tokens: d = 192, 4 bits 452 and 486 us, d = 224, 8 bits 579 and 535, d = 256 615 and 581.
 #ifndef SRFT_POOL_CHUNK_H
 #define SRFT_POOL_CHUNK_H
 #include "pool_attention.h"
@@ -28,8 +31,9 @@
 constexpr int kPoolAhead = 2;                                    // reads of LDS ahead of the matrix instructions (739 us without); 4 and 6 measure the same up to d = 128 and spill above
 constexpr int kPoolRoom = 2;                                     // powers of two that scales may grow before the exponent changes
 
-// How a workgroup goes through its blocks of rows (see there), and what is the same in all lanes then in scalar registers.  Not so in the causal form above 192
-// dimensions: in the registers that are left there its loop takes 6 % longer for it (8192 new tokens behind 8192, 2 query heads to each of 4: 947 -> 1010 us).
+// How a workgroup goes through its blocks of rows (see there), and what is the same in all lanes then in scalar registers.  Not so in the causal form
+// above 192 dimensions: in the registers that are left there its loop takes 6 % longer for it (8192 new tokens behind 8192, 2 query heads to each of
+// 4: 947 -> 1010 us).
 template <int D, int FORM> constexpr bool kPoolWalk = FORM != kPoolCausal || D <= 192;
 template <bool WALK> __device__ __forceinline__ int pool_same(int x) { return WALK ? __builtin_amdgcn_readfirstlane(x) : x; }
 template <bool WALK> __device__ __forceinline__ pool_view pool_same(pool_view v) {
@@ -43,8 +47,9 @@ template <bool WALK, int FORM> __device__ __forceinline__ pool_gap<FORM> pool_sa
     return g;
 }
 
-// Rows end with the matrix by way of LDS (pool_finish_together) where segments are short, in the sliding form, and registers allow it: at 192 dimensions and more the
-// loop spills for it.  8192 tokens, 4 query heads to each of 8, that see 64: 164 us, now 153 (d = 128), that see 1024: 300, now 288; d = 160, 4 heads: 127 and 118.
+// Rows end with the matrix by way of LDS (pool_finish_together) where segments are short, in the sliding form, and registers allow it: at 192
+// dimensions and more the loop spills for it.  8192 tokens, 4 query heads to each of 8, that see 64: 164 us, now 153 (d = 128), that see 1024: 300,
+// now 288; d = 160, 4 heads: 127 and 118.
 template <int D, int FORM> constexpr bool kPoolTogether = FORM == kPoolSliding && D <= 160;
 
 template <int D, int BITS, int FORM>
@@ -80,8 +85,9 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
     const uint32_t off_code = (u_key & 15) * CB + u_at * (int)sizeof(code_t), off_scale = 4 * ((u_key & 15) * n_scales + 16 * u_at / a.g);
     unsigned char *const k_dst = k_lds[0] + u_key * KROW + 32 * u_at, *const v_dst = v_lds[0] + u_key * VROW + 32 * u_at;    // in the first buffer
 
-    // The block of rows that a share begins in is found by a lane each, and the next ones in their order.  (Found by counting from a key head's first one
-    // every time, 8192 new tokens that see 64, 8 query heads to each of 4 of 64 channels, took 388 us, now 118; that see 1024, 4 to each of 8 of 128, 394, now 291.)
+    // The block of rows that a share begins in is found by a lane each, and the next ones in their order.  (Found by counting from a key head's first
+    // one every time, 8192 new tokens that see 64, 8 query heads to each of 4 of 64 channels, took 388 us, now 118; that see 1024, 4 to each of 8 of
+    // 128, 394, now 291.)
     int seq = pool_sequence_of(a.chunk_before, n_seq, unit), head = 0, rt = 0, t0 = 0, blocks = 0, tiles = 0;
     pool_view view;
     const auto take = [&]() __attribute__((always_inline)) {
@@ -175,7 +181,8 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
             floatx16 s[KB];
             const unsigned char* const kr = &k_lds[buffer][l32 * KROW + 16 * half];
             const unsigned char* const vr = &v_lds[buffer][(4 * half + (lane & 15) / 4) * VROW + (16 * (lane >> 4 & 1) + 4 * (lane & 3)) * 2];
-            // Both products read their operands kPoolAhead matrix instructions ahead; the fences keep the compiler from moving the reads to their uses.
+            // Both products read their operands kPoolAhead matrix instructions ahead; the fences keep the compiler from moving the reads to their
+            // uses.
             half8 f[kPoolAhead];
             const auto read_k = [&](int j) __attribute__((always_inline)) {          // of the scores' j-th: block of keys j % KB, channels from 16 (j / KB) on
                 return __builtin_bit_cast(half8, *reinterpret_cast<const uint4*>(kr + 32 * (j % KB) * KROW + 32 * (j / KB)));
@@ -258,7 +265,8 @@ __global__ void __launch_bounds__(64 * kPoolChunkWaves, 2) srft_pool_chunk_kerne
                 for (int i = 0; i < N; ++i) {
                     typedef __attribute__((address_space(1))) const char* global_t;
                     const auto load = [&](const void* base, uint64_t bytes, uint32_t off, auto* to) __attribute__((always_inline)) {
-                        // a scalar address for each block (the asm keeps the compiler from adding a lane's offset to the base, a pair of registers for each array)
+                        // a scalar address for each block (the asm keeps the compiler from adding a lane's offset to the base, a pair of registers
+                        // for each array)
                         global_t p0 = (global_t)base + at[0] * bytes, p1 = p0;
                         if constexpr (!ONE) p1 = (global_t)base + at[1] * bytes;
                         asm("" : "+s"(p0));

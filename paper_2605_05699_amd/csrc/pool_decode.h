@@ -4,10 +4,10 @@
 // Bound by the chain of a tile in a wavefront, its loads, decoding and products one after the other: 24 sequences up to 32,768 tokens, 8 key heads
 // of 128 channels, 4 bits: 388 MB in 112 us, 3.5 TB/s, where a kernel that only reads gets 6.2 to 6.5 (62 us).  The vector ALU is busy for 54 % of a
 // SIMD's clocks (66 % of a wavefront's life), the matrix unit for 14 %; neither they nor the bytes bind alone, and two wavefronts a SIMD, which
-// is what the registers leave, do not cover each other's waits.  Codes are loaded past the L2, where nobody reads them again: 6 % slower without that.  A wavefront has
-// a tile of KEYS keys to itself, keys on the rows of the score product and 16 query rows on its columns (16x16x32; CB blocks of
-// them): a lane holds, for ITS row (lane % 16), the keys of its quarter of the wavefront (lane / 16), which is what the running maximum
-// and sum want and what the product with the values takes as its B operand.  Scores and weights stay in registers.
+// is what the registers leave, do not cover each other's waits.  Codes are loaded past the L2, where nobody reads them again: 6 % slower without
+// that.  A wavefront has a tile of KEYS keys to itself, keys on the rows of the score product and 16 query rows on its columns (16x16x32; CB blocks
+// of them): a lane holds, for ITS row (lane % 16), the keys of its quarter of the wavefront (lane / 16), which is what the running maximum and sum
+// want and what the product with the values takes as its B operand.  Scores and weights stay in registers.
 //   scores: one group of 32 channels a step, the codes (exact in fp16) against q' as fp16 hi + lo, and the group's scale on the result in
 //           fp32: no rounding but fp32's.  (The codes themselves, not the 1024 + code that half of the decoding gives: what the offsets add up to
 //           is a thousand times the queries' sum, in whose last bits a group is lost whose large queries meet small codes.)
@@ -159,16 +159,23 @@ __device__ __forceinline__ uint32_t pool_product2(float a, float f, float b, flo
 // above, one wavefront is left, and asking for two is faster as long as that spills no more than some 40 registers.  Formats that do, groups of
 // 16, 32 and d: 8 bits, d = 96 in groups of 16 199 / 156; d = 128 248 / 193, 183 / 161, 180 / 159; d = 192 with one group 260 / 225;
 // d = 224 418 / 328, 335 / 278, 320 / 276; d = 256 472 / 380, 371 / 311, 359 / 309; 4 bits, d = 224 with one group 293 / 227.  With two blocks
-// of rows (24 rows a key head): 8 bits, d = 96 in groups of 16 289 / 211, d = 128 in groups of 32 280 / 211, with one 279 / 212; 4 bits, the same three
-// 282 / 196, 274 / 187, 275 / 187.  Beyond 40: d = 128 in groups of 16, two blocks, at 4 bits (87 spilled) 332 / 414, at 8 (120) 361 / 566.
+// of rows (24 rows a key head): 8 bits, d = 96 in groups of 16 289 / 211, d = 128 in groups of 32 280 / 211, with one 279 / 212; 4 bits, the same
+// three 282 / 196, 274 / 187, 275 / 187.  Beyond 40: d = 128 in groups of 16, two blocks, at 4 bits (87 spilled) 332 / 414, at 8 (120) 361 / 566.
 // (All formats: profiles/pool_decode_registers.txt.)
+// The table is the causal form's.  The sliding and shared forms take up to 17 registers more and end above where causal does not in the formats
+// named here, d / channels to a scale / bits: one wavefront is left there.  The whole call, us, with one (with two asked for, which spills up to 9):
+// sliding, 24 sequences up to 32,768 tokens that see 4096 + 64, 8 rows a key head, 160/160/4 74 (62), 256/256/4 107 (86), 192/16/8 113 (93),
+// 192/32/8 92 (80), 96/32/8 52 (48), 96/96/8 51 (46), with 24 rows 80 (63); shared, 31 samples of 5 prompts up to 5000 tokens, 4 rows, 128/16/4
+// 39 (42), 224/32/4 61 (62), 256/256/4 66 (69), 160/16/8 50 (48), 192/16/8 56 (53), 192/32/8 54 (51), 96/32/8 35 (38), 96/96/8 35 (38), with 24
+// rows 64 (63) and 64 (64).
 constexpr int pool_decode_waves(int d, int bits, int cb, int gm) {
     if (cb == 2) return d == (gm == kGroup16 ? 96 : 128) ? 2 : 1;
     if (bits == 4) return d == 224 && gm == kGroupWide ? 2 : 1;
     return d == 128 || d >= 224 || (d == 96 && gm == kGroup16) || (d == 192 && gm == kGroupWide) ? 2 : 1;
 }
 // Whether a segment's first tile is asked for before its queries are in LDS (4 bits, groups of 32, with / without: d = 64 84 / 85, 96 104 / 107,
-// 160 147 / 148).  Not where the registers are full: at d = 128 one wavefront is left with it (149 / 123), nor above 160 (256: 209 -> 291 when it was tried).
+// 160 147 / 148).  Not where the registers are full: at d = 128 one wavefront is left with it (149 / 123), nor above 160 (256: 209 -> 291 when it was
+// tried).
 constexpr bool pool_decode_early(int d, int bits, int cb, int gm) { return pool_decode_waves(d, bits, cb, gm) == 1 && d <= 160 && d != 128; }
 template <int D, int BITS, int CB, int GM, int FORM>
 __global__ void __launch_bounds__(64 * kPoolTeam, pool_decode_waves(D, BITS, CB, GM)) srft_pool_decode_kernel(const pool_attention_args a) {
@@ -704,7 +711,8 @@ struct pool_common {
     __device__ __forceinline__ const float* heads(const float* part, int r) const {
         return chunk ? part + 32 * D + 4 * (r % kPoolBlock) : part + 16 * D + 4 * (r % 16);
     }
-    // 4 of the 16 channels of block c of row r: those from 4 quarter on; of pool_chunk by position, unit quarter / 2 of two and half of it quarter % 2
+    // 4 of the 16 channels of block c of row r: those from 4 quarter on; of pool_chunk by position, unit quarter / 2 of two and half of it quarter %
+    // 2
     __device__ __forceinline__ floatx4 channels(const float* part, int r, int c, int quarter) const {
         return reinterpret_cast<const floatx4*>(part)[chunk ? (2 * c + (quarter >> 1)) * 64 + 32 * (quarter & 1) + r % kPoolBlock : c * 64 + 16 * quarter + r % 16];
     }
